@@ -355,6 +355,127 @@ rs_status rs_route_static(const float *d_logits, int32_t n, int32_t vocab,
                           const float *d_logit_scale, float tau, int32_t active,
                           rs_route_out *d_out, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Caches in pages, for callers that run attention themselves and whose
+ * sequences are too uneven for slots of max_ctx positions: rotary rows, the rows
+ * of a QKV projection into the pages, and attention of new tokens over them.
+ * The spans of a call are named as in rs_catchup_prefill: sequence b brings rows
+ * d_span_offset[b] .. d_span_offset[b+1]) at positions d_pos0[b], d_pos0[b]+1, ...
+ * of the sequence whose page table row is d_seq_slot[b].
+ *
+ * One layer's cache.  Position p of a slot lies in page page_table[slot][p /
+ * page_size] at place p % page_size; K and V of a position as rs_kv_bytes
+ * describes them, page by page (with page_size = max_ctx and one page per slot
+ * it is that layout). */
+typedef struct rs_paged_kv {
+    void          *k;            /* DEVICE bf16 [n_pages][n_kv_heads][page_size][head_dim]    */
+    void          *v;            /* DEVICE bf16 [n_pages][n_kv_heads][head_dim][page_size]    */
+    const int32_t *page_table;   /* DEVICE int32 [n_slots][max_pages]; an entry that no call needs may hold anything */
+    int32_t n_pages;             /* >= 1                                                      */
+    int32_t page_size;           /* a power of two, 16 .. 1024                                */
+    int32_t n_slots;             /* >= 1                                                      */
+    int32_t max_pages;           /* >= 1; page_size * max_pages <= 2^30                       */
+    int32_t n_kv_heads;          /* >= 1                                                      */
+    int32_t head_dim;            /* 32, 64 or 128                                             */
+} rs_paged_kv;
+
+/* Element types of q, k, v and outputs. */
+#define RS_F32   0
+#define RS_BF16  1
+
+/* A rotary embedding: pair i of a head's first rot_dim channels is turned by the
+ * angle position * d_inv_freq[i] (computed in double) and multiplied by
+ * amplitude; the other channels pass unchanged. */
+typedef struct rs_rope {
+    int32_t rot_dim;             /* multiple of 8, 8 .. head_dim                              */
+    int32_t interleaved;         /* 0: pairs (i, i + rot_dim / 2); 1: pairs (2 i, 2 i + 1)    */
+    const double *d_inv_freq;    /* DEVICE double [rot_dim / 2]                               */
+    float   amplitude;           /* finite; 1 for an unscaled embedding                       */
+} rs_rope;
+
+/* Frequencies of a rotary embedding, on the host: base frequency i is
+ * theta^(-2 i / rot_dim).
+ *   RS_ROPE_PLAIN    the base frequencies, amplitude 1 (factor is ignored)
+ *   RS_ROPE_LINEAR   divided by factor (positions interpolated), amplitude 1
+ *   RS_ROPE_BY_PARTS (arXiv 2309.00071) a wavelength of which beta_fast or more fit
+ *                    original_ctx stays, one of which at most beta_slow fit is
+ *                    divided by factor, between the two linearly in the number
+ *                    that fit; amplitude 0.1 ln(factor) + 1
+ * h_inv_freq: HOST double [rot_dim / 2]; h_amplitude: HOST float or NULL.
+ * Errors: RS_EINVAL (rot_dim no positive even number, theta <= 1, factor < 1, original_ctx < 1,
+ * beta_fast <= beta_slow, unknown kind, null pointer). */
+#define RS_ROPE_PLAIN    0
+#define RS_ROPE_LINEAR   1
+#define RS_ROPE_BY_PARTS 2
+rs_status rs_rope_frequencies(int32_t rot_dim, double theta, int32_t kind, double factor,
+                              double original_ctx, double beta_fast, double beta_slow,
+                              double *h_inv_freq, float *h_amplitude);
+
+/* Rotate n_rows rows of n_heads heads to their positions.
+ *   d_pos      DEVICE int32 [n_rows], any value
+ *   dtype      RS_F32 or RS_BF16: type of d_x and d_out; the rotation is computed in fp32 and rounded once
+ *   d_x        DEVICE [n_rows][n_heads][head_dim]; rows x_stride elements apart, heads back to back
+ *   inverse    1: by the negative angle (what a gradient passing back through the rotation needs, and, divided by
+ *              amplitude squared, what takes a rotation off again)
+ *   d_out      DEVICE, rows out_stride elements apart; may be d_x itself if the strides are equal, and may not
+ *              overlap it otherwise
+ * head_dim is a multiple of 8, at most 1024; pointers are 16-byte aligned and strides multiples of 16 bytes.
+ * Errors: RS_EINVAL, RS_EHIP. */
+rs_status rs_rope_rows(const rs_rope *rope, int32_t n_rows, const int32_t *d_pos, int32_t dtype,
+                       int32_t n_heads, int32_t head_dim, const void *d_x, int64_t x_stride,
+                       int32_t inverse, void *d_out, int64_t out_stride, void *stream);
+
+/* The rows of a QKV projection: q rotated to its position into d_q_out, k
+ * rotated and rounded to bf16 into the K pages, v rounded into the V pages.
+ *   n_seqs, n_rows  1 <= n_seqs <= 1024, n_rows >= 1: rows the buffers hold; rows at or past the last span's end
+ *                   are neither read nor written
+ *   d_seq_slot      DEVICE int32 [n_seqs]; spans of one slot must not share positions
+ *   d_span_offset   DEVICE int32 [n_seqs + 1], non-decreasing, 0 <= entries <= n_rows (a span may be empty), or
+ *                   NULL: one row for each sequence (n_rows >= n_seqs)
+ *   d_pos0          DEVICE int32 [n_seqs]
+ *   rope            NULL: nothing is rotated
+ *   dtype           RS_F32 or RS_BF16: type of q, k, v and q_out
+ *   d_q, d_k, d_v   DEVICE [n_rows][heads][head_dim], rows a stride (elements) apart, heads back to back: three
+ *                   buffers, or three places in the rows of one; n_q_heads >= 1 (any number), cache->n_kv_heads
+ *   d_q_out         DEVICE; may be d_q itself if the strides are equal
+ *   d_flags         DEVICE uint32 [n_seqs] or NULL: RS_FLAG_BADARG is or-ed into the word of a sequence with a slot, span
+ *                   or position out of range, whose rows are all skipped, or with a row whose page is no page of
+ *                   the cache, which is skipped; nothing else is written (the caller clears the words)
+ * pointers are 16-byte aligned and strides multiples of 16 bytes.
+ * Errors: RS_EINVAL, RS_ECAPACITY (n_seqs), RS_EHIP. */
+rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows,
+                          const int32_t *d_seq_slot, const int32_t *d_span_offset, const int32_t *d_pos0,
+                          const rs_rope *rope, int32_t dtype, int32_t n_q_heads,
+                          const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride,
+                          const void *d_v, int64_t v_stride, void *d_q_out, int64_t q_out_stride,
+                          uint32_t *d_flags, void *stream);
+
+/* Attention of the rows of each span over their sequence's pages: the row at
+ * position p sees the positions max(0, p - window + 1) .. p (window 0: 0 .. p),
+ * its own and those of the span before it among them: append first.  Query head
+ * h reads KV head h / (n_q_heads / n_kv_heads).
+ *   out = sum_j softmax_j(scale q . k_j) v_j;  lse = ln sum_j exp(scale q . k_j)
+ *   n_seqs .. d_pos0  as in rs_paged_append (slots may repeat: nothing is written to the cache)
+ *   dtype             type of d_q and d_out.  Sums are fp32.  RS_F32: products of fp32 q and fp32 probabilities with the
+ *                     bf16 cache, exact to fp32; RS_BF16: probabilities may be rounded to bf16 for the matrix cores
+ *   n_q_heads         a multiple of n_kv_heads, at most 16 times as many
+ *   scale             > 0, finite
+ *   window            >= 0
+ *   d_out             DEVICE [n_rows][n_q_heads][head_dim], rows out_stride elements apart; must not overlap d_q
+ *   d_lse             DEVICE fp32 [n_rows][n_q_heads] or NULL
+ *   d_flags           as in rs_paged_append; a sequence out of range has its rows skipped, one that sees a position
+ *                     whose page is no page of the cache is computed with some other page in its place
+ *   d_scratch         DEVICE, 256-byte aligned, of at least rs_paged_attention_scratch_bytes (0 on a bad argument) for these
+ *                     counts; any content.  Calls and graph replays that overlap must not share it
+ * What lies in the pages at positions that no row sees may be anything, NaN too.
+ * Errors: RS_EINVAL, RS_ECAPACITY (n_seqs), RS_EHIP. */
+size_t    rs_paged_attention_scratch_bytes(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, int32_t n_q_heads);
+rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows,
+                             const int32_t *d_seq_slot, const int32_t *d_span_offset, const int32_t *d_pos0,
+                             int32_t dtype, int32_t n_q_heads, const void *d_q, int64_t q_stride,
+                             float scale, int32_t window, void *d_out, int64_t out_stride, float *d_lse,
+                             uint32_t *d_flags, void *d_scratch, size_t scratch_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -42,6 +42,15 @@ class _RsWeights(C.Structure):
         (n, C.POINTER(C.c_void_p)) for n in ("attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")]
 
 
+class _RsPagedKv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p)] + [(n, C.c_int32) for n in (
+        "n_pages", "page_size", "n_slots", "max_pages", "n_kv_heads", "head_dim")]
+
+
+class _RsRope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("d_inv_freq", C.c_void_p), ("amplitude", C.c_float)]
+
+
 class _RsRouterWeights(C.Structure):
     _fields_ = [("d", C.c_int32), ("r", C.c_int32), ("ln_eps", C.c_float)] + [
         (n, C.POINTER(C.c_void_p)) for n in ("w1", "b1", "w2", "b2")] + [
@@ -55,7 +64,7 @@ def _load() -> C.CDLL:
             f"{path} is missing: build it first (python -c 'import __graft_entry__ as g; g.build()' "
             "or python paper_2507_17307_amd/build.py). There is no fallback path.")
     lib = C.CDLL(path)
-    vp, i32, f32, sz = C.c_void_p, C.c_int32, C.c_float, C.c_size_t
+    vp, i32, i64, f32, f64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_double, C.c_size_t
     lib.rs_last_error.restype = C.c_char_p
     lib.rs_last_error.argtypes = []
     lib.rs_abi_version.restype = i32
@@ -84,6 +93,16 @@ def _load() -> C.CDLL:
     lib.rs_route_static.argtypes = [vp, i32, i32, vp, f32, i32, vp, vp]
     lib.rs_stitch_generate.restype = i32
     lib.rs_stitch_generate.argtypes = [vp, vp, i32, vp, i32, i32, i32, i32, vp, f32, i32, vp, i32, vp, vp]
+    lib.rs_rope_frequencies.restype = i32
+    lib.rs_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp, vp]
+    lib.rs_rope_rows.restype = i32
+    lib.rs_rope_rows.argtypes = [C.POINTER(_RsRope), i32, vp, i32, i32, i32, vp, i64, i32, vp, i64, vp]
+    lib.rs_paged_append.restype = i32
+    lib.rs_paged_append.argtypes = [C.POINTER(_RsPagedKv), i32, i32, vp, vp, vp, C.POINTER(_RsRope), i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]
+    lib.rs_paged_attention_scratch_bytes.restype = sz
+    lib.rs_paged_attention_scratch_bytes.argtypes = [C.POINTER(_RsPagedKv), i32, i32, i32]
+    lib.rs_paged_attention.restype = i32
+    lib.rs_paged_attention.argtypes = [C.POINTER(_RsPagedKv), i32, i32, vp, vp, vp, i32, i32, vp, i64, f32, i32, vp, i64, vp, vp, vp, sz, vp]
     lib.rs_set_spin_limit.restype = i32
     lib.rs_set_spin_limit.argtypes = [vp, C.c_uint32]
     lib.rs_set_phase_timer.restype = i32
@@ -217,6 +236,130 @@ def rs_stitch_generate(slm: int, llm: int, seq_slot: int, d_seq, n_prompt: int, 
 
 def rs_set_sampling(handle: int, enabled: bool, key: int = 0) -> None:
     _check(lib.rs_set_sampling(handle, int(bool(enabled)), key & 0xFFFFFFFFFFFFFFFF))
+
+
+# ------------------------------------------------------------------ caches in pages
+RS_F32, RS_BF16 = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BY_PARTS = range(3)
+_ROW_TYPES = {torch.float32: RS_F32, torch.bfloat16: RS_BF16}
+
+
+def _rows(name: str, t: torch.Tensor, device: torch.device):
+    """(address, row stride) of a tensor [rows, heads, channels] whose heads lie back to back; the C side checks the rest."""
+    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError(f"{name} must be [rows, heads, head_dim] with the heads of a row back to back, not {tuple(t.shape)} with strides {t.stride()}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the call's other tensors on {device}")
+    return t.data_ptr(), t.stride(0)
+
+
+def _ints(name: str, t: Optional[torch.Tensor], n: int, device: torch.device) -> Optional[int]:
+    """Address of n 32-bit integers."""
+    if t is None:
+        return None
+    if t.dtype not in (torch.int32, torch.uint32) or not t.is_contiguous() or t.numel() < n or t.device != device:
+        raise ValueError(f"{name} must hold {n} contiguous 32-bit integers on {device}")
+    return t.data_ptr()
+
+
+def _device_stream(device: torch.device, stream) -> Optional[int]:
+    """The launch goes to the current device, which has to be the tensors' own."""
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, not on {device}")
+    if _raw_device is not None and _raw_device() != device.index or _raw_device is None and torch.cuda.current_device() != device.index:
+        raise ValueError(f"tensors are on {device}, which is not the current device")
+    return _stream(stream)
+
+
+class PagedCache:
+    """Marshalled rs_paged_kv over one layer's tensors, which it keeps alive: k [n_pages, n_kv_heads, page_size, head_dim] and
+    v [n_pages, n_kv_heads, head_dim, page_size] bf16, page_table [n_slots, max_pages] int32, all contiguous on one device."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor):
+        if k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 or k.dim() != 4 or v.shape != (k.shape[0], k.shape[1], k.shape[3], k.shape[2]):
+            raise ValueError("k must be bf16 [pages, KV heads, positions, channels], v bf16 [pages, KV heads, channels, positions]")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2:
+            raise ValueError("page_table must be int32 [slots, pages]")
+        if not (k.is_contiguous() and v.is_contiguous() and page_table.is_contiguous()) or not k.device == v.device == page_table.device:
+            raise ValueError("k, v and page_table must be contiguous and on one device")
+        self.k, self.v, self.page_table, self.device = k, v, page_table, k.device
+        self.n_kv_heads, self.page_size, self.head_dim = k.shape[1], k.shape[2], k.shape[3]
+        self.struct = _RsPagedKv(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), k.shape[0], k.shape[2], page_table.shape[0],
+                                 page_table.shape[1], k.shape[1], k.shape[3])
+
+
+class Rope:
+    """Marshalled rs_rope over its frequencies (float64 [rot_dim / 2] on the GPU), which it keeps alive."""
+
+    def __init__(self, inv_freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0):
+        if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be contiguous float64 [rot_dim / 2]")
+        self.inv_freq, self.device = inv_freq, inv_freq.device
+        self.struct = _RsRope(2 * inv_freq.numel(), int(bool(interleaved)), inv_freq.data_ptr(), amplitude)
+
+
+def rs_rope_frequencies(rot_dim: int, theta: float, kind: int = ROPE_PLAIN, factor: float = 1.0, original_ctx: float = 32768.0,
+                        beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(float64 host tensor [rot_dim / 2], amplitude)."""
+    freq, amp = torch.empty(max(rot_dim, 0) // 2, dtype=torch.float64), C.c_float()
+    _check(lib.rs_rope_frequencies(rot_dim, theta, kind, factor, original_ctx, beta_fast, beta_slow, freq.data_ptr() or None, C.byref(amp)))
+    return freq, amp.value
+
+
+def rs_rope_rows(rope: Rope, d_pos: torch.Tensor, x: torch.Tensor, out: torch.Tensor, inverse: bool = False, stream=None) -> None:
+    """x, out: [rows, heads, head_dim] of one type (out may be x); d_pos: int32 [rows]."""
+    dev = x.device
+    if x.dtype not in _ROW_TYPES or out.dtype != x.dtype or out.shape != x.shape or rope.device != dev:
+        raise ValueError("x and out must be fp32 or bf16, of one type, shape and device, which is the frequencies' too")
+    px, sx = _rows("x", x, dev)
+    po, so = _rows("out", out, dev)
+    n, heads, hd = x.shape
+    _check(lib.rs_rope_rows(C.byref(rope.struct), n, _ints("d_pos", d_pos, n, dev), _ROW_TYPES[x.dtype], heads, hd, px, sx, int(bool(inverse)), po, so,
+                            _device_stream(dev, stream)))
+
+
+def _check_paged_rows(cache: PagedCache, n_rows: int, rows) -> None:
+    for name, t, heads in rows:
+        if t.dtype != rows[0][1].dtype or t.dtype not in _ROW_TYPES:
+            raise ValueError(f"{name} must be fp32 or bf16, as the call's other rows are")
+        if t.shape[0] < n_rows or t.shape[1] != heads or t.shape[2] != cache.head_dim:
+            raise ValueError(f"{name} must be at least [{n_rows}, {heads}, {cache.head_dim}], not {tuple(t.shape)}")
+
+
+def rs_paged_append(cache: PagedCache, n_seqs: int, n_rows: int, d_seq_slot, d_span_offset, d_pos0, rope: Optional[Rope], q, k, v, q_out,
+                    d_flags=None, stream=None) -> None:
+    """q, q_out: [rows, query heads, head_dim]; k, v: [rows, KV heads, head_dim]; views of one projection's rows do."""
+    dev = cache.device
+    (pq, sq), (pk, sk), (pv, sv), (po, so) = _rows("q", q, dev), _rows("k", k, dev), _rows("v", v, dev), _rows("q_out", q_out, dev)
+    nq, nkv = q.shape[1], cache.n_kv_heads
+    _check_paged_rows(cache, n_rows, (("q", q, nq), ("k", k, nkv), ("v", v, nkv), ("q_out", q_out, nq)))
+    if rope is not None and rope.device != dev:
+        raise ValueError(f"the frequencies are on {rope.device}, the cache on {dev}")
+    _check(lib.rs_paged_append(C.byref(cache.struct), n_seqs, n_rows, _ints("d_seq_slot", d_seq_slot, n_seqs, dev),
+                               _ints("d_span_offset", d_span_offset, n_seqs + 1, dev), _ints("d_pos0", d_pos0, n_seqs, dev),
+                               None if rope is None else C.byref(rope.struct), _ROW_TYPES[q.dtype], nq, pq, sq, pk, sk, pv, sv, po, so,
+                               _ints("d_flags", d_flags, n_seqs, dev), _device_stream(dev, stream)))
+
+
+def rs_paged_attention_scratch_bytes(cache: PagedCache, n_seqs: int, n_rows: int, n_q_heads: int) -> int:
+    return lib.rs_paged_attention_scratch_bytes(C.byref(cache.struct), n_seqs, n_rows, n_q_heads)
+
+
+def rs_paged_attention(cache: PagedCache, n_seqs: int, n_rows: int, d_seq_slot, d_span_offset, d_pos0, q, scale: float, window: int, out, d_lse, d_scratch,
+                       d_flags=None, stream=None) -> None:
+    """q, out: [rows, query heads, head_dim]; d_lse: fp32 [rows, query heads] or None; d_scratch: uint8."""
+    dev = cache.device
+    (pq, sq), (po, so) = _rows("q", q, dev), _rows("out", out, dev)
+    nq = q.shape[1]
+    _check_paged_rows(cache, n_rows, (("q", q, nq), ("out", out, nq)))
+    if d_lse is not None and (d_lse.dtype != torch.float32 or not d_lse.is_contiguous() or d_lse.numel() < n_rows * nq or d_lse.device != dev):
+        raise ValueError(f"d_lse must be contiguous fp32 [{n_rows}, {nq}] on {dev}")
+    if d_scratch is None or d_scratch.device != dev or not d_scratch.is_contiguous():
+        raise ValueError(f"d_scratch must be a contiguous tensor on {dev}")
+    _check(lib.rs_paged_attention(C.byref(cache.struct), n_seqs, n_rows, _ints("d_seq_slot", d_seq_slot, n_seqs, dev),
+                                  _ints("d_span_offset", d_span_offset, n_seqs + 1, dev), _ints("d_pos0", d_pos0, n_seqs, dev), _ROW_TYPES[q.dtype], nq, pq, sq,
+                                  scale, window, po, so, _ptr(d_lse), _ints("d_flags", d_flags, n_seqs, dev), d_scratch.data_ptr(),
+                                  d_scratch.numel() * d_scratch.element_size(), _device_stream(dev, stream)))
 
 
 PHASE_QKV, PHASE_OPROJ, PHASE_GATEUP, PHASE_DOWN, PHASE_LMHEAD, PHASE_ATTN = range(6)

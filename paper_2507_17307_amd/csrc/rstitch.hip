@@ -1267,3 +1267,5 @@ extern "C" rs_status rs_route_static(const float *d_logits, int32_t n, int32_t v
     if (rs_status rc = route_static_scratch(&ptr)) return rc;
     return launch_route(d_logits, n, vocab, d_logit_scale, tau, active, d_out, (rs::SoftPartial *)ptr, (hipStream_t)stream);
 }
+
+#include "paged_api.h"
