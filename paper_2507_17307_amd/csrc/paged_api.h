@@ -55,18 +55,49 @@ PagedSpans paged_spans(const rs_paged_kv *c, int32_t n_seqs, int32_t n_rows, con
     return s;
 }
 
-template <typename T, int HD>
-rs_status launch_paged_attention(const PagedAttnArgs &a, hipStream_t st) {
-    hipLaunchKernelGGL((k_paged_attention<T, HD>), dim3(a.s.n_rows, (a.n_q + 3) / 4), dim3(256), 0, st, a);
+// Which kernel takes a call: blocks of 16 or 32 columns where the spans have no more than that on average, else of 128.
+struct PagedShape { int cols, rows, runs; size_t odd, ml, o, total; };
+PagedShape paged_shape(int head_dim, int n_seqs, int n_rows, int group) {
+    PagedShape p{};
+    const long long slots = ((long long)n_rows * group + n_seqs - 1) / n_seqs;
+    p.cols = slots <= 16 ? 16 : slots <= 32 ? 32 : PAGED_COLS;
+    p.rows = p.cols / group;
+    p.runs = p.cols == PAGED_COLS ? PAGED_WIDE_RUNS : PAGED_NARROW_RUNS;
+    p.odd = align_up((size_t)p.runs * sizeof(int4));
+    p.ml = p.odd + align_up((size_t)p.runs * 4);
+    p.o = p.ml + align_up((size_t)2 * p.runs * 2 * p.cols * 4);
+    p.total = p.o + align_up((size_t)2 * p.runs * p.cols * head_dim * 4);
+    return p;
+}
+
+template <int HD, int PL, int COLS>
+rs_status launch_paged(const PagedAttnArgs &a, int runs, hipStream_t st) {
+    if constexpr (COLS == PAGED_COLS) hipLaunchKernelGGL((k_paged_wide<HD, PL>), dim3(runs), dim3(256), 0, st, a);
+    else {
+        constexpr size_t lds = paged_narrow_lds<HD, COLS / 16>();
+        if (rs_status rc = allow_lds<k_paged_narrow<HD, PL, COLS / 16>>(lds, "paged_narrow")) return rc;
+        hipLaunchKernelGGL((k_paged_narrow<HD, PL, COLS / 16>), dim3(runs), dim3(256), lds, st, a);
+    }
     RS_LAUNCHED("paged_attention");
+    constexpr int per = 1024 / HD;
+    hipLaunchKernelGGL((k_paged_join<HD, PL, COLS>), dim3(runs, (a.rows * a.group + per - 1) / per), dim3(256), 0, st, a);
+    RS_LAUNCHED("paged_join");
     return RS_OK;
 }
-template <typename T>
-rs_status launch_paged_attention_hd(int head_dim, const PagedAttnArgs &a, hipStream_t st) {
+template <int HD, int PL>
+rs_status launch_paged_cols(const PagedAttnArgs &a, const PagedShape &p, hipStream_t st) {
+    switch (p.cols) {
+        case 16: return launch_paged<HD, PL, 16>(a, p.runs, st);
+        case 32: return launch_paged<HD, PL, 32>(a, p.runs, st);
+        default: return launch_paged<HD, PL, PAGED_COLS>(a, p.runs, st);
+    }
+}
+template <int PL>
+rs_status launch_paged_hd(int head_dim, const PagedAttnArgs &a, const PagedShape &p, hipStream_t st) {
     switch (head_dim) {
-        case 32: return launch_paged_attention<T, 32>(a, st);
-        case 64: return launch_paged_attention<T, 64>(a, st);
-        default: return launch_paged_attention<T, 128>(a, st);
+        case 32: return launch_paged_cols<32, PL>(a, p, st);
+        case 64: return launch_paged_cols<64, PL>(a, p, st);
+        default: return launch_paged_cols<128, PL>(a, p, st);
     }
 }
 
@@ -166,7 +197,7 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
 size_t rs_paged_attention_scratch_bytes(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, int32_t n_q_heads) {
     if (const char *why = check_paged_attention(cache, n_q_heads)) { fail(RS_EINVAL, "%s", why); return 0; }
     if (n_seqs < 1 || n_rows < 1 || n_seqs > PAGED_MAX_SEQS || n_rows > (1 << 22)) { fail(RS_EINVAL, "n_seqs must be in 1..%d and n_rows in 1..2^22", PAGED_MAX_SEQS); return 0; }
-    return ALIGN;
+    return paged_shape(cache->head_dim, n_seqs, n_rows, n_q_heads / cache->n_kv_heads).total;
 }
 
 rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, const int32_t *d_seq_slot, const int32_t *d_span_offset,
@@ -184,12 +215,14 @@ rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n
     const size_t need = rs_paged_attention_scratch_bytes(cache, n_seqs, n_rows, n_q_heads);
     if (scratch_bytes < need) return fail(RS_EINVAL, "scratch of %zu bytes is smaller than the %zu needed", scratch_bytes, need);
     PagedAttnArgs a{};
+    const PagedShape p = paged_shape(hd, n_seqs, n_rows, n_q_heads / cache->n_kv_heads);
     a.s = paged_spans(cache, n_seqs, n_rows, d_seq_slot, d_span_offset, d_pos0, d_flags);
     a.kc = (const uint16_t *)cache->k; a.vc = (const uint16_t *)cache->v;
     a.q = d_q; a.out = d_out; a.lse = d_lse; a.q_stride = q_stride; a.out_stride = out_stride;
-    a.n_q = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.window = window;
+    a.n_q = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.window = window; a.rows = p.rows;
     a.c = scale * 1.44269504088896341f;
-    return dtype == RS_F32 ? launch_paged_attention_hd<float>(hd, a, (hipStream_t)stream) : launch_paged_attention_hd<uint16_t>(hd, a, (hipStream_t)stream);
+    a.cuts = (int4 *)d_scratch; a.odd = (unsigned int *)((unsigned char *)d_scratch + p.odd); a.part_ml = (float *)((unsigned char *)d_scratch + p.ml); a.part_o = (float *)((unsigned char *)d_scratch + p.o);
+    return dtype == RS_F32 ? launch_paged_hd<3>(hd, a, p, (hipStream_t)stream) : launch_paged_hd<1>(hd, a, p, (hipStream_t)stream);
 }
 
 }  // extern "C"

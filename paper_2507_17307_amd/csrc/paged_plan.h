@@ -37,4 +37,43 @@ RS_HD int append_blocks_most(int n_seqs, int n_rows) {
     return few < n_rows ? few : n_rows;
 }
 
+// ------------------------------------------------------------------------------------------------
+// Split of an attention call.  An item is a block of `rows` rows of one span (what the columns of a workgroup's tiles hold, times the query
+// heads of a KV head) and one KV head; its work are the tiles of positions that some row of the block sees.  Items are counted
+// sequence by sequence, KV head by KV head, block by block; the tiles of all items in that order are dealt to the workgroups in equal
+// runs, whatever the spans and contexts are.  A run may start and end inside an item: what is cut is joined by a second kernel.
+// ------------------------------------------------------------------------------------------------
+RS_HD int paged_blocks(const Span &s, int rows) { return (s.m + rows - 1) / rows; }
+
+// Positions lo .. hi - 1 that rows r0 .. r1 - 1 of the span see between them.
+RS_HD void paged_seen(const Span &s, int r0, int r1, int window, int &lo, int &hi) {
+    const int first = s.p0 + r0;
+    lo = window > 0 && first >= window ? first - window + 1 : 0;
+    hi = s.p0 + r1;
+}
+
+// Tiles t0 .. t1 - 1 of block j.
+RS_HD void paged_tiles(const Span &s, int rows, int window, int tile_shift, int j, int &t0, int &t1) {
+    int lo, hi;
+    const int r0 = j * rows, r1 = r0 + rows < s.m ? r0 + rows : s.m;
+    paged_seen(s, r0, r1, window, lo, hi);
+    t0 = lo >> tile_shift; t1 = ((hi - 1) >> tile_shift) + 1;
+}
+
+// First tile of run w of W over T tiles (no product beyond T).
+RS_HD long long paged_run(long long T, int W, int w) { return T / W * w + T % W * w / W; }
+
+// The run that tile t < T is in.
+RS_HD int paged_run_of(long long T, int W, long long t) {
+    int lo = 0, hi = W - 1;
+    while (lo < hi) { const int mid = (lo + hi) / 2; if (paged_run(T, W, mid + 1) > t) hi = mid; else lo = mid + 1; }
+    return lo;
+}
+
+// Runs that T tiles are dealt to: `most` of them, fewer where a run would get less than `least` tiles.
+RS_HD int paged_runs(long long T, int most, int least) {
+    const long long n = (T + least - 1) / least;
+    return n < 1 ? 1 : n < most ? (int)n : most;
+}
+
 }  // namespace rs
