@@ -56,13 +56,14 @@ PagedSpans paged_spans(const rs_paged_kv *c, int32_t n_seqs, int32_t n_rows, con
 }
 
 // Which kernel takes a call: blocks of 16 or 32 columns where the spans have no more than that on average, else of 128.
-struct PagedShape { int cols, rows, runs; size_t odd, ml, o, total; };
-PagedShape paged_shape(int head_dim, int n_seqs, int n_rows, int group) {
+struct PagedShape { int cols, rows, runs; long long items; size_t odd, ml, o, total; };
+PagedShape paged_shape(int head_dim, int n_seqs, int n_rows, int group, int n_kv) {
     PagedShape p{};
     const long long slots = ((long long)n_rows * group + n_seqs - 1) / n_seqs;
     p.cols = slots <= 16 ? 16 : slots <= 32 ? 32 : PAGED_COLS;
     p.rows = p.cols / group;
     p.runs = p.cols == PAGED_COLS ? PAGED_WIDE_RUNS : PAGED_NARROW_RUNS;
+    p.items = ((long long)n_rows / p.rows + n_seqs) * n_kv;                     // at most
     p.odd = align_up((size_t)p.runs * sizeof(int4));
     p.ml = p.odd + align_up((size_t)p.runs * 4);
     p.o = p.ml + align_up((size_t)2 * p.runs * 2 * p.cols * 4);
@@ -71,25 +72,23 @@ PagedShape paged_shape(int head_dim, int n_seqs, int n_rows, int group) {
 }
 
 template <int HD, int PL, int COLS>
-rs_status launch_paged(const PagedAttnArgs &a, int runs, hipStream_t st) {
-    if constexpr (COLS == PAGED_COLS) hipLaunchKernelGGL((k_paged_wide<HD, PL>), dim3(runs), dim3(256), 0, st, a);
-    else {
-        constexpr size_t lds = paged_narrow_lds<HD, COLS / 16>();
-        if (rs_status rc = allow_lds<k_paged_narrow<HD, PL, COLS / 16>>(lds, "paged_narrow")) return rc;
-        hipLaunchKernelGGL((k_paged_narrow<HD, PL, COLS / 16>), dim3(runs), dim3(256), lds, st, a);
-    }
+rs_status launch_paged(const PagedAttnArgs &a, const PagedShape &p, hipStream_t st) {
+    if constexpr (COLS == PAGED_COLS) hipLaunchKernelGGL((k_paged_wide<HD, PL>), dim3(p.runs), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_paged_narrow<HD, PL, COLS / 16>), dim3(p.runs), dim3(64), 0, st, a);
     RS_LAUNCHED("paged_attention");
-    constexpr int per = 1024 / HD;
-    hipLaunchKernelGGL((k_paged_join<HD, PL, COLS>), dim3(runs, (a.rows * a.group + per - 1) / per), dim3(256), 0, st, a);
+    // about 2048 workgroups for the items that can be cut (one a run at most); the others end at once
+    constexpr int per = join_cols<HD, COLS>();
+    const int cut = p.items < p.runs ? (int)p.items : p.runs, most = (a.rows * a.group + per - 1) / per, want = (2048 + cut - 1) / cut;
+    hipLaunchKernelGGL((k_paged_join<HD, PL, COLS>), dim3(p.runs, want < most ? want : most), dim3(256), 0, st, a);
     RS_LAUNCHED("paged_join");
     return RS_OK;
 }
 template <int HD, int PL>
 rs_status launch_paged_cols(const PagedAttnArgs &a, const PagedShape &p, hipStream_t st) {
     switch (p.cols) {
-        case 16: return launch_paged<HD, PL, 16>(a, p.runs, st);
-        case 32: return launch_paged<HD, PL, 32>(a, p.runs, st);
-        default: return launch_paged<HD, PL, PAGED_COLS>(a, p.runs, st);
+        case 16: return launch_paged<HD, PL, 16>(a, p, st);
+        case 32: return launch_paged<HD, PL, 32>(a, p, st);
+        default: return launch_paged<HD, PL, PAGED_COLS>(a, p, st);
     }
 }
 template <int PL>
@@ -197,7 +196,7 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
 size_t rs_paged_attention_scratch_bytes(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, int32_t n_q_heads) {
     if (const char *why = check_paged_attention(cache, n_q_heads)) { fail(RS_EINVAL, "%s", why); return 0; }
     if (n_seqs < 1 || n_rows < 1 || n_seqs > PAGED_MAX_SEQS || n_rows > (1 << 22)) { fail(RS_EINVAL, "n_seqs must be in 1..%d and n_rows in 1..2^22", PAGED_MAX_SEQS); return 0; }
-    return paged_shape(cache->head_dim, n_seqs, n_rows, n_q_heads / cache->n_kv_heads).total;
+    return paged_shape(cache->head_dim, n_seqs, n_rows, n_q_heads / cache->n_kv_heads, cache->n_kv_heads).total;
 }
 
 rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, const int32_t *d_seq_slot, const int32_t *d_span_offset,
@@ -215,7 +214,7 @@ rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n
     const size_t need = rs_paged_attention_scratch_bytes(cache, n_seqs, n_rows, n_q_heads);
     if (scratch_bytes < need) return fail(RS_EINVAL, "scratch of %zu bytes is smaller than the %zu needed", scratch_bytes, need);
     PagedAttnArgs a{};
-    const PagedShape p = paged_shape(hd, n_seqs, n_rows, n_q_heads / cache->n_kv_heads);
+    const PagedShape p = paged_shape(hd, n_seqs, n_rows, n_q_heads / cache->n_kv_heads, cache->n_kv_heads);
     a.s = paged_spans(cache, n_seqs, n_rows, d_seq_slot, d_span_offset, d_pos0, d_flags);
     a.kc = (const uint16_t *)cache->k; a.vc = (const uint16_t *)cache->v;
     a.q = d_q; a.out = d_out; a.lse = d_lse; a.q_stride = q_stride; a.out_stride = out_stride;

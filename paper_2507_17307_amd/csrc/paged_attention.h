@@ -24,8 +24,8 @@ namespace rs {
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int PAGED_COLS = 128;                // columns of a workgroup of k_paged_wide
-constexpr int PAGED_WIDE_TILE = 6, PAGED_NARROW_TILE = 5;      // log2 positions of a tile
-constexpr int PAGED_WIDE_RUNS = 512, PAGED_NARROW_RUNS = 1024, PAGED_NARROW_LEAST = 4;
+constexpr int PAGED_TILE = 6;                  // log2 positions of a tile
+constexpr int PAGED_WIDE_RUNS = 512, PAGED_NARROW_RUNS = 1024;
 
 struct PagedAttnArgs {
     PagedSpans s;
@@ -44,77 +44,86 @@ struct PagedRun { PagedItem at; int ta; long long left, T; int W; };       // fi
 
 constexpr int PAGED_RUN_LDS = 8;               // long long
 
-// What run w has to do; false: nothing.  All threads of the workgroup (256) get the same.  sh: PAGED_RUN_LDS long long.
-__device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int tile_shift, int most, int least, int w, long long *sh, PagedRun &run) {
+// What run w of `most` has to do; false: nothing.  All NT threads of the workgroup get the same.  sh: PAGED_RUN_LDS long long (one wave: not used).
+template <int NT>
+__device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int most, int w, long long *sh, PagedRun &run) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.s.n_seqs;
     // tiles per KV head of a few sequences a thread, or of one sequence by several threads
     int share = 1;
-    while (share < 64 && 2 * share * n <= 256) share *= 2;
-    const int per = (n * share + 255) / 256, b0 = min(tid / share * per, n), b1 = min(b0 + per, n), sub = tid % share;
-    long long mine = 0, one = 0;                             // of all the thread's sequences; of the last one
-    for (int b = b0; b < b1; ++b) {
+    while (share < 64 && 2 * share * n <= NT) share *= 2;
+    const int per = (n * share + NT - 1) / NT, b0 = min(tid / share * per, n), b1 = min(b0 + per, n), sub = tid % share;
+    auto tiles = [&](int b, int from, int by) __attribute__((always_inline)) {
         Span s;
-        one = 0;
-        if (!paged_span(a.s, b, s)) { if (blockIdx.x == 0 && sub == 0) paged_flag(a.s, b); }
+        long long sum = 0;
+        if (!paged_span(a.s, b, s)) { if (blockIdx.x == 0 && from == 0) paged_flag(a.s, b); }
         else {
             const int nb = paged_blocks(s, a.rows);
-            for (int j = sub; j < nb; j += share) { int t0, t1; paged_tiles(s, a.rows, a.window, tile_shift, j, t0, t1); one += t1 - t0; }
+            for (int j = from; j < nb; j += by) { int t0, t1; paged_tiles(s, a.rows, a.window, PAGED_TILE, j, t0, t1); sum += t1 - t0; }
         }
-        mine += one;
-    }
-    for (int o = 1; o < share; o <<= 1) { one += __shfl_xor(one, o, RS_WAVE); }
-    if (share > 1) mine = one;
+        return sum;
+    };
+    long long mine = 0;
+    for (int b = b0; b < b1; ++b) mine += tiles(b, sub, share);
+    for (int o = 1; o < share; o <<= 1) mine += __shfl_xor(mine, o, RS_WAVE);
     const long long own = sub == 0 ? mine * a.s.n_kv : 0;
     long long end = own;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) { const long long u = __shfl_up(end, o, RS_WAVE); if (lane >= o) end += u; }
-    if (lane == 63) sh[wave] = end;
-    __syncthreads();
-    for (int i = 0; i < wave; ++i) end += sh[i];
-    const long long T = sh[0] + sh[1] + sh[2] + sh[3];
-    const int W = paged_runs(T, most, least);
-    if (w >= W || T == 0) return false;
-    const long long t0 = paged_run(T, W, w), t1 = paged_run(T, W, w + 1);
-    run.T = T; run.W = W; run.left = t1 - t0;
-    if (t0 >= t1) return false;                              // (more runs than tiles)
-    if (sub == 0 && t0 >= end - own && t0 < end) {
-        long long rem = t0 - (end - own);
-        int b = b0;
-        long long of = mine;
+    long long T;
+    if constexpr (NT == 64) T = __shfl(end, 63, RS_WAVE);
+    else {
+        if (lane == 63) sh[wave] = end;
+        __syncthreads();
+        T = 0;
+        for (int i = 0; i < NT / 64; ++i) { if (i < wave) end += sh[i]; T += sh[i]; }
+    }
+    const int W = T < most ? (int)T : most;                  // (a tile a run at least)
+    if (w >= W) return false;
+    const long long t0 = paged_run(T, W, w);
+    run.T = T; run.W = W; run.left = paged_run(T, W, w + 1) - t0;
+    long long rem = 0, of = 0;
+    int b = 0;
+    const bool found = sub == 0 && t0 >= end - own && t0 < end;
+    if (found) {
+        rem = t0 - (end - own);
+        of = mine; b = b0;
         if (per > 1)
-            for (; b < b1; ++b) {
-                Span s;
-                of = 0;
-                if (paged_span(a.s, b, s)) {
-                    const int nb = paged_blocks(s, a.rows);
-                    for (int j = 0; j < nb; ++j) { int u0, u1; paged_tiles(s, a.rows, a.window, tile_shift, j, u0, u1); of += u1 - u0; }
-                }
+            for (;; ++b) {                                     // (one of the thread's sequences has it)
+                of = tiles(b, 0, 1);
                 if (rem < of * a.s.n_kv) break;
                 rem -= of * a.s.n_kv;
             }
-        sh[4] = b; sh[5] = rem; sh[6] = of;
     }
-    __syncthreads();
+    if constexpr (NT == 64) {
+        const int who = __ffsll((unsigned long long)__ballot(found)) - 1;
+        b = __shfl(b, who, RS_WAVE); rem = __shfl(rem, who, RS_WAVE); of = __shfl(of, who, RS_WAVE);
+    } else {
+        if (found) { sh[4] = b; sh[5] = rem; sh[6] = of; }
+        __syncthreads();
+        b = (int)sh[4]; rem = sh[5]; of = sh[6];
+    }
     PagedItem &it = run.at;
-    it.b = (int)sh[4];
-    long long rem = sh[5];
-    const long long of = sh[6];
+    it.b = __builtin_amdgcn_readfirstlane(b);
     (void)paged_span(a.s, it.b, it.s);
     it.n_blk = paged_blocks(it.s, a.rows);
-    it.kvh = (int)(rem / of);
-    rem -= it.kvh * of;
-    // the block, by every wave: a lane sums a run of blocks
-    const int each = (it.n_blk + 63) / 64, j0 = min(lane * each, it.n_blk), j1 = min(j0 + each, it.n_blk);
-    long long sum = 0;
-    for (int j = j0; j < j1; ++j) { int u0, u1; paged_tiles(it.s, a.rows, a.window, tile_shift, j, u0, u1); sum += u1 - u0; }
-    long long upto = sum;
+    const int kvh = rem >> 31 == 0 && of >> 31 == 0 ? (int)((unsigned)rem / (unsigned)of) : (int)(rem / of);
+    it.kvh = __builtin_amdgcn_readfirstlane(kvh);
+    rem -= kvh * of;
+    int j = 0, u0, u1;
+    if (it.n_blk > 1) {
+        // the block, by every wave: a lane sums a run of blocks
+        const int each = (it.n_blk + 63) / 64, j0 = min(lane * each, it.n_blk), j1 = min(j0 + each, it.n_blk);
+        long long sum = 0;
+        for (int i = j0; i < j1; ++i) { paged_tiles(it.s, a.rows, a.window, PAGED_TILE, i, u0, u1); sum += u1 - u0; }
+        long long upto = sum;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const long long u = __shfl_up(upto, o, RS_WAVE); if (lane >= o) upto += u; }
-    const int who = __ffsll((unsigned long long)__ballot(rem < upto)) - 1;             // (rem < of: some lane has it)
-    rem -= __shfl(upto - sum, who, RS_WAVE);
-    int j = who * each, u0, u1;
+        for (int o = 1; o < 64; o <<= 1) { const long long u = __shfl_up(upto, o, RS_WAVE); if (lane >= o) upto += u; }
+        const int who = __ffsll((unsigned long long)__ballot(rem < upto)) - 1;             // (rem < of: some lane has it)
+        rem -= __shfl(upto - sum, who, RS_WAVE);
+        j = who * each;
+    }
     for (;; ++j) {
-        paged_tiles(it.s, a.rows, a.window, tile_shift, j, u0, u1);
+        paged_tiles(it.s, a.rows, a.window, PAGED_TILE, j, u0, u1);
         if (rem < u1 - u0) break;
         rem -= u1 - u0;
     }
@@ -138,12 +147,14 @@ __device__ __forceinline__ void paged_note_cut(const PagedAttnArgs &a, const Pag
     if (threadIdx.x == 0) a.cuts[w] = make_int4(it.b, it.kvh, it.blk, paged_run_of(run.T, run.W, paged_run(run.T, run.W, w) - (ta - t0)));
 }
 
-// Pages of the positions pos .. pos + n - 1 (one page's), of which lo .. hi - 1 are needed: its number, or some page where none is needed or there is none.
-__device__ __forceinline__ int paged_page(const PagedAttnArgs &a, const PagedItem &it, int pos, int n, int lo, int hi) {
-    if (pos >= hi || pos + n <= lo) return 0;
-    const int page = a.s.table[(size_t)it.s.slot * a.s.max_pages + (pos >> a.s.page_shift)];
-    if (page >= 0 && page < a.s.n_pages) return page;
-    paged_flag(a.s, it.b);
+// Page table entry of position pos, or of the position nearest to it among the needed ones, lo .. hi - 1; asked for ahead of its use, which checks it:
+__device__ __forceinline__ int paged_entry(const PagedAttnArgs &a, const Span &s, int pos, int lo, int hi) {
+    return a.s.table[(size_t)s.slot * a.s.max_pages + (min(max(pos, lo), hi - 1) >> a.s.page_shift)];
+}
+// a page of the cache, whatever the entry holds.
+__device__ __forceinline__ int paged_page(const PagedAttnArgs &a, int b, int entry) {
+    if ((unsigned)entry < (unsigned)a.s.n_pages) return entry;
+    paged_flag(a.s, b);
     return 0;
 }
 
@@ -213,10 +224,10 @@ __device__ __forceinline__ void paged_store_cols(const PagedAttnArgs &a, int row
 }
 
 // Columns c_from .. c_to - 1 of c0 .. c0 + 31 of an item, by one wave, for items whose sums hold a NaN: V's
-// infinities and NaN stay out of the products and reach the columns that see them by being counted.  Operands come straight from the pages.
+// infinities and NaN stay out of the products and reach the columns that see them by being counted.  Operands come straight from the pages, 32
+// channels of the result at a time: few registers, so that the kernel it is part of starts fast when there is nothing of the kind.
 template <int HD, int PL>
 __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const PagedItem &it, int c0, int c_from, int c_to) {
-    constexpr int NS = HD / 16, ND = HD / 32;
     const int lane = threadIdx.x & 63, col = lane & 31, hh = lane >> 5, c = c0 + col, row = c / a.group, head = it.kvh * a.group + c - row * a.group;
     const int r0 = it.blk * a.rows, nr = min(a.rows, it.s.m - r0);
     const bool valid = c < nr * a.group;
@@ -226,282 +237,344 @@ __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const Page
     if (!valid) see_hi = 0;
     const int k_row = 16 * ((col >> 4) & 1) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3), in_page = (1 << a.s.page_shift) - 1;
     const size_t q_at = (size_t)(it.s.first + r0 + row) * a.q_stride + (size_t)head * HD + 8 * hh;
-    float m = -INFINITY, l = 0.f;
-    f32x16_t o[ND], zero;
+#pragma unroll 1
+    for (int d = 0; d < HD / 32; ++d) {
+        float m = -INFINITY, l = 0.f;
+        f32x16_t o;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+        for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll 1
+        for (int first = lo & ~31; first < hi; first += 32) {
+            const size_t kp = ((size_t)paged_page(a, it.b, paged_entry(a, it.s, first + k_row, lo, hi)) * a.s.n_kv + it.kvh) << a.s.page_shift;
+            f32x16_t sc;
 #pragma unroll
-    for (int d = 0; d < ND; ++d) o[d] = zero;
-    for (int first = lo & ~31; first < hi; first += 32) {
-        const size_t kp = ((size_t)paged_page(a, it, first + (k_row & 16), 16, lo, hi) * a.s.n_kv + it.kvh) << a.s.page_shift;
-        f32x16_t sc = zero;
-        for (int s = 0; s < NS; ++s) {
-            const bf16x8_t A = *reinterpret_cast<const bf16x8_t *>(a.kc + (kp + ((first + k_row) & in_page)) * HD + 16 * s + 8 * hh);
-            bf16x8_t q[PL];
-            paged_load_q<PL>(a.q, q_at + 16 * s, valid, q);
+            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll 1
+            for (int s = 0; s < HD / 16; ++s) {
+                const bf16x8_t A = *reinterpret_cast<const bf16x8_t *>(a.kc + (kp + ((first + k_row) & in_page)) * HD + 16 * s + 8 * hh);
+                bf16x8_t q[PL];
+                paged_load_q<PL>(a.q, q_at + 16 * s, valid, q);
 #pragma unroll
-            for (int pl = PL - 1; pl >= 0; --pl) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, q[pl], sc, 0, 0, 0);
-        }
-        float p[16], see[16], mx = -INFINITY;
+                for (int pl = PL - 1; pl >= 0; --pl) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, q[pl], sc, 0, 0, 0);
+            }
+            float mx = -INFINITY;
+            auto sees = [&](int i) __attribute__((always_inline)) { const int at = first + 16 * (i >> 3) + 8 * hh + (i & 7); return at >= see_lo && at < see_hi; };
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int at = first + 16 * (i >> 3) + 8 * hh + (i & 7);
-            see[i] = at >= see_lo && at < see_hi ? 1.f : 0.f;
-            p[i] = see[i] > 0.f ? sc[i] : -INFINITY;
-            mx = fmaxf(mx, p[i]);
-        }
-        mx = fmaxf(mx, __shfl_xor(mx, 32, RS_WAVE));
-        const float m_new = fmaxf(m, mx), mc = m_new == -INFINITY ? 0.f : m_new * a.c, alpha = __builtin_amdgcn_exp2f(fmaf(m, a.c, -mc));
-        m = m_new;
-        l *= alpha;
+            for (int i = 0; i < 16; ++i) { sc[i] = sees(i) ? sc[i] : -INFINITY; mx = fmaxf(mx, sc[i]); }
+            mx = fmaxf(mx, __shfl_xor(mx, 32, RS_WAVE));
+            const float m_new = fmaxf(m, mx), mc = m_new == -INFINITY ? 0.f : m_new * a.c, alpha = __builtin_amdgcn_exp2f(fmaf(m, a.c, -mc));
+            m = m_new;
+            l *= alpha;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) { p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -mc)); l += p[i]; }
+            for (int i = 0; i < 16; ++i) { sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.c, -mc)); l += sc[i]; o[i] *= alpha; }
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+            for (int s = 0; s < 2; ++s) {
+                float p8[8], see8[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            float p8[8], see8[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { p8[i] = p[8 * s + i]; see8[i] = see[8 * s + i]; }
-            bf16x8_t pb8[PL], sb[1];
-            paged_planes<PL>(p8, pb8);
-            paged_planes<1>(see8, sb);
-            const int at = first + 16 * s + 8 * hh;
-            const size_t vp = ((size_t)paged_page(a, it, at, 8, lo, hi) * a.s.n_kv + it.kvh) * HD;
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
+                for (int i = 0; i < 8; ++i) { p8[i] = sc[8 * s + i]; see8[i] = sees(8 * s + i) ? 1.f : 0.f; }
+                bf16x8_t pb[PL], sb[1];
+                paged_planes<PL>(p8, pb);
+                paged_planes<1>(see8, sb);
+                const int at = first + 16 * s + 8 * hh;
+                const size_t vp = ((size_t)paged_page(a, it.b, paged_entry(a, it.s, at, lo, hi)) * a.s.n_kv + it.kvh) * HD;
                 const uint4 v = *reinterpret_cast<const uint4 *>(a.vc + ((vp + 32 * d + col) << a.s.page_shift) + (at & in_page));
 #pragma unroll
-                for (int pl = PL - 1; pl >= 0; --pl) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(paged_pick<0>(v), pb8[pl], o[d], 0, 0, 0);
-                const f32x16_t up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(paged_pick<1>(v), sb[0], zero, 0, 0, 0);
-                const f32x16_t down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(paged_pick<2>(v), sb[0], zero, 0, 0, 0);
-                const f32x16_t nan = __builtin_amdgcn_mfma_f32_32x32x16_bf16(paged_pick<3>(v), sb[0], zero, 0, 0, 0);
+                for (int pl = PL - 1; pl >= 0; --pl) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(paged_pick<0>(v), pb[pl], o, 0, 0, 0);
+#pragma unroll 1
+                for (int kind = 1; kind < 4; ++kind) {
+                    f32x16_t n;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    o[d][i] += (up[i] > 0.f ? INFINITY : 0.f) + (down[i] > 0.f ? -INFINITY : 0.f) + (nan[i] > 0.f ? __uint_as_float(0x7fc00000u) : 0.f);
+                    for (int i = 0; i < 16; ++i) n[i] = 0.f;
+                    n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kind == 1 ? paged_pick<1>(v) : kind == 2 ? paged_pick<2>(v) : paged_pick<3>(v), sb[0], n, 0, 0, 0);
+                    const float special = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : __uint_as_float(0x7fc00000u);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] += n[i] > 0.f ? special : 0.f;
+                }
             }
+        }
+        l += __shfl_xor(l, 32, RS_WAVE);
+        if (valid && c >= c_from && c < c_to) {
+            const size_t at = (size_t)(it.s.first + r0 + row);
+            const float inv = 1.f / l;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                paged_store4<PL>(a.out, at * a.out_stride + (size_t)head * HD + 32 * d + 2 * i + 4 * hh, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+            if (d == 0 && hh == 0 && a.lse) a.lse[at * a.n_q + head] = (m * a.c + __log2f(l)) * 0.69314718055994531f;
         }
     }
-    l += __shfl_xor(l, 32, RS_WAVE);
-    if (valid && c >= c_from && c < c_to) paged_store_cols<HD, PL>(a, it.s.first + r0 + row, head, c, 0, -1, hh, m, l, o);
 }
 
-// ------------------------------------------------------------------------------------------------
-// k_paged_narrow: up to 16 NB columns a block (decode steps, spans of a few rows).  grid: runs, block 256.  Bound by the cache's bytes: K and V go
-// from the pages straight to registers in operand layout, each wave takes every fourth tile (32 positions) of the run with a softmax
-// state of its own, the four states of an item meet in LDS.
-// ------------------------------------------------------------------------------------------------
-template <int HD, int NB>
-__host__ __device__ constexpr size_t paged_narrow_lds() { return (size_t)4 * 16 * NB * (HD + 4) * 4 + 2 * 4 * 16 * NB * 4; }
-
-template <int HD, int PL, int NB>
-__global__ void __launch_bounds__(256, PL * NB > 3 ? 1 : 2) k_paged_narrow(PagedAttnArgs a) {
-    constexpr int NS = HD / 32, ND = HD / 16, COLS = 16 * NB, PITCH = HD + 4;
-    extern __shared__ __align__(16) unsigned char smem[];
-    float *o_sh = reinterpret_cast<float *>(smem), *m_sh = o_sh + 4 * COLS * PITCH, *l_sh = m_sh + 4 * COLS;      // [wave][column]
-    __shared__ long long run_sh[PAGED_RUN_LDS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, hq = lane >> 4, w = blockIdx.x, ps = 1 << a.s.page_shift;
-    PagedRun run;
-    const bool some = paged_find_run(a, PAGED_NARROW_TILE, PAGED_NARROW_RUNS, PAGED_NARROW_LEAST, w, run_sh, run);
-    if (tid == 0) { a.cuts[w] = make_int4(-1, 0, 0, 0); a.odd[w] = 0; }
-    if (!some) return;
-    PagedItem it = run.at;
-    int ta = run.ta;
-    unsigned int odd = 0;
-    for (int n_items = 0;; ++n_items) {
-        int t0, t1;
-        paged_tiles(it.s, a.rows, a.window, PAGED_NARROW_TILE, it.blk, t0, t1);
-        const int tb = (int)min((long long)t1, ta + run.left);
-        const int r0 = it.blk * a.rows, nr = min(a.rows, it.s.m - r0), n_col = nr * a.group;
-        int lo, hi;
-        paged_seen(it.s, r0, r0 + nr, a.window, lo, hi);
-        // ---- this lane's columns
-        int see_lo[NB], see_hi[NB];                                   // positions that the column sees
-        bf16x8_t q[NB][NS][PL];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const int c = 16 * nb + col, r = c / a.group, h = it.kvh * a.group + c - r * a.group;
-            const bool valid = c < n_col;
-            paged_seen(it.s, r0 + r, r0 + r + 1, a.window, see_lo[nb], see_hi[nb]);
-            if (!valid) see_hi[nb] = 0;
-            const size_t at = (size_t)(it.s.first + r0 + r) * a.q_stride + (size_t)h * HD + 8 * hq;
-#pragma unroll
-            for (int s = 0; s < NS; ++s) paged_load_q<PL>(a.q, at + 32 * s, valid, q[nb][s]);
-        }
-        float m[NB], l[NB];
-        f32x4_t o[NB][ND];
-        // K: the lane's row col of block blk is position 8 (col / 4) + 4 blk + col % 4 of the tile; V: channel col, positions 8 hq ..
-        const int k_pos = 8 * (col >> 2), v_pos = 8 * hq;
-        const size_t page_size = (size_t)a.s.n_kv << a.s.page_shift, head = (size_t)it.kvh << a.s.page_shift;
-        uint4 k[2][NS], v[ND];
-        int kpage = 0, vpage = 0;
-        auto pages = [&](int t) __attribute__((always_inline)) { kpage = paged_page(a, it, 32 * t + k_pos, 8, lo, hi); vpage = paged_page(a, it, 32 * t + v_pos, 8, lo, hi); };
-        auto load_k = [&](int t, int page) __attribute__((always_inline)) {
-            const uint16_t *p = a.kc + (page * page_size + head + ((32 * t + k_pos + (col & 3)) & (ps - 1))) * HD + 8 * hq;
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-                for (int s = 0; s < NS; ++s) k[blk][s] = *reinterpret_cast<const uint4 *>(p + blk * 4 * HD + 32 * s);
-        };
-        auto load_v = [&](int t, int page) __attribute__((always_inline)) {
-            const uint16_t *p = a.vc + (page * page_size + head) * HD + ((size_t)col << a.s.page_shift) + ((32 * t + v_pos) & (ps - 1));
-#pragma unroll
-            for (int d = 0; d < ND; ++d) v[d] = *reinterpret_cast<const uint4 *>(p + ((size_t)(16 * d) << a.s.page_shift));
-        };
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            m[nb] = -INFINITY; l[nb] = 0.f;
-#pragma unroll
-            for (int d = 0; d < ND; ++d) o[nb][d] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-        }
-        int t = ta + wave;
-        if (t < tb) {
-            pages(t);
-            load_k(t, kpage); load_v(t, vpage);
-            if (t + 4 < tb) pages(t + 4);
-        }
-        for (; t < tb; t += 4) {
-            const bool more = t + 4 < tb;
-            const int first = 32 * t + 8 * hq;                                        // position of the lane's scores
-            f32x4_t sc[NB][2];
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    sc[nb][blk] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int s = 0; s < NS; ++s)
-#pragma unroll
-                        for (int pl = PL - 1; pl >= 0; --pl)
-                            sc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[blk][s]), q[nb][s][pl], sc[nb][blk], 0, 0, 0);
-                }
-            // (K's registers are free: the next tile's arrives while this one's V is multiplied, and the other way round)
-            const int next_v = vpage;
-            if (more) load_k(t + 4, kpage);
-            if (t + 8 < tb) pages(t + 8);
-            if (32 * t + 32 > hi)
-#pragma unroll
-                for (int d = 0; d < ND; ++d) v[d] = paged_first(v[d], hi - first);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                float p[8], mx = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    p[i] = first + i >= see_lo[nb] && first + i < see_hi[nb] ? sc[nb][i >> 2][i & 3] : -INFINITY;
-                    mx = fmaxf(mx, p[i]);
-                }
-                mx = fmaxf(mx, __shfl_xor(mx, 16, RS_WAVE));
-                mx = fmaxf(mx, __shfl_xor(mx, 32, RS_WAVE));
-                const float m_new = fmaxf(m[nb], mx), mc = m_new == -INFINITY ? 0.f : m_new * a.c;
-                const float alpha = __builtin_amdgcn_exp2f(fmaf(m[nb], a.c, -mc));            // (no score so far: 0)
-                m[nb] = m_new;
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -mc)); sum += p[i]; }
-                l[nb] = l[nb] * alpha + sum;
-#pragma unroll
-                for (int d = 0; d < ND; ++d) { o[nb][d][0] *= alpha; o[nb][d][1] *= alpha; o[nb][d][2] *= alpha; o[nb][d][3] *= alpha; }
-                bf16x8_t pb[PL];
-                paged_planes<PL>(p, pb);
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int pl = PL - 1; pl >= 0; --pl)
-                        o[nb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v[d]), pb[pl], o[nb][d], 0, 0, 0);
-            }
-            if (more) load_v(t + 4, next_v);
-        }
-        float poison = 0.f;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int d = 0; d < ND; ++d) poison += 16 * nb + col < n_col ? (o[nb][d][0] + o[nb][d][1]) + (o[nb][d][2] + o[nb][d][3]) : 0.f;
-        // ---- the four waves' states meet: each leaves its own, then four channels of a column a thread
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            l[nb] += __shfl_xor(l[nb], 16, RS_WAVE);
-            l[nb] += __shfl_xor(l[nb], 32, RS_WAVE);
-            const int at = wave * COLS + 16 * nb + col;
-            if (hq == 0) { m_sh[at] = m[nb]; l_sh[at] = l[nb]; }
-            if (16 * nb + col < n_col)
-#pragma unroll
-                for (int d = 0; d < ND; ++d) *reinterpret_cast<float4 *>(o_sh + at * PITCH + 16 * d + 4 * hq) = make_float4(o[nb][d][0], o[nb][d][1], o[nb][d][2], o[nb][d][3]);
-        }
-        const bool again = __syncthreads_or(poison != poison);
-        const bool whole = ta == t0 && tb == t1;
-        const int part = whole ? -1 : 2 * w + (ta == t0);
-        if (again && whole) odd |= 1u << (n_items & 31);
-        for (int i = tid; i < n_col * (HD / 4); i += 256) {
-            const int c = i / (HD / 4), d = 4 * (i - c * (HD / 4));
-            float mw[4], M = -INFINITY, L = 0.f;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) { mw[k] = m_sh[k * COLS + c]; M = fmaxf(M, mw[k]); }
-            const float Mc = M == -INFINITY ? 0.f : M * a.c;
-            float x[4] = {};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(mw[k], a.c, -Mc));
-                const float4 y = *reinterpret_cast<const float4 *>(o_sh + (k * COLS + c) * PITCH + d);
-                L = fmaf(l_sh[k * COLS + c], e, L);
-                x[0] = fmaf(y.x, e, x[0]); x[1] = fmaf(y.y, e, x[1]); x[2] = fmaf(y.z, e, x[2]); x[3] = fmaf(y.w, e, x[3]);
-            }
-            if (whole) {
-                const int r = c / a.group, h = it.kvh * a.group + c - r * a.group;
-                const size_t row = (size_t)(it.s.first + r0 + r);
-                const float inv = 1.f / L;
-                paged_store4<PL>(a.out, row * a.out_stride + (size_t)h * HD + d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-                if (d == 0 && a.lse) a.lse[row * a.n_q + h] = (Mc + __log2f(L)) * 0.69314718055994531f;
-            } else {
-                *reinterpret_cast<float4 *>(a.part_o + ((size_t)part * COLS + c) * HD + d) = make_float4(x[0], x[1], x[2], x[3]);
-                if (d == 0) { a.part_ml[(size_t)part * 2 * COLS + c] = M; a.part_ml[((size_t)part * 2 + 1) * COLS + c] = L; }
-            }
-        }
-        if (ta > t0 && tb == t1) paged_note_cut(a, run, it, w, ta, t0);
-        run.left -= tb - ta;
-        if (run.left <= 0) break;
-        paged_next(a, it);
-        int n1;
-        paged_tiles(it.s, a.rows, a.window, PAGED_NARROW_TILE, it.blk, ta, n1);
-        __syncthreads();
-    }
-    if (tid == 0) a.odd[w] = odd;
+// K and V tiles in LDS: rows of K (positions), rows of V (channels, 64 positions), in 16-byte pieces whose order differs from row to row, since a direct load
+// cannot pad them and the operand reads (one piece of 16 rows at a time) would meet in the same banks.  A load fetches a contiguous kilobyte's worth of whole
+// rows: 128 bytes and more of a row side by side, where operands straight from the pages would be pieces of 64.
+// The 16 rows of K that a read takes together are consecutive (wide, rows = 32) or 0 .. 3, 8 .. 11, 16 .. 19, 24 .. 27 (narrow, rows = 16).
+template <int HD, int ROWS>
+__device__ __forceinline__ unsigned paged_k_swizzle(unsigned row) {
+    if (ROWS == 32) return HD == 128 ? row & 15 : HD == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
+    return HD == 128 ? (row & 3) | ((row >> 1) & 12) : HD == 64 ? ((row >> 1) & 1) | ((row >> 2) & 6) : (row >> 3) & 3;
 }
-
-// ------------------------------------------------------------------------------------------------
-// k_paged_wide: blocks of 128 columns (chunks of a prompt).  grid: runs, block 256.  Bound by the matrix cores: a tile of 64 positions goes to LDS
-// once for all columns, by direct loads that are one tile ahead (two buffers); a wave has 32 columns.  Rows of a buffer are
-// 16-byte pieces in an order that differs from row to row, since a direct load cannot pad them and the operand reads (32 rows, one
-// piece) would meet in the same banks.
-// ------------------------------------------------------------------------------------------------
-template <int HD> __device__ __forceinline__ int wide_k_swizzle(int row) { return HD == 128 ? row & 15 : HD == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
+__device__ __forceinline__ unsigned paged_v_swizzle(unsigned channel) { return (channel >> 1) & 7; }
 
 typedef const __attribute__((address_space(1))) unsigned char paged_global;
 typedef __attribute__((address_space(3))) unsigned char paged_local;
 
+template <int N>
+__device__ __forceinline__ void paged_wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// The wave's LDS reads have arrived: what they read may be overwritten by a load.
+__device__ __forceinline__ void paged_wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Rows 16 g .. 16 g + 15 of a tile of K at `at` (uniform: its first row in its page) into kb.
+template <int HD, int ROWS>
+__device__ __forceinline__ void paged_fetch_k(const unsigned char *at, unsigned char *kb, int g) {
+    constexpr int RPI = 512 / HD;                             // rows a load fetches
+    const unsigned lane = threadIdx.x & 63, kr = lane / (HD / 8);
+#pragma unroll
+    for (int i = 0; i < 16 / RPI; ++i) {
+        const unsigned r = RPI * i + kr, piece = (lane & (HD / 8 - 1)) ^ paged_k_swizzle<HD, ROWS>(16 * g + r);
+        __builtin_amdgcn_global_load_lds((paged_global *)(at + (r * (HD * 2) + piece * 16)), (paged_local *)(kb + (16 * g + RPI * i) * (HD * 2)), 16, 0, 0);
+    }
+}
+// The piece of eight positions that a lane fetches of channels 8 i + lane / 8.
+__device__ __forceinline__ int paged_v_piece(int i) { const unsigned lane = threadIdx.x & 63; return (lane & 7) ^ paged_v_swizzle(8 * i + (lane >> 3)); }
+// Channels 8 i .. 8 i + 7 of a tile of V: `at` + `lane_at` is the lane's piece of channel 0 in its page.
+__device__ __forceinline__ void paged_fetch_v(const unsigned char *at, unsigned lane_at, unsigned char *vb, int page_shift, int i) {
+    const unsigned lane = threadIdx.x & 63;
+    __builtin_amdgcn_global_load_lds((paged_global *)(at + (lane_at + ((8u * i + (lane >> 3)) << (page_shift + 1)))), (paged_local *)(vb + i * 1024), 16, 0, 0);
+}
+
+// ------------------------------------------------------------------------------------------------
+// k_paged_narrow: up to 16 NB columns a block (decode steps, spans of a few rows).  grid: runs, block 64: a wave by itself, four of them on a CU, each
+// with one tile of K and one of V in LDS.  Bound by the cache's bytes: K of the next tile is on its way while V of this one is multiplied, and the
+// other way round, also from one item to the next, so that a CU has about 100 KB under way.
+// ------------------------------------------------------------------------------------------------
+template <int HD, int PL, int NB>
+__global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
+    constexpr int NS = HD / 32, ND = HD / 16, COLS = 16 * NB, NL = HD / 8;             // NL: loads of a tile of K, and of V
+    __shared__ __align__(16) unsigned char kb[64 * HD * 2], vb[64 * HD * 2];
+    const int lane = threadIdx.x, col = lane & 15, hq = lane >> 4, w = blockIdx.x, ps = 1 << a.s.page_shift;
+    PagedRun run;
+    const bool some = paged_find_run<64>(a, PAGED_NARROW_RUNS, w, nullptr, run);
+    if (lane == 0) { a.cuts[w] = make_int4(-1, 0, 0, 0); a.odd[w] = 0; }
+    if (!some) return;
+    // ---- the tile that is fetched next: `left` tiles of the run from it on, positions lo .. hi - 1 of its item are needed
+    PagedItem fit = run.at;
+    int ft = run.ta, f_t0, f_t1, f_lo, f_hi;
+    long long left = run.left;
+    auto look = [&]() __attribute__((always_inline)) {
+        const int r0 = fit.blk * a.rows;
+        paged_seen(fit.s, r0, min(r0 + a.rows, fit.s.m), a.window, f_lo, f_hi);
+        f_t0 = f_lo >> PAGED_TILE; f_t1 = ((f_hi - 1) >> PAGED_TILE) + 1;
+    };
+    auto ask = [&]() __attribute__((always_inline)) { return paged_entry(a, fit.s, 64 * ft + 16 * (lane & 3), f_lo, f_hi); };
+    auto fetch_k = [&](int t, int kvh, int page) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const size_t at = (((size_t)__builtin_amdgcn_readlane(page, g) * a.s.n_kv + kvh) << a.s.page_shift) + ((64 * t + 16 * g) & (ps - 1));
+            paged_fetch_k<HD, 16>((const unsigned char *)(a.kc + at * HD), kb, g);
+        }
+    };
+    auto fetch_v = [&](int t, int kvh, int page) __attribute__((always_inline)) {
+        // (a piece of the lane's and the one it takes of every other load; a page of 64 positions and more holds the whole tile)
+        if (ps >= 64) {
+            const size_t at = ((((size_t)__builtin_amdgcn_readfirstlane(page) * a.s.n_kv + kvh) * HD) << a.s.page_shift) + ((64 * t) & (ps - 1));
+#pragma unroll
+            for (int i = 0; i < NL; ++i) paged_fetch_v((const unsigned char *)(a.vc + at), 16 * paged_v_piece(i), vb, a.s.page_shift, i);
+        } else {
+            const unsigned char *at[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int piece = paged_v_piece(k);
+                at[k] = (const unsigned char *)(a.vc + (((((size_t)__shfl(page, piece >> 1, RS_WAVE) * a.s.n_kv + kvh) * HD) << a.s.page_shift) + ((64 * t + 8 * piece) & (ps - 1))));
+            }
+#pragma unroll
+            for (int i = 0; i < NL; ++i) paged_fetch_v(at[i & 1], 0, vb, a.s.page_shift, i);
+        }
+    };
+    auto step = [&]() __attribute__((always_inline)) {
+        --left; ++ft;
+        if (left > 0 && ft == f_t1) { paged_next(a, fit); look(); ft = f_t0; }
+    };
+    look();
+    int page = paged_page(a, fit.b, ask());
+    fetch_k(ft, fit.kvh, page);
+    fetch_v(ft, fit.kvh, page);
+    // ---- the tile that is multiplied
+    PagedItem it = fit;
+    int t = ft, t0 = f_t0, t1 = f_t1, hi = f_hi, ta = ft;
+    step();
+    int entry = left > 0 ? ask() : 0, n_items = 0;
+    unsigned int odd = 0;
+    int see_lo[NB], see_hi[NB], n_col = 0;                                // positions that the lane's columns see
+    bf16x8_t q[NB][NS][PL];
+    float m[NB], l[NB];
+    f32x4_t o[NB][ND];
+    bool begin = true;
+    while (true) {
+        if (begin) {
+            const int r0 = it.blk * a.rows;
+            n_col = min(a.rows, it.s.m - r0) * a.group;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int c = 16 * nb + col, r = c / a.group, h = it.kvh * a.group + c - r * a.group;
+                const bool valid = c < n_col;
+                paged_seen(it.s, r0 + r, r0 + r + 1, a.window, see_lo[nb], see_hi[nb]);
+                if (!valid) see_hi[nb] = 0;
+                const size_t at = (size_t)(it.s.first + r0 + r) * a.q_stride + (size_t)h * HD + 8 * hq;
+#pragma unroll
+                for (int s = 0; s < NS; ++s) paged_load_q<PL>(a.q, at + 32 * s, valid, q[nb][s]);
+                m[nb] = -INFINITY; l[nb] = 0.f;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) o[nb][d] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+            }
+            begin = false;
+        }
+        // ---- scores: register i of block 2 s32 + blk is position 64 t + 32 s32 + 8 hq + 4 blk + i of column col
+        paged_wait_loads<NL>();                                           // all but V of this tile
+        f32x4_t sc[NB][4];
+#pragma unroll
+        for (int kbk = 0; kbk < 4; ++kbk) {
+            const int r = 32 * (kbk >> 1) + 8 * (col >> 2) + 4 * (kbk & 1) + (col & 3);
+            bf16x8_t A[NS];
+#pragma unroll
+            for (int s = 0; s < NS; ++s) A[s] = *reinterpret_cast<const bf16x8_t *>(kb + r * (HD * 2) + ((4 * s + hq) ^ paged_k_swizzle<HD, 16>(r)) * 16);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                sc[nb][kbk] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int pl = PL - 1; pl >= 0; --pl) sc[nb][kbk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[s], q[nb][s][pl], sc[nb][kbk], 0, 0, 0);
+            }
+        }
+        // ---- the next tile's K goes where this one's was
+        const bool more = left > 0;
+        PagedItem nit = fit;
+        int nt = ft, n_t0 = f_t0, n_t1 = f_t1, n_hi = f_hi;
+        if (more) {
+            page = paged_page(a, fit.b, entry);
+            step();
+            if (left > 0) entry = ask();
+            paged_wait_reads();
+            fetch_k(nt, nit.kvh, page);
+        }
+        // ---- softmax
+        const int first = 64 * t + 8 * hq;
+        const bool all = 64 * t + 64 <= it.s.p0 + it.blk * a.rows + 1 && a.window == 0;             // every column sees the whole tile
+        bf16x8_t pb[NB][2][PL];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            float p[16], mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int at = first + 32 * (i >> 3) + (i & 7);
+                p[i] = all || (at >= see_lo[nb] && at < see_hi[nb]) ? sc[nb][i >> 2][i & 3] : -INFINITY;
+                mx = fmaxf(mx, p[i]);
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 16, RS_WAVE));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, RS_WAVE));
+            const float m_new = fmaxf(m[nb], mx), mc = m_new == -INFINITY ? 0.f : m_new * a.c;
+            const float alpha = __builtin_amdgcn_exp2f(fmaf(m[nb], a.c, -mc));                // (no score so far: 0)
+            m[nb] = m_new;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -mc)); sum += p[i]; }
+            l[nb] = l[nb] * alpha + sum;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) { o[nb][d][0] *= alpha; o[nb][d][1] *= alpha; o[nb][d][2] *= alpha; o[nb][d][3] *= alpha; }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float p8[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p8[i] = p[8 * s + i];
+                paged_planes<PL>(p8, pb[nb][s]);
+            }
+        }
+        // ---- P V
+        if (more) paged_wait_loads<NL>(); else paged_wait_loads<0>();     // all but K of the next tile
+        const bool end = 64 * t + 64 > hi;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            uint4 v[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                v[s] = *reinterpret_cast<const uint4 *>(vb + (16 * d + col) * 128 + ((4 * s + hq) ^ paged_v_swizzle(col)) * 16);
+                if (end) v[s] = paged_first(v[s], hi - first - 32 * s);
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int pl = PL - 1; pl >= 0; --pl)
+                        o[nb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v[s]), pb[nb][s][pl], o[nb][d], 0, 0, 0);
+        }
+        if (more) { paged_wait_reads(); fetch_v(nt, nit.kvh, page); }
+        // ---- the item's or the run's last tile
+        if (t + 1 == t1 || !more) {
+            const bool whole = ta == t0 && t + 1 == t1;
+            const int part = 2 * w + (ta == t0), r0 = it.blk * a.rows;
+            float poison = 0.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                l[nb] += __shfl_xor(l[nb], 16, RS_WAVE);
+                l[nb] += __shfl_xor(l[nb], 32, RS_WAVE);
+                const int c = 16 * nb + col, r = c / a.group, h = it.kvh * a.group + c - r * a.group;
+                if (c >= n_col) continue;
+                const size_t row = (size_t)(it.s.first + r0 + r);
+                const float inv = 1.f / l[nb];
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    const f32x4_t x = o[nb][d];
+                    poison += (x[0] + x[1]) + (x[2] + x[3]);
+                    if (whole) paged_store4<PL>(a.out, row * a.out_stride + (size_t)h * HD + 16 * d + 4 * hq, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+                    else *reinterpret_cast<float4 *>(a.part_o + ((size_t)part * COLS + c) * HD + 16 * d + 4 * hq) = make_float4(x[0], x[1], x[2], x[3]);
+                }
+                if (hq == 0) {
+                    if (!whole) { a.part_ml[(size_t)part * 2 * COLS + c] = m[nb]; a.part_ml[((size_t)part * 2 + 1) * COLS + c] = l[nb]; }
+                    else if (a.lse) a.lse[row * a.n_q + h] = (m[nb] * a.c + __log2f(l[nb])) * 0.69314718055994531f;
+                }
+            }
+            if (whole && __any(poison != poison)) odd |= 1u << (n_items & 31);
+            if (ta > t0 && t + 1 == t1) paged_note_cut(a, run, it, w, ta, t0);
+            if (!more) break;
+            ++n_items;
+            begin = true;
+            ta = n_t0;
+        }
+        it = nit; t = nt; t0 = n_t0; t1 = n_t1; hi = n_hi;
+    }
+    if (lane == 0) a.odd[w] = odd;
+}
+
+// ------------------------------------------------------------------------------------------------
+// k_paged_wide: blocks of 128 columns (chunks of a prompt).  grid: runs, block 256.  Bound by the matrix cores: a tile of 64 positions goes to LDS
+// once for all columns, by direct loads that are one tile ahead (two buffers); a wave has 32 columns.
+// Sharing the XCD's L2: neighbouring runs, which read the same K and V, are an XCD's, and they read the same tiles at the same time, because a run begins each item at
+// the tile that its count of tiles so far gives, modulo the item's, and goes round.  Begun at the first tile each, runs were spread over the whole context
+// and 11 % of the requests met in L2: 8.7 GB at 6 TB/s from beyond it for the four chunks of 2048 rows on up to 14000 positions.
+// ------------------------------------------------------------------------------------------------
 template <int HD, int PL>
 __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
-    constexpr int NS = HD / 16, ND = HD / 32, COLS = PAGED_COLS, KB = 64 * HD * 2, RPI = 1024 / (HD * 2);      // rows of K a load fetches
+    constexpr int NS = HD / 16, ND = HD / 32, COLS = PAGED_COLS, KB = 64 * HD * 2;
     constexpr int RB = PL == 1 ? 2 : 1;                                   // blocks of 32 positions whose scores are held at a time
     __shared__ __align__(16) unsigned char k0[KB], k1[KB], v0[KB], v1[KB];
     __shared__ long long run_sh[PAGED_RUN_LDS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hh = lane >> 5, w = blockIdx.x, ps = 1 << a.s.page_shift;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hh = lane >> 5, ps = 1 << a.s.page_shift;
+    const int w = (blockIdx.x & 7) * (PAGED_WIDE_RUNS / 8) + (blockIdx.x >> 3);         // (workgroups go round the eight XCDs)
     PagedRun run;
-    const bool some = paged_find_run(a, PAGED_WIDE_TILE, PAGED_WIDE_RUNS, 1, w, run_sh, run);
+    const bool some = paged_find_run<256>(a, PAGED_WIDE_RUNS, w, run_sh, run);
     if (tid == 0) { a.cuts[w] = make_int4(-1, 0, 0, 0); a.odd[w] = 0; }
     if (!some) return;
     PagedItem it = run.at;
     int ta = run.ta;
-    const size_t page_bytes = ((size_t)a.s.n_kv << a.s.page_shift) * HD * 2;
-    // this lane's part of a load of K (rows 16 wave + RPI i + kr) and of V (channels 8 (4 i + wave) + lane / 8; one piece of eight positions)
-    const int kr = lane / (HD / 8), v_piece = (lane & 7) ^ (lane >> 3);
+    const int v_piece = paged_v_piece(wave);                          // (wave, wave + 4, ..: the same of each)
     // operand reads: row of K that lane % 32 stands for
     const int k_row = 16 * ((col >> 4) & 1) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
     unsigned int odd = 0;
+    int done = 0;
     for (int n_items = 0;; ++n_items) {
         int t0, t1;
-        paged_tiles(it.s, a.rows, a.window, PAGED_WIDE_TILE, it.blk, t0, t1);
+        paged_tiles(it.s, a.rows, a.window, PAGED_TILE, it.blk, t0, t1);
         const int tb = (int)min((long long)t1, ta + run.left);
         const int r0 = it.blk * a.rows, nr = min(a.rows, it.s.m - r0), n_col = nr * a.group;
         int lo, hi;
@@ -519,42 +592,47 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
         }
         float m, l;
         f32x16_t o[ND];
-        const unsigned char *kh = (const unsigned char *)a.kc + (((size_t)it.kvh << a.s.page_shift) * HD) * 2;
-        const unsigned char *vh = (const unsigned char *)a.vc + (((size_t)it.kvh << a.s.page_shift) * HD) * 2;
-        int kpage, vpage;
-        auto pages = [&](int t) __attribute__((always_inline)) {
-            kpage = paged_page(a, it, 64 * t + 16 * wave, 16, lo, hi);
-            vpage = paged_page(a, it, 64 * t + 8 * v_piece, 8, lo, hi);
-        };
-        auto fetch = [&](int t, unsigned char *kb, unsigned char *vb) __attribute__((always_inline)) {
-            const unsigned char *kp = kh + kpage * page_bytes + (size_t)((64 * t + 16 * wave) & (ps - 1)) * (HD * 2);
+        auto ask = [&](int t) __attribute__((always_inline)) { return paged_entry(a, it.s, 64 * t + 16 * (lane & 3), lo, hi); };
+        auto fetch = [&](int t, int entry, unsigned char *kb, unsigned char *vb) __attribute__((always_inline)) {
+            const int page = paged_page(a, it.b, entry);
+            const size_t k_at = (((size_t)__builtin_amdgcn_readlane(page, wave) * a.s.n_kv + it.kvh) << a.s.page_shift) + ((64 * t + 16 * wave) & (ps - 1));
+            paged_fetch_k<HD, 32>((const unsigned char *)(a.kc + k_at * HD), kb, wave);
+            if (ps >= 64) {
+                const size_t v_at = ((((size_t)__builtin_amdgcn_readfirstlane(page) * a.s.n_kv + it.kvh) * HD) << a.s.page_shift) + ((64 * t) & (ps - 1));
 #pragma unroll
-            for (int i = 0; i < 16 / RPI; ++i) {
-                const int r = RPI * i + kr;                                              // of the wave's 16 rows
-                const int piece = (lane & (HD / 8 - 1)) ^ wide_k_swizzle<HD>(16 * wave + r);
-                __builtin_amdgcn_global_load_lds((paged_global *)(kp + r * (HD * 2) + piece * 16), (paged_local *)(kb + (16 * wave + RPI * i) * (HD * 2)), 16, 0, 0);
-            }
-            const unsigned char *vp = vh + vpage * page_bytes + (size_t)((64 * t + 8 * v_piece) & (ps - 1)) * 2;
+                for (int i = 0; i < HD / 8; i += 4) paged_fetch_v((const unsigned char *)(a.vc + v_at), 16 * v_piece, vb, a.s.page_shift, i + wave);
+            } else {
+                const size_t v_at = ((((size_t)__shfl(page, v_piece >> 1, RS_WAVE) * a.s.n_kv + it.kvh) * HD) << a.s.page_shift) + ((64 * t + 8 * v_piece) & (ps - 1));
 #pragma unroll
-            for (int i = 0; i < HD / 32; ++i) {
-                const int ch = 8 * (4 * i + wave);
-                __builtin_amdgcn_global_load_lds((paged_global *)(vp + ((size_t)(ch + (lane >> 3)) << (a.s.page_shift + 1))), (paged_local *)(vb + ch * 128), 16, 0, 0);
+                for (int i = 0; i < HD / 8; i += 4) paged_fetch_v((const unsigned char *)(a.vc + v_at), 0, vb, a.s.page_shift, i + wave);
             }
         };
         // RB blocks of 32 positions from `first` on, which lie from row 32 rb0 of the buffers on
         auto block = [&](int first, int rb0, const unsigned char *kb, const unsigned char *vb) __attribute__((always_inline)) {
             f32x16_t sc[RB];
+            // operands are read ahead of the products: all of K's, and V's first ones beside the last of them
+            bf16x8_t kf[RB][NS], vf[2][ND];
+            auto v_at = [&](int s, int d) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8_t *>(vb + (32 * d + col) * 128 + ((4 * rb0 + 2 * s + hh) ^ paged_v_swizzle(col)) * 16); };
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int r = 32 * (rb0 + rb) + k_row;
+#pragma unroll
+                for (int s = 0; s < NS; ++s) kf[rb][s] = *reinterpret_cast<const bf16x8_t *>(kb + r * (HD * 2) + ((2 * s + hh) ^ paged_k_swizzle<HD, 32>(r)) * 16);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[rb][i] = 0.f;
-                const int r = 32 * (rb0 + rb) + k_row;
+                if (rb == RB - 1) {
 #pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const bf16x8_t A = *reinterpret_cast<const bf16x8_t *>(kb + r * (HD * 2) + ((2 * s + hh) ^ wide_k_swizzle<HD>(r)) * 16);
-#pragma unroll
-                    for (int pl = PL - 1; pl >= 0; --pl) sc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, q[s][pl], sc[rb], 0, 0, 0);
+                    for (int d = 0; d < ND; ++d) vf[0][d] = v_at(0, d);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int pl = PL - 1; pl >= 0; --pl) sc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[rb][s], q[s][pl], sc[rb], 0, 0, 0);
             }
             // score i of block rb is position first + 32 rb + 16 (i / 8) + 8 hh + i % 8
             const bool edge = first + 32 * RB > it.s.p0 + r0 + 1 || (a.window > 0 && first < it.s.p0 + r0 + nr - a.window) || n_col < 32 * wave + 32;
@@ -587,7 +665,6 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) { sc[rb][i] = __builtin_amdgcn_exp2f(fmaf(sc[rb][i], a.c, -mc)); l += sc[rb][i]; }
-            auto v_at = [&](int s, int d) __attribute__((always_inline)) { return vb + (32 * d + col) * 128 + ((4 * rb0 + 2 * s + hh) ^ (col & 7)) * 16; };
 #pragma unroll
             for (int s = 0; s < 2 * RB; ++s) {
                 float p[8];
@@ -595,12 +672,15 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
                 for (int i = 0; i < 8; ++i) p[i] = sc[s >> 1][8 * (s & 1) + i];
                 bf16x8_t pb[PL];
                 paged_planes<PL>(p, pb);
+                if (s + 1 < 2 * RB) {
 #pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const bf16x8_t A = *reinterpret_cast<const bf16x8_t *>(v_at(s, d));
-#pragma unroll
-                    for (int pl = PL - 1; pl >= 0; --pl) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, pb[pl], o[d], 0, 0, 0);
+                    for (int d = 0; d < ND; ++d) vf[(s + 1) & 1][d] = v_at(s + 1, d);
                 }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int pl = PL - 1; pl >= 0; --pl) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s & 1][d], pb[pl], o[d], 0, 0, 0);
             }
         };
         auto compute = [&](int t, const unsigned char *kb, const unsigned char *vb) __attribute__((always_inline)) {
@@ -612,7 +692,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
             if (64 * t + 64 <= hi) return;
             for (int i = tid; i < HD * 8; i += 256) {
                 const int ch = i >> 3, piece = i & 7, n = hi - 64 * t - 8 * piece;
-                uint4 *at = reinterpret_cast<uint4 *>(vb + ch * 128 + (piece ^ (ch & 7)) * 16);
+                uint4 *at = reinterpret_cast<uint4 *>(vb + ch * 128 + (piece ^ paged_v_swizzle(ch)) * 16);
                 if (n < 8) *at = paged_first(*at, n);
             }
             __syncthreads();
@@ -623,22 +703,25 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        pages(ta);
-        fetch(ta, k0, v0);
-        pages(ta + 1);
-        for (int t = ta; t < tb; t += 2) {
-            __builtin_amdgcn_s_waitcnt(0x0f70);                                   // vmcnt(0): this wave's share of tile t has arrived
+        // (a whole item from the tile on at which a run that has multiplied as many tiles as this one stands, and round: see above)
+        const int n = tb - ta, from = n == t1 - t0 ? done % n : 0;
+        auto tile = [&](int i) __attribute__((always_inline)) { i += from; return ta + (i >= n ? i - n : i); };
+        fetch(tile(0), ask(tile(0)), k0, v0);
+        int entry = ask(tile(1));
+        for (int i = 0; i < n; i += 2) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);                                   // vmcnt(0): this wave's share of tile i has arrived
             __syncthreads();
-            clear_end(t, v0);
-            if (t + 1 < tb) { fetch(t + 1, k1, v1); pages(t + 2); }
-            if (busy) compute(t, k0, v0);
-            if (t + 1 >= tb) break;
+            clear_end(tile(i), v0);
+            if (i + 1 < n) { fetch(tile(i + 1), entry, k1, v1); entry = ask(tile(i + 2)); }
+            if (busy) compute(tile(i), k0, v0);
+            if (i + 1 >= n) break;
             __builtin_amdgcn_s_waitcnt(0x0f70);
             __syncthreads();
-            clear_end(t + 1, v1);
-            if (t + 2 < tb) { fetch(t + 2, k0, v0); pages(t + 3); }
-            if (busy) compute(t + 1, k1, v1);
+            clear_end(tile(i + 1), v1);
+            if (i + 2 < n) { fetch(tile(i + 2), entry, k0, v0); entry = ask(tile(i + 3)); }
+            if (busy) compute(tile(i + 1), k1, v1);
         }
+        done += n;
         l += __shfl_xor(l, 32, RS_WAVE);
         float poison = 0.f;
 #pragma unroll
@@ -653,7 +736,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
         if (run.left <= 0) break;
         paged_next(a, it);
         int n1;
-        paged_tiles(it.s, a.rows, a.window, PAGED_WIDE_TILE, it.blk, ta, n1);
+        paged_tiles(it.s, a.rows, a.window, PAGED_TILE, it.blk, ta, n1);
     }
     if (tid == 0) a.odd[w] = odd;
 }
@@ -662,9 +745,16 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
 // k_paged_join: the pieces of a cut item, in the order of their runs.  grid (runs, column groups), block 256: HD / 4 threads a column.
 // And the items, whole or cut, whose sums hold a NaN, once more.
 // ------------------------------------------------------------------------------------------------
+template <int HD, int COLS>
+__host__ __device__ constexpr int join_groups() { return COLS == PAGED_COLS ? 1 : 4; }                     // threads that share a column's pieces between them: many pieces where blocks are small
+template <int HD, int COLS>
+__host__ __device__ constexpr int join_cols() { return 1024 / HD / join_groups<HD, COLS>(); }            // columns a workgroup
+
 template <int HD, int PL, int COLS>
 __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
+    constexpr int TPC = HD / 4, G = join_groups<HD, COLS>(), CPW = join_cols<HD, COLS>(), BATCH = 8;
     __shared__ long long run_sh[PAGED_RUN_LDS];
+    __shared__ float o_sh[G > 1 ? G : 1][CPW][HD + 4];
     const int w = blockIdx.x, wave = threadIdx.x >> 6;
     const int4 cut = a.cuts[w];
     const unsigned int odd = blockIdx.y == 0 ? a.odd[w] : 0;
@@ -674,48 +764,81 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
         it.b = cut.x; it.kvh = cut.y; it.blk = cut.z;
         (void)paged_span(a.s, cut.x, it.s);
         const int r0 = it.blk * a.rows, n_col = min(a.rows, it.s.m - r0) * a.group, n = w - cut.w + 1;
-        constexpr int TPC = HD / 4, CPW = 256 / TPC;                               // threads a column, columns at a time
-        const int c = blockIdx.y * CPW + threadIdx.x / TPC, d = 4 * (threadIdx.x % TPC);
+        const int unit = threadIdx.x / TPC, g = unit / CPW, lc = unit % CPW, d = 4 * (threadIdx.x % TPC);
+        for (int from = blockIdx.y * CPW; from < n_col; from += gridDim.y * CPW) {
+        const int c = from + lc;
         bool nan = false;
+        float M = -INFINITY, L = 0.f, x[4] = {};
         if (c < n_col) {
-            // piece i is the start of run cut.w + i, except the first one, which is the end of its run
-            auto part = [&](int i) __attribute__((always_inline)) { return 2 * (size_t)(cut.w + i) + (i == 0); };
-            float M = -INFINITY, L = 0.f, x[4] = {};
-            for (int i = 0; i < n; ++i) M = fmaxf(M, a.part_ml[part(i) * 2 * COLS + c]);
-            const float Mc = M == -INFINITY ? 0.f : M * a.c;
-#pragma unroll 4
-            for (int i = 0; i < n; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(a.part_ml[part(i) * 2 * COLS + c], a.c, -Mc));
-                const float4 y = *reinterpret_cast<const float4 *>(a.part_o + (part(i) * COLS + c) * HD + d);
-                L = fmaf(a.part_ml[(part(i) * 2 + 1) * COLS + c], e, L);
+            // piece i is the start of run cut.w + i, except the first one, which is the end of its run.  A batch's loads are under way together.
+            for (int i0 = g; i0 < n; i0 += G * BATCH) {
+                float m[BATCH], l[BATCH];
+                float4 y[BATCH];
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) {
+                    const int i = min(i0 + G * k, n - 1);
+                    const size_t part = 2 * (size_t)(cut.w + i) + (i == 0);
+                    m[k] = a.part_ml[part * 2 * COLS + c]; l[k] = a.part_ml[(part * 2 + 1) * COLS + c];
+                    y[k] = *reinterpret_cast<const float4 *>(a.part_o + (part * COLS + c) * HD + d);
+                }
+                float top = M;
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) { if (i0 + G * k >= n) m[k] = -INFINITY; top = fmaxf(top, m[k]); }
+                const float tc = top == -INFINITY ? 0.f : top * a.c, e0 = __builtin_amdgcn_exp2f(fmaf(M, a.c, -tc));
+                M = top; L *= e0; x[0] *= e0; x[1] *= e0; x[2] *= e0; x[3] *= e0;
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(m[k], a.c, -tc));
+                    if (i0 + G * k >= n) continue;
+                    L = fmaf(l[k], e, L);
+                    x[0] = fmaf(y[k].x, e, x[0]); x[1] = fmaf(y[k].y, e, x[1]); x[2] = fmaf(y[k].z, e, x[2]); x[3] = fmaf(y[k].w, e, x[3]);
+                }
+            }
+        }
+        if constexpr (G > 1) {
+            *reinterpret_cast<float4 *>(&o_sh[g][lc][d]) = make_float4(x[0], x[1], x[2], x[3]);
+            if (d == 0) { o_sh[g][lc][HD] = M; o_sh[g][lc][HD + 1] = L; }
+            __syncthreads();
+            float top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < G; ++k) top = fmaxf(top, o_sh[k][lc][HD]);
+            const float tc = top == -INFINITY ? 0.f : top * a.c;
+            M = top; L = 0.f; x[0] = x[1] = x[2] = x[3] = 0.f;
+#pragma unroll
+            for (int k = 0; k < G; ++k) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(o_sh[k][lc][HD], a.c, -tc));
+                const float4 y = *reinterpret_cast<const float4 *>(&o_sh[k][lc][d]);
+                L = fmaf(o_sh[k][lc][HD + 1], e, L);
                 x[0] = fmaf(y.x, e, x[0]); x[1] = fmaf(y.y, e, x[1]); x[2] = fmaf(y.z, e, x[2]); x[3] = fmaf(y.w, e, x[3]);
             }
+        }
+        if (c < n_col && g == 0) {
             const int r = c / a.group, h = it.kvh * a.group + c - r * a.group;
             const size_t row = (size_t)(it.s.first + r0 + r);
             const float inv = 1.f / L, all = (x[0] + x[1]) + (x[2] + x[3]);
             nan = all != all;
             paged_store4<PL>(a.out, row * a.out_stride + (size_t)h * HD + d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-            if (d == 0 && a.lse) a.lse[row * a.n_q + h] = (Mc + __log2f(L)) * 0.69314718055994531f;
+            if (d == 0 && a.lse) a.lse[row * a.n_q + h] = ((M == -INFINITY ? 0.f : M * a.c) + __log2f(L)) * 0.69314718055994531f;
         }
         if (__syncthreads_or(nan)) {
-            const int from = blockIdx.y * CPW, c0 = (from & ~31) + 32 * wave;
+            const int c0 = (from & ~31) + 32 * wave;
             if (c0 < min(from + CPW, n_col)) paged_careful<HD, PL>(a, it, c0, from, from + CPW);
+        }
         }
     }
     if (!odd) return;
     PagedRun run;
     constexpr bool WIDE = COLS == PAGED_COLS;
-    constexpr int SHIFT = WIDE ? PAGED_WIDE_TILE : PAGED_NARROW_TILE;
-    if (!paged_find_run(a, SHIFT, WIDE ? PAGED_WIDE_RUNS : PAGED_NARROW_RUNS, WIDE ? 1 : PAGED_NARROW_LEAST, w, run_sh, run)) return;
+    if (!paged_find_run<256>(a, WIDE ? PAGED_WIDE_RUNS : PAGED_NARROW_RUNS, w, run_sh, run)) return;
     it = run.at;
     for (int k = 0, ta = run.ta;; ++k) {
         int t0, t1;
-        paged_tiles(it.s, a.rows, a.window, SHIFT, it.blk, t0, t1);
+        paged_tiles(it.s, a.rows, a.window, PAGED_TILE, it.blk, t0, t1);
         if (odd >> (k & 31) & 1 && ta == t0 && run.left >= t1 - t0 && 32 * wave < COLS) paged_careful<HD, PL>(a, it, 32 * wave, 0, COLS);
         run.left -= t1 - ta;
         if (run.left <= 0) return;
         paged_next(a, it);
-        paged_tiles(it.s, a.rows, a.window, SHIFT, it.blk, ta, t1);
+        paged_tiles(it.s, a.rows, a.window, PAGED_TILE, it.blk, ta, t1);
     }
 }
 

@@ -61,19 +61,16 @@ RS_HD void paged_tiles(const Span &s, int rows, int window, int tile_shift, int 
 }
 
 // First tile of run w of W over T tiles (no product beyond T).
-RS_HD long long paged_run(long long T, int W, int w) { return T / W * w + T % W * w / W; }
+RS_HD long long paged_run(long long T, int W, int w) {
+    if (T >> 31 == 0) { const unsigned t = (unsigned)T, n = (unsigned)W, k = (unsigned)w; return t / n * k + t % n * k / n; }      // (W is at most 2^11)
+    return T / W * w + T % W * w / W;
+}
 
 // The run that tile t < T is in.
 RS_HD int paged_run_of(long long T, int W, long long t) {
     int lo = 0, hi = W - 1;
     while (lo < hi) { const int mid = (lo + hi) / 2; if (paged_run(T, W, mid + 1) > t) hi = mid; else lo = mid + 1; }
     return lo;
-}
-
-// Runs that T tiles are dealt to: `most` of them, fewer where a run would get less than `least` tiles.
-RS_HD int paged_runs(long long T, int most, int least) {
-    const long long n = (T + least - 1) / least;
-    return n < 1 ? 1 : n < most ? (int)n : most;
 }
 
 }  // namespace rs
