@@ -323,23 +323,58 @@ __device__ __forceinline__ void paged_wait_loads() { asm volatile("s_waitcnt vmc
 // The wave's LDS reads have arrived: what they read may be overwritten by a load.
 __device__ __forceinline__ void paged_wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+// A buffer over what lies behind `at` (uniform): loads from it take a 32-bit place a lane, in one register, and what they have in common in a scalar one.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_buffer(const void *at) { return __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, 0x7fffffff, 0x00027000); }
+
+// The larger of a lane's value and that of the lane 32 further or before.
+__device__ __forceinline__ float paged_max_halves(float x) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+
 // Rows 16 g .. 16 g + 15 of a tile of K at `at` (uniform: its first row in its page) into kb.
 template <int HD, int ROWS>
-__device__ __forceinline__ void paged_fetch_k(const unsigned char *at, unsigned char *kb, int g) {
+__device__ __forceinline__ void paged_fetch_k(const void *at, unsigned char *kb, int g) {
     constexpr int RPI = 512 / HD;                             // rows a load fetches
     const unsigned lane = threadIdx.x & 63, kr = lane / (HD / 8);
+    const __amdgpu_buffer_rsrc_t buf = paged_buffer(at);
 #pragma unroll
     for (int i = 0; i < 16 / RPI; ++i) {
         const unsigned r = RPI * i + kr, piece = (lane & (HD / 8 - 1)) ^ paged_k_swizzle<HD, ROWS>(16 * g + r);
-        __builtin_amdgcn_global_load_lds((paged_global *)(at + (r * (HD * 2) + piece * 16)), (paged_local *)(kb + (16 * g + RPI * i) * (HD * 2)), 16, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (paged_local *)(kb + (16 * g + RPI * i) * (HD * 2)), 16, kr * (HD * 2) + piece * 16, RPI * i * (HD * 2), 0, 0);
     }
 }
 // The piece of eight positions that a lane fetches of channels 8 i + lane / 8.
 __device__ __forceinline__ int paged_v_piece(int i) { const unsigned lane = threadIdx.x & 63; return (lane & 7) ^ paged_v_swizzle(8 * i + (lane >> 3)); }
-// Channels 8 i .. 8 i + 7 of a tile of V: `at` + `lane_at` is the lane's piece of channel 0 in its page.
-__device__ __forceinline__ void paged_fetch_v(const unsigned char *at, unsigned lane_at, unsigned char *vb, int page_shift, int i) {
-    const unsigned lane = threadIdx.x & 63;
-    __builtin_amdgcn_global_load_lds((paged_global *)(at + (lane_at + ((8u * i + (lane >> 3)) << (page_shift + 1)))), (paged_local *)(vb + i * 1024), 16, 0, 0);
+
+// Channels 8 i .. 8 i + 7 of a tile of V, for i = i0, i0 + STEP ..  `page`: of the positions 16 g .. of the tile in lane g.
+// (A page of 64 positions and more holds the whole tile; the pieces of smaller ones lie in pages that differ from lane to lane.)
+template <int HD, int STEP>
+__device__ __forceinline__ void paged_fetch_v(const PagedAttnArgs &a, int t, int kvh, int page, unsigned char *vb, int i0) {
+    const unsigned lane = threadIdx.x & 63, in_page = (1u << a.s.page_shift) - 1, pitch = a.s.page_shift + 1;
+    if (a.s.page_shift >= PAGED_TILE) {
+        const size_t at = ((((size_t)__builtin_amdgcn_readfirstlane(page) * a.s.n_kv + kvh) * HD) << a.s.page_shift) + (64 * t & in_page);
+        const __amdgpu_buffer_rsrc_t buf = paged_buffer(a.vc + at);
+#pragma unroll
+        for (int i = 0; i < HD / 8; i += STEP)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (paged_local *)(vb + (i + i0) * 1024), 16, ((lane >> 3) << pitch) + 16 * paged_v_piece(i + i0), (8 * (i + i0)) << pitch, 0, 0);
+    } else {
+        // (every second load of a lane takes the same piece)
+        constexpr int KINDS = STEP % 2 ? 2 : 1;
+        const unsigned char *at[KINDS];
+#pragma unroll
+        for (int k = 0; k < KINDS; ++k) {
+            const int piece = paged_v_piece(i0 + k);
+            const size_t first = ((((size_t)__shfl(page, piece >> 1, RS_WAVE) * a.s.n_kv + kvh) * HD) << a.s.page_shift) + ((64 * t + 8 * piece) & in_page);
+            at[k] = (const unsigned char *)(a.vc + first) + (size_t)((8 * (i0 + k) + (lane >> 3)) << pitch);
+        }
+#pragma unroll
+        for (int i = 0; i < HD / 8; i += STEP) {
+            const unsigned char *&p = at[i % 2 % KINDS];
+            __builtin_amdgcn_global_load_lds((paged_global *)p, (paged_local *)(vb + (i + i0) * 1024), 16, 0, 0);
+            p += (size_t)(8 * STEP * KINDS) << pitch;
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -370,26 +405,10 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const size_t at = (((size_t)__builtin_amdgcn_readlane(page, g) * a.s.n_kv + kvh) << a.s.page_shift) + ((64 * t + 16 * g) & (ps - 1));
-            paged_fetch_k<HD, 16>((const unsigned char *)(a.kc + at * HD), kb, g);
+            paged_fetch_k<HD, 16>(a.kc + at * HD, kb, g);
         }
     };
-    auto fetch_v = [&](int t, int kvh, int page) __attribute__((always_inline)) {
-        // (a piece of the lane's and the one it takes of every other load; a page of 64 positions and more holds the whole tile)
-        if (ps >= 64) {
-            const size_t at = ((((size_t)__builtin_amdgcn_readfirstlane(page) * a.s.n_kv + kvh) * HD) << a.s.page_shift) + ((64 * t) & (ps - 1));
-#pragma unroll
-            for (int i = 0; i < NL; ++i) paged_fetch_v((const unsigned char *)(a.vc + at), 16 * paged_v_piece(i), vb, a.s.page_shift, i);
-        } else {
-            const unsigned char *at[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int piece = paged_v_piece(k);
-                at[k] = (const unsigned char *)(a.vc + (((((size_t)__shfl(page, piece >> 1, RS_WAVE) * a.s.n_kv + kvh) * HD) << a.s.page_shift) + ((64 * t + 8 * piece) & (ps - 1))));
-            }
-#pragma unroll
-            for (int i = 0; i < NL; ++i) paged_fetch_v(at[i & 1], 0, vb, a.s.page_shift, i);
-        }
-    };
+    auto fetch_v = [&](int t, int kvh, int page) __attribute__((always_inline)) { paged_fetch_v<HD, 1>(a, t, kvh, page, vb, 0); };
     auto step = [&]() __attribute__((always_inline)) {
         --left; ++ft;
         if (left > 0 && ft == f_t1) { paged_next(a, fit); look(); ft = f_t0; }
@@ -567,7 +586,6 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
     if (!some) return;
     PagedItem it = run.at;
     int ta = run.ta;
-    const int v_piece = paged_v_piece(wave);                          // (wave, wave + 4, ..: the same of each)
     // operand reads: row of K that lane % 32 stands for
     const int k_row = 16 * ((col >> 4) & 1) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
     unsigned int odd = 0;
@@ -580,7 +598,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
         int lo, hi;
         paged_seen(it.s, r0, r0 + nr, a.window, lo, hi);
         const int c = 32 * wave + col, row = c / a.group, head = it.kvh * a.group + c - row * a.group;
-        const bool valid = c < n_col, busy = 32 * wave < n_col;
+        const bool valid = c < n_col, busy = 32 * wave < n_col;        // (columns that are none have q = 0; nothing of theirs is stored)
         int see_lo, see_hi;
         paged_seen(it.s, r0 + row, r0 + row + 1, a.window, see_lo, see_hi);
         if (!valid) see_hi = 0;
@@ -596,46 +614,43 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
         auto fetch = [&](int t, int entry, unsigned char *kb, unsigned char *vb) __attribute__((always_inline)) {
             const int page = paged_page(a, it.b, entry);
             const size_t k_at = (((size_t)__builtin_amdgcn_readlane(page, wave) * a.s.n_kv + it.kvh) << a.s.page_shift) + ((64 * t + 16 * wave) & (ps - 1));
-            paged_fetch_k<HD, 32>((const unsigned char *)(a.kc + k_at * HD), kb, wave);
-            if (ps >= 64) {
-                const size_t v_at = ((((size_t)__builtin_amdgcn_readfirstlane(page) * a.s.n_kv + it.kvh) * HD) << a.s.page_shift) + ((64 * t) & (ps - 1));
-#pragma unroll
-                for (int i = 0; i < HD / 8; i += 4) paged_fetch_v((const unsigned char *)(a.vc + v_at), 16 * v_piece, vb, a.s.page_shift, i + wave);
-            } else {
-                const size_t v_at = ((((size_t)__shfl(page, v_piece >> 1, RS_WAVE) * a.s.n_kv + it.kvh) * HD) << a.s.page_shift) + ((64 * t + 8 * v_piece) & (ps - 1));
-#pragma unroll
-                for (int i = 0; i < HD / 8; i += 4) paged_fetch_v((const unsigned char *)(a.vc + v_at), 0, vb, a.s.page_shift, i + wave);
-            }
+            paged_fetch_k<HD, 32>(a.kc + k_at * HD, kb, wave);
+            paged_fetch_v<HD, 4>(a, t, it.kvh, page, vb, wave);
         };
         // RB blocks of 32 positions from `first` on, which lie from row 32 rb0 of the buffers on
         auto block = [&](int first, int rb0, const unsigned char *kb, const unsigned char *vb) __attribute__((always_inline)) {
             f32x16_t sc[RB];
-            // operands are read ahead of the products: all of K's, and V's first ones beside the last of them
+            // operands are read ahead of the products: those of the first block, then one beside each product
             bf16x8_t kf[RB][NS], vf[2][ND];
             auto v_at = [&](int s, int d) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8_t *>(vb + (32 * d + col) * 128 + ((4 * rb0 + 2 * s + hh) ^ paged_v_swizzle(col)) * 16); };
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
+            auto read_k = [&](int rb) __attribute__((always_inline)) {
                 const int r = 32 * (rb0 + rb) + k_row;
 #pragma unroll
                 for (int s = 0; s < NS; ++s) kf[rb][s] = *reinterpret_cast<const bf16x8_t *>(kb + r * (HD * 2) + ((2 * s + hh) ^ paged_k_swizzle<HD, 32>(r)) * 16);
-            }
+            };
+            read_k(0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[rb][i] = 0.f;
-                if (rb == RB - 1) {
+                if (rb + 1 < RB) read_k(rb + 1);
+                else
 #pragma unroll
                     for (int d = 0; d < ND; ++d) vf[0][d] = v_at(0, d);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
 #pragma unroll
                 for (int s = 0; s < NS; ++s)
 #pragma unroll
                     for (int pl = PL - 1; pl >= 0; --pl) sc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[rb][s], q[s][pl], sc[rb], 0, 0, 0);
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);           // one LDS read,
+                    __builtin_amdgcn_sched_group_barrier(0x008, PL, 0);          // the products of one operand
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             // score i of block rb is position first + 32 rb + 16 (i / 8) + 8 hh + i % 8
-            const bool edge = first + 32 * RB > it.s.p0 + r0 + 1 || (a.window > 0 && first < it.s.p0 + r0 + nr - a.window) || n_col < 32 * wave + 32;
+            const bool edge = first + 32 * RB > it.s.p0 + r0 + 1 || (a.window > 0 && first < it.s.p0 + r0 + nr - a.window);
             if (edge)
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
@@ -649,7 +664,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[rb][i]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, RS_WAVE));
+            mx = paged_max_halves(mx);
             // the maximum that p is relative to may lag behind by 2^8: the sums have room, and most tiles rescale nothing
             if (__any((mx - m) * a.c > 8.f || (m == -INFINITY && mx > -INFINITY))) {
                 const float m_new = fmaxf(m, mx), alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * a.c);
