@@ -242,32 +242,37 @@ def rs_set_sampling(handle: int, enabled: bool, key: int = 0) -> None:
 RS_F32, RS_BF16 = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BY_PARTS = range(3)
 _ROW_TYPES = {torch.float32: RS_F32, torch.bfloat16: RS_BF16}
+_INT_TYPES = (torch.int32, torch.uint32)
 
 
-def _rows(name: str, t: torch.Tensor, device: torch.device):
+def _rows(name: str, t: torch.Tensor, device: int):
     """(address, row stride) of a tensor [rows, heads, channels] whose heads lie back to back; the C side checks the rest."""
-    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+    if t.dim() != 3 or not t.is_contiguous() and (t.stride(2) != 1 or t.stride(1) != t.shape[2]):
         raise ValueError(f"{name} must be [rows, heads, head_dim] with the heads of a row back to back, not {tuple(t.shape)} with strides {t.stride()}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the call's other tensors on {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, the call's other tensors on {_device_name(device)}")
     return t.data_ptr(), t.stride(0)
 
 
-def _ints(name: str, t: Optional[torch.Tensor], n: int, device: torch.device) -> Optional[int]:
+def _ints(name: str, t: Optional[torch.Tensor], n: int, device: int) -> Optional[int]:
     """Address of n 32-bit integers."""
     if t is None:
         return None
-    if t.dtype not in (torch.int32, torch.uint32) or not t.is_contiguous() or t.numel() < n or t.device != device:
-        raise ValueError(f"{name} must hold {n} contiguous 32-bit integers on {device}")
+    if t.dtype not in _INT_TYPES or not t.is_contiguous() or t.numel() < n or t.get_device() != device:
+        raise ValueError(f"{name} must hold {n} contiguous 32-bit integers on {_device_name(device)}")
     return t.data_ptr()
 
 
-def _device_stream(device: torch.device, stream) -> Optional[int]:
+def _device_name(device: int) -> str:
+    return "the CPU" if device < 0 else f"cuda:{device}"
+
+
+def _device_stream(device: int, stream) -> Optional[int]:
     """The launch goes to the current device, which has to be the tensors' own."""
-    if device.type != "cuda":
-        raise ValueError(f"tensors must be on a GPU, not on {device}")
-    if _raw_device is not None and _raw_device() != device.index or _raw_device is None and torch.cuda.current_device() != device.index:
-        raise ValueError(f"tensors are on {device}, which is not the current device")
+    if device < 0:
+        raise ValueError("tensors must be on a GPU")
+    if device != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
+        raise ValueError(f"tensors are on cuda:{device}, which is not the current device")
     return _stream(stream)
 
 
@@ -282,10 +287,11 @@ class PagedCache:
             raise ValueError("page_table must be int32 [slots, pages]")
         if not (k.is_contiguous() and v.is_contiguous() and page_table.is_contiguous()) or not k.device == v.device == page_table.device:
             raise ValueError("k, v and page_table must be contiguous and on one device")
-        self.k, self.v, self.page_table, self.device = k, v, page_table, k.device
+        self.k, self.v, self.page_table, self.device = k, v, page_table, k.get_device()
         self.n_kv_heads, self.page_size, self.head_dim = k.shape[1], k.shape[2], k.shape[3]
         self.struct = _RsPagedKv(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), k.shape[0], k.shape[2], page_table.shape[0],
                                  page_table.shape[1], k.shape[1], k.shape[3])
+        self._ref = C.byref(self.struct)
 
 
 class Rope:
@@ -294,8 +300,9 @@ class Rope:
     def __init__(self, inv_freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0):
         if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be contiguous float64 [rot_dim / 2]")
-        self.inv_freq, self.device = inv_freq, inv_freq.device
+        self.inv_freq, self.device = inv_freq, inv_freq.get_device()
         self.struct = _RsRope(2 * inv_freq.numel(), int(bool(interleaved)), inv_freq.data_ptr(), amplitude)
+        self._ref = C.byref(self.struct)
 
 
 def rs_rope_frequencies(rot_dim: int, theta: float, kind: int = ROPE_PLAIN, factor: float = 1.0, original_ctx: float = 32768.0,
@@ -308,56 +315,61 @@ def rs_rope_frequencies(rot_dim: int, theta: float, kind: int = ROPE_PLAIN, fact
 
 def rs_rope_rows(rope: Rope, d_pos: torch.Tensor, x: torch.Tensor, out: torch.Tensor, inverse: bool = False, stream=None) -> None:
     """x, out: [rows, heads, head_dim] of one type (out may be x); d_pos: int32 [rows]."""
-    dev = x.device
+    dev = x.get_device()
     if x.dtype not in _ROW_TYPES or out.dtype != x.dtype or out.shape != x.shape or rope.device != dev:
         raise ValueError("x and out must be fp32 or bf16, of one type, shape and device, which is the frequencies' too")
     px, sx = _rows("x", x, dev)
     po, so = _rows("out", out, dev)
     n, heads, hd = x.shape
-    _check(lib.rs_rope_rows(C.byref(rope.struct), n, _ints("d_pos", d_pos, n, dev), _ROW_TYPES[x.dtype], heads, hd, px, sx, int(bool(inverse)), po, so,
+    _check(lib.rs_rope_rows(rope._ref, n, _ints("d_pos", d_pos, n, dev), _ROW_TYPES[x.dtype], heads, hd, px, sx, int(bool(inverse)), po, so,
                             _device_stream(dev, stream)))
 
 
-def _check_paged_rows(cache: PagedCache, n_rows: int, rows) -> None:
-    for name, t, heads in rows:
-        if t.dtype != rows[0][1].dtype or t.dtype not in _ROW_TYPES:
-            raise ValueError(f"{name} must be fp32 or bf16, as the call's other rows are")
-        if t.shape[0] < n_rows or t.shape[1] != heads or t.shape[2] != cache.head_dim:
-            raise ValueError(f"{name} must be at least [{n_rows}, {heads}, {cache.head_dim}], not {tuple(t.shape)}")
+def _paged_rows(name: str, t: torch.Tensor, cache: PagedCache, n_rows: int, heads: int, dtype: torch.dtype):
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < n_rows or shape[1] != heads or shape[2] != cache.head_dim or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} and at least [{n_rows}, {heads}, {cache.head_dim}], not {t.dtype} {tuple(shape)}")
+    return _rows(name, t, cache.device)
+
+
+def _paged_type(q: torch.Tensor) -> int:
+    if q.dtype not in _ROW_TYPES or q.dim() != 3:
+        raise ValueError(f"q must be fp32 or bf16 [rows, heads, head_dim], not {q.dtype} {tuple(q.shape)}")
+    return _ROW_TYPES[q.dtype]
 
 
 def rs_paged_append(cache: PagedCache, n_seqs: int, n_rows: int, d_seq_slot, d_span_offset, d_pos0, rope: Optional[Rope], q, k, v, q_out,
                     d_flags=None, stream=None) -> None:
     """q, q_out: [rows, query heads, head_dim]; k, v: [rows, KV heads, head_dim]; views of one projection's rows do."""
-    dev = cache.device
-    (pq, sq), (pk, sk), (pv, sv), (po, so) = _rows("q", q, dev), _rows("k", k, dev), _rows("v", v, dev), _rows("q_out", q_out, dev)
-    nq, nkv = q.shape[1], cache.n_kv_heads
-    _check_paged_rows(cache, n_rows, (("q", q, nq), ("k", k, nkv), ("v", v, nkv), ("q_out", q_out, nq)))
+    dev, kind, nq, nkv = cache.device, _paged_type(q), q.shape[1], cache.n_kv_heads
+    pq, sq = _paged_rows("q", q, cache, n_rows, nq, q.dtype)
+    pk, sk = _paged_rows("k", k, cache, n_rows, nkv, q.dtype)
+    pv, sv = _paged_rows("v", v, cache, n_rows, nkv, q.dtype)
+    po, so = _paged_rows("q_out", q_out, cache, n_rows, nq, q.dtype)
     if rope is not None and rope.device != dev:
-        raise ValueError(f"the frequencies are on {rope.device}, the cache on {dev}")
-    _check(lib.rs_paged_append(C.byref(cache.struct), n_seqs, n_rows, _ints("d_seq_slot", d_seq_slot, n_seqs, dev),
+        raise ValueError(f"the frequencies are on {_device_name(rope.device)}, the cache on {_device_name(dev)}")
+    _check(lib.rs_paged_append(cache._ref, n_seqs, n_rows, _ints("d_seq_slot", d_seq_slot, n_seqs, dev),
                                _ints("d_span_offset", d_span_offset, n_seqs + 1, dev), _ints("d_pos0", d_pos0, n_seqs, dev),
-                               None if rope is None else C.byref(rope.struct), _ROW_TYPES[q.dtype], nq, pq, sq, pk, sk, pv, sv, po, so,
+                               None if rope is None else rope._ref, kind, nq, pq, sq, pk, sk, pv, sv, po, so,
                                _ints("d_flags", d_flags, n_seqs, dev), _device_stream(dev, stream)))
 
 
 def rs_paged_attention_scratch_bytes(cache: PagedCache, n_seqs: int, n_rows: int, n_q_heads: int) -> int:
-    return lib.rs_paged_attention_scratch_bytes(C.byref(cache.struct), n_seqs, n_rows, n_q_heads)
+    return lib.rs_paged_attention_scratch_bytes(cache._ref, n_seqs, n_rows, n_q_heads)
 
 
 def rs_paged_attention(cache: PagedCache, n_seqs: int, n_rows: int, d_seq_slot, d_span_offset, d_pos0, q, scale: float, window: int, out, d_lse, d_scratch,
                        d_flags=None, stream=None) -> None:
     """q, out: [rows, query heads, head_dim]; d_lse: fp32 [rows, query heads] or None; d_scratch: uint8."""
-    dev = cache.device
-    (pq, sq), (po, so) = _rows("q", q, dev), _rows("out", out, dev)
-    nq = q.shape[1]
-    _check_paged_rows(cache, n_rows, (("q", q, nq), ("out", out, nq)))
-    if d_lse is not None and (d_lse.dtype != torch.float32 or not d_lse.is_contiguous() or d_lse.numel() < n_rows * nq or d_lse.device != dev):
-        raise ValueError(f"d_lse must be contiguous fp32 [{n_rows}, {nq}] on {dev}")
-    if d_scratch is None or d_scratch.device != dev or not d_scratch.is_contiguous():
-        raise ValueError(f"d_scratch must be a contiguous tensor on {dev}")
-    _check(lib.rs_paged_attention(C.byref(cache.struct), n_seqs, n_rows, _ints("d_seq_slot", d_seq_slot, n_seqs, dev),
-                                  _ints("d_span_offset", d_span_offset, n_seqs + 1, dev), _ints("d_pos0", d_pos0, n_seqs, dev), _ROW_TYPES[q.dtype], nq, pq, sq,
+    dev, kind, nq = cache.device, _paged_type(q), q.shape[1]
+    pq, sq = _paged_rows("q", q, cache, n_rows, nq, q.dtype)
+    po, so = _paged_rows("out", out, cache, n_rows, nq, q.dtype)
+    if d_lse is not None and (d_lse.dtype != torch.float32 or not d_lse.is_contiguous() or d_lse.numel() < n_rows * nq or d_lse.get_device() != dev):
+        raise ValueError(f"d_lse must be contiguous fp32 [{n_rows}, {nq}] on {_device_name(dev)}")
+    if d_scratch is None or d_scratch.get_device() != dev or not d_scratch.is_contiguous():
+        raise ValueError(f"d_scratch must be a contiguous tensor on {_device_name(dev)}")
+    _check(lib.rs_paged_attention(cache._ref, n_seqs, n_rows, _ints("d_seq_slot", d_seq_slot, n_seqs, dev),
+                                  _ints("d_span_offset", d_span_offset, n_seqs + 1, dev), _ints("d_pos0", d_pos0, n_seqs, dev), kind, nq, pq, sq,
                                   scale, window, po, so, _ptr(d_lse), _ints("d_flags", d_flags, n_seqs, dev), d_scratch.data_ptr(),
                                   d_scratch.numel() * d_scratch.element_size(), _device_stream(dev, stream)))
 

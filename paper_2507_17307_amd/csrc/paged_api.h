@@ -56,7 +56,7 @@ PagedSpans paged_spans(const rs_paged_kv *c, int32_t n_seqs, int32_t n_rows, con
 }
 
 // Which kernel takes a call: blocks of 16 or 32 columns where the spans have no more than that on average, else of 128.
-struct PagedShape { int cols, rows, runs; long long items; size_t odd, ml, o, total; };
+struct PagedShape { int cols, rows, runs; long long items; size_t of, odd, ml, o, total; };
 PagedShape paged_shape(int head_dim, int n_seqs, int n_rows, int group, int n_kv) {
     PagedShape p{};
     const long long slots = ((long long)n_rows * group + n_seqs - 1) / n_seqs;
@@ -64,7 +64,8 @@ PagedShape paged_shape(int head_dim, int n_seqs, int n_rows, int group, int n_kv
     p.rows = p.cols / group;
     p.runs = p.cols == PAGED_COLS ? PAGED_WIDE_RUNS : PAGED_NARROW_RUNS;
     p.items = ((long long)n_rows / p.rows + n_seqs) * n_kv;                     // at most
-    p.odd = align_up((size_t)p.runs * sizeof(int4));
+    p.of = align_up((size_t)p.runs * sizeof(int4));
+    p.odd = p.of + align_up((size_t)p.runs * sizeof(int2));
     p.ml = p.odd + align_up((size_t)p.runs * 4);
     p.o = p.ml + align_up((size_t)2 * p.runs * 2 * p.cols * 4);
     p.total = p.o + align_up((size_t)2 * p.runs * p.cols * head_dim * 4);
@@ -73,13 +74,13 @@ PagedShape paged_shape(int head_dim, int n_seqs, int n_rows, int group, int n_kv
 
 template <int HD, int PL, int COLS>
 rs_status launch_paged(const PagedAttnArgs &a, const PagedShape &p, hipStream_t st) {
-    if constexpr (COLS == PAGED_COLS) hipLaunchKernelGGL((k_paged_wide<HD, PL>), dim3(p.runs), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_paged_narrow<HD, PL, COLS / 16>), dim3(p.runs), dim3(64), 0, st, a);
+    if constexpr (COLS == PAGED_COLS) hipLaunchKernelGGL((k_paged_wide<HD, PL>), dim3(a.runs), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_paged_narrow<HD, PL, COLS / 16>), dim3(a.runs), dim3(64), 0, st, a);
     RS_LAUNCHED("paged_attention");
     // about 2048 workgroups for the items that can be cut (one a run at most); the others end at once
     constexpr int per = join_cols<HD, COLS>();
-    const int cut = p.items < p.runs ? (int)p.items : p.runs, most = (a.rows * a.group + per - 1) / per, want = (2048 + cut - 1) / cut;
-    hipLaunchKernelGGL((k_paged_join<HD, PL, COLS>), dim3(p.runs, want < most ? want : most), dim3(256), 0, st, a);
+    const int cut = p.items < a.runs ? (int)p.items : a.runs, most = (a.rows * a.group + per - 1) / per, want = (2048 + cut - 1) / cut;
+    hipLaunchKernelGGL((k_paged_join<HD, PL, COLS>), dim3(a.runs, want < most ? want : most), dim3(256), 0, st, a);
     RS_LAUNCHED("paged_join");
     return RS_OK;
 }
@@ -219,8 +220,9 @@ rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n
     a.kc = (const uint16_t *)cache->k; a.vc = (const uint16_t *)cache->v;
     a.q = d_q; a.out = d_out; a.lse = d_lse; a.q_stride = q_stride; a.out_stride = out_stride;
     a.n_q = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.window = window; a.rows = p.rows;
+    a.runs = p.cols == PAGED_COLS && dtype == RS_F32 ? PAGED_WIDE_RUNS3 : p.runs;
     a.c = scale * 1.44269504088896341f;
-    a.cuts = (int4 *)d_scratch; a.odd = (unsigned int *)((unsigned char *)d_scratch + p.odd); a.part_ml = (float *)((unsigned char *)d_scratch + p.ml); a.part_o = (float *)((unsigned char *)d_scratch + p.o);
+    a.cuts = (int4 *)d_scratch; a.cut_of = (int2 *)((unsigned char *)d_scratch + p.of); a.odd = (unsigned int *)((unsigned char *)d_scratch + p.odd); a.part_ml = (float *)((unsigned char *)d_scratch + p.ml); a.part_o = (float *)((unsigned char *)d_scratch + p.o);
     return dtype == RS_F32 ? launch_paged_hd<3>(hd, a, p, (hipStream_t)stream) : launch_paged_hd<1>(hd, a, p, (hipStream_t)stream);
 }
 

@@ -25,16 +25,17 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int PAGED_COLS = 128;                // columns of a workgroup of k_paged_wide
 constexpr int PAGED_TILE = 6;                  // log2 positions of a tile
-constexpr int PAGED_WIDE_RUNS = 512, PAGED_NARROW_RUNS = 1024;
+constexpr int PAGED_WIDE_RUNS = 512, PAGED_WIDE_RUNS3 = 256, PAGED_NARROW_RUNS = 1024;      // of a call, at most: what the CUs hold at a time (RUNS3: with three planes)
 
 struct PagedAttnArgs {
     PagedSpans s;
     const uint16_t *kc, *vc;
     const void *q; void *out; float *lse;
     size_t q_stride, out_stride;
-    int n_q, group, window, rows;              // rows: of a block of columns
+    int n_q, group, window, rows, runs;        // rows: of a block of columns; runs: workgroups of the call
     float c;                                   // scale log2 e
-    int4 *cuts;                                // per run: the cut item that ends in it {sequence, KV head, block, first run}, sequence < 0: none
+    int4 *cuts;                                // per run: the cut item that ends in it {first row, KV head, columns, first run}, first row < 0: none
+    int2 *cut_of;                              // ... and its {sequence, block}
     unsigned int *odd;                         // per run: bit k % 32: its item k is whole and its sums hold a NaN
     float *part_ml, *part_o;                   // [2 runs][2][columns], [2 runs][columns][head_dim]
 };
@@ -42,18 +43,40 @@ struct PagedAttnArgs {
 struct PagedItem { int b, kvh, blk, n_blk; Span s; };
 struct PagedRun { PagedItem at; int ta; long long left, T; int W; };       // first item, first tile of it, tiles of the run
 
-constexpr int PAGED_RUN_LDS = 8;               // long long
+// Sum over this lane and those before it: in 32 bits without LDS where no sum passes them.
+__device__ __forceinline__ long long wave_prefix(long long v) {
+    if (!__any(v >= 1 << 24)) {
+        int x = (int)v;
+        x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8: within rows of 16 lanes
+        x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast15 into rows 1 and 3
+        x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // row_bcast31 into rows 2 and 3
+        return x;
+    }
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const long long u = __shfl_up(v, o, RS_WAVE); if (lane >= o) v += u; }
+    return v;
+}
+__device__ __forceinline__ long long lane_value(long long v, int lane) {
+    return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, lane));
+}
 
-// What run w of `most` has to do; false: nothing.  All NT threads of the workgroup get the same.  sh: PAGED_RUN_LDS long long (one wave: not used).
+constexpr int PAGED_RUN_LDS = 12;              // long long
+
+// What run w has to do; false: nothing.  All NT threads of the workgroup get the same.  sh: PAGED_RUN_LDS long long (one wave: not used).
 template <int NT>
-__device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int most, int w, long long *sh, PagedRun &run) {
+__device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int w, long long *sh, PagedRun &run) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.s.n_seqs;
-    // tiles per KV head of a few sequences a thread, or of one sequence by several threads
+    // tiles per KV head of a few sequences a thread, or, where there are many rows, of one sequence by several threads
     int share = 1;
-    while (share < 64 && 2 * share * n <= NT) share *= 2;
+    if (a.s.n_rows > 64 * a.rows) while (share < 64 && 2 * share * n <= NT) share *= 2;
     const int per = (n * share + NT - 1) / NT, b0 = min(tid / share * per, n), b1 = min(b0 + per, n), sub = tid % share;
+    Span s;
+    s.first = s.m = s.slot = s.p0 = 0;
     auto tiles = [&](int b, int from, int by) __attribute__((always_inline)) {
-        Span s;
         long long sum = 0;
         if (!paged_span(a.s, b, s)) { if (blockIdx.x == 0 && from == 0) paged_flag(a.s, b); }
         else {
@@ -66,18 +89,15 @@ __device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int most,
     for (int b = b0; b < b1; ++b) mine += tiles(b, sub, share);
     for (int o = 1; o < share; o <<= 1) mine += __shfl_xor(mine, o, RS_WAVE);
     const long long own = sub == 0 ? mine * a.s.n_kv : 0;
-    long long end = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const long long u = __shfl_up(end, o, RS_WAVE); if (lane >= o) end += u; }
-    long long T;
-    if constexpr (NT == 64) T = __shfl(end, 63, RS_WAVE);
+    long long end = wave_prefix(own), T;
+    if constexpr (NT == 64) T = lane_value(end, 63);
     else {
         if (lane == 63) sh[wave] = end;
         __syncthreads();
         T = 0;
         for (int i = 0; i < NT / 64; ++i) { if (i < wave) end += sh[i]; T += sh[i]; }
     }
-    const int W = T < most ? (int)T : most;                  // (a tile a run at least)
+    const int W = T < a.runs ? (int)T : a.runs;              // (a tile a run at least)
     if (w >= W) return false;
     const long long t0 = paged_run(T, W, w);
     run.T = T; run.W = W; run.left = paged_run(T, W, w + 1) - t0;
@@ -94,32 +114,31 @@ __device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int most,
                 rem -= of * a.s.n_kv;
             }
     }
+    PagedItem &it = run.at;
     if constexpr (NT == 64) {
         const int who = __ffsll((unsigned long long)__ballot(found)) - 1;
-        b = __shfl(b, who, RS_WAVE); rem = __shfl(rem, who, RS_WAVE); of = __shfl(of, who, RS_WAVE);
+        it.b = __builtin_amdgcn_readlane(b, who); rem = lane_value(rem, who); of = lane_value(of, who);
+        it.s.first = __builtin_amdgcn_readlane(s.first, who); it.s.m = __builtin_amdgcn_readlane(s.m, who);
+        it.s.slot = __builtin_amdgcn_readlane(s.slot, who); it.s.p0 = __builtin_amdgcn_readlane(s.p0, who);
     } else {
-        if (found) { sh[4] = b; sh[5] = rem; sh[6] = of; }
+        if (found) { sh[4] = b; sh[5] = rem; sh[6] = of; sh[7] = s.first; sh[8] = s.m; sh[9] = s.slot; sh[10] = s.p0; }
         __syncthreads();
-        b = (int)sh[4]; rem = sh[5]; of = sh[6];
+        auto value = [&](int i) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane((int)sh[i]); };
+        it.b = value(4); rem = lane_value(sh[5], 0); of = lane_value(sh[6], 0);
+        it.s.first = value(7); it.s.m = value(8); it.s.slot = value(9); it.s.p0 = value(10);
     }
-    PagedItem &it = run.at;
-    it.b = __builtin_amdgcn_readfirstlane(b);
-    (void)paged_span(a.s, it.b, it.s);
     it.n_blk = paged_blocks(it.s, a.rows);
-    const int kvh = rem >> 31 == 0 && of >> 31 == 0 ? (int)((unsigned)rem / (unsigned)of) : (int)(rem / of);
-    it.kvh = __builtin_amdgcn_readfirstlane(kvh);
-    rem -= kvh * of;
+    it.kvh = rem >> 31 == 0 && of >> 31 == 0 ? (int)((unsigned)rem / (unsigned)of) : (int)(rem / of);
+    rem -= it.kvh * of;
     int j = 0, u0, u1;
     if (it.n_blk > 1) {
         // the block, by every wave: a lane sums a run of blocks
         const int each = (it.n_blk + 63) / 64, j0 = min(lane * each, it.n_blk), j1 = min(j0 + each, it.n_blk);
         long long sum = 0;
         for (int i = j0; i < j1; ++i) { paged_tiles(it.s, a.rows, a.window, PAGED_TILE, i, u0, u1); sum += u1 - u0; }
-        long long upto = sum;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { const long long u = __shfl_up(upto, o, RS_WAVE); if (lane >= o) upto += u; }
+        const long long upto = wave_prefix(sum);
         const int who = __ffsll((unsigned long long)__ballot(rem < upto)) - 1;             // (rem < of: some lane has it)
-        rem -= __shfl(upto - sum, who, RS_WAVE);
+        rem -= lane_value(upto - sum, who);
         j = who * each;
     }
     for (;; ++j) {
@@ -142,9 +161,12 @@ __device__ __forceinline__ void paged_next(const PagedAttnArgs &a, PagedItem &it
     it.n_blk = paged_blocks(it.s, a.rows);
 }
 
-// If item `it`, of which this run w starts at tile ta > t0 and reaches the end, has been cut: who joins it.
+// If item `it`, of which this run w starts at tile ta > t0 and reaches the end, has been cut: what the joining kernel needs.
 __device__ __forceinline__ void paged_note_cut(const PagedAttnArgs &a, const PagedRun &run, const PagedItem &it, int w, int ta, int t0) {
-    if (threadIdx.x == 0) a.cuts[w] = make_int4(it.b, it.kvh, it.blk, paged_run_of(run.T, run.W, paged_run(run.T, run.W, w) - (ta - t0)));
+    if (threadIdx.x != 0) return;
+    const int r0 = it.blk * a.rows;
+    a.cuts[w] = make_int4(it.s.first + r0, it.kvh, min(a.rows, it.s.m - r0) * a.group, paged_run_of(run.T, run.W, paged_run(run.T, run.W, w) - (ta - t0)));
+    a.cut_of[w] = make_int2(it.b, it.blk);
 }
 
 // Page table entry of position pos, or of the position nearest to it among the needed ones, lo .. hi - 1; asked for ahead of its use, which checks it:
@@ -388,7 +410,7 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
     __shared__ __align__(16) unsigned char kb[64 * HD * 2], vb[64 * HD * 2];
     const int lane = threadIdx.x, col = lane & 15, hq = lane >> 4, w = blockIdx.x, ps = 1 << a.s.page_shift;
     PagedRun run;
-    const bool some = paged_find_run<64>(a, PAGED_NARROW_RUNS, w, nullptr, run);
+    const bool some = paged_find_run<64>(a, w, nullptr, run);
     if (lane == 0) { a.cuts[w] = make_int4(-1, 0, 0, 0); a.odd[w] = 0; }
     if (!some) return;
     // ---- the tile that is fetched next: `left` tiles of the run from it on, positions lo .. hi - 1 of its item are needed
@@ -573,15 +595,15 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
 // and 11 % of the requests met in L2: 8.7 GB at 6 TB/s from beyond it for the four chunks of 2048 rows on up to 14000 positions.
 // ------------------------------------------------------------------------------------------------
 template <int HD, int PL>
-__global__ void __launch_bounds__(256, 2) k_paged_wide(PagedAttnArgs a) {
+__global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnArgs a) {
     constexpr int NS = HD / 16, ND = HD / 32, COLS = PAGED_COLS, KB = 64 * HD * 2;
     constexpr int RB = PL == 1 ? 2 : 1;                                   // blocks of 32 positions whose scores are held at a time
     __shared__ __align__(16) unsigned char k0[KB], k1[KB], v0[KB], v1[KB];
     __shared__ long long run_sh[PAGED_RUN_LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hh = lane >> 5, ps = 1 << a.s.page_shift;
-    const int w = (blockIdx.x & 7) * (PAGED_WIDE_RUNS / 8) + (blockIdx.x >> 3);         // (workgroups go round the eight XCDs)
+    const int w = (blockIdx.x & 7) * (a.runs / 8) + (blockIdx.x >> 3);         // (workgroups go round the eight XCDs)
     PagedRun run;
-    const bool some = paged_find_run<256>(a, PAGED_WIDE_RUNS, w, run_sh, run);
+    const bool some = paged_find_run<256>(a, w, run_sh, run);
     if (tid == 0) { a.cuts[w] = make_int4(-1, 0, 0, 0); a.odd[w] = 0; }
     if (!some) return;
     PagedItem it = run.at;
@@ -774,11 +796,8 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
     const int4 cut = a.cuts[w];
     const unsigned int odd = blockIdx.y == 0 ? a.odd[w] : 0;
     if (cut.x < 0 && !odd) return;
-    PagedItem it;
     if (cut.x >= 0) {
-        it.b = cut.x; it.kvh = cut.y; it.blk = cut.z;
-        (void)paged_span(a.s, cut.x, it.s);
-        const int r0 = it.blk * a.rows, n_col = min(a.rows, it.s.m - r0) * a.group, n = w - cut.w + 1;
+        const int kvh = cut.y, n_col = cut.z, n = w - cut.w + 1;
         const int unit = threadIdx.x / TPC, g = unit / CPW, lc = unit % CPW, d = 4 * (threadIdx.x % TPC);
         for (int from = blockIdx.y * CPW; from < n_col; from += gridDim.y * CPW) {
         const int c = from + lc;
@@ -791,20 +810,21 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
                 float4 y[BATCH];
 #pragma unroll
                 for (int k = 0; k < BATCH; ++k) {
-                    const int i = min(i0 + G * k, n - 1);
+                    const int i = i0 + G * k;
+                    m[k] = -INFINITY; l[k] = 0.f; y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (i >= n) continue;
                     const size_t part = 2 * (size_t)(cut.w + i) + (i == 0);
                     m[k] = a.part_ml[part * 2 * COLS + c]; l[k] = a.part_ml[(part * 2 + 1) * COLS + c];
                     y[k] = *reinterpret_cast<const float4 *>(a.part_o + (part * COLS + c) * HD + d);
                 }
                 float top = M;
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) { if (i0 + G * k >= n) m[k] = -INFINITY; top = fmaxf(top, m[k]); }
+                for (int k = 0; k < BATCH; ++k) top = fmaxf(top, m[k]);
                 const float tc = top == -INFINITY ? 0.f : top * a.c, e0 = __builtin_amdgcn_exp2f(fmaf(M, a.c, -tc));
                 M = top; L *= e0; x[0] *= e0; x[1] *= e0; x[2] *= e0; x[3] *= e0;
 #pragma unroll
                 for (int k = 0; k < BATCH; ++k) {
                     const float e = __builtin_amdgcn_exp2f(fmaf(m[k], a.c, -tc));
-                    if (i0 + G * k >= n) continue;
                     L = fmaf(l[k], e, L);
                     x[0] = fmaf(y[k].x, e, x[0]); x[1] = fmaf(y[k].y, e, x[1]); x[2] = fmaf(y[k].z, e, x[2]); x[3] = fmaf(y[k].w, e, x[3]);
                 }
@@ -828,8 +848,8 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
             }
         }
         if (c < n_col && g == 0) {
-            const int r = c / a.group, h = it.kvh * a.group + c - r * a.group;
-            const size_t row = (size_t)(it.s.first + r0 + r);
+            const int r = c / a.group, h = kvh * a.group + c - r * a.group;
+            const size_t row = (size_t)(cut.x + r);
             const float inv = 1.f / L, all = (x[0] + x[1]) + (x[2] + x[3]);
             nan = all != all;
             paged_store4<PL>(a.out, row * a.out_stride + (size_t)h * HD + d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
@@ -837,15 +857,17 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
         }
         if (__syncthreads_or(nan)) {
             const int c0 = (from & ~31) + 32 * wave;
+            PagedItem it;
+            it.b = a.cut_of[w].x; it.blk = a.cut_of[w].y; it.kvh = kvh;
+            (void)paged_span(a.s, it.b, it.s);
             if (c0 < min(from + CPW, n_col)) paged_careful<HD, PL>(a, it, c0, from, from + CPW);
         }
         }
     }
     if (!odd) return;
     PagedRun run;
-    constexpr bool WIDE = COLS == PAGED_COLS;
-    if (!paged_find_run<256>(a, WIDE ? PAGED_WIDE_RUNS : PAGED_NARROW_RUNS, w, run_sh, run)) return;
-    it = run.at;
+    if (!paged_find_run<256>(a, w, run_sh, run)) return;
+    PagedItem it = run.at;
     for (int k = 0, ta = run.ta;; ++k) {
         int t0, t1;
         paged_tiles(it.s, a.rows, a.window, PAGED_TILE, it.blk, t0, t1);
