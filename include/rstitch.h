@@ -476,6 +476,27 @@ rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n
                              float scale, int32_t window, void *d_out, int64_t out_stride, float *d_lse,
                              uint32_t *d_flags, void *d_scratch, size_t scratch_bytes, void *stream);
 
+/* A model whose K/V cache is in pages: rs_decode_step and rs_catchup_prefill as
+ * for a model of rs_create_model, with the sequences' pages in the place of
+ * slots of max_ctx positions.  Pages are the caller's to hand out: before a call,
+ * page_table has to name a page for every position up to the last row's of each
+ * sequence.  The table is read on the device when a call runs, so it may change
+ * from call to call, also of a call that is replayed.
+ *   cache   k, v: the pages of all layers, [n_layers][n_pages]..; 256-byte aligned;
+ *           one page table for all of them, rows = sequence slots.  n_kv_heads and
+ *           head_dim are the configuration's, n_slots >= max_seqs, page_size *
+ *           max_pages >= max_ctx
+ *   workspace  as in rs_create_model, of at least rs_paged_workspace_bytes (0 on a
+ *           bad argument)
+ * A row whose page is no page of the cache is skipped and RS_FLAG_BADARG set in the
+ * record of its sequence, and in that of one which sees such a page.
+ * rs_stitch_generate does not take such a model (RS_ENOTIMPL).
+ * Errors: as rs_create_model. */
+size_t    rs_paged_workspace_bytes(const rs_config *cfg, const rs_paged_kv *cache);
+rs_status rs_create_model_paged(const rs_config *cfg, const rs_weights *weights,
+                                const rs_paged_kv *cache, void *workspace,
+                                size_t workspace_bytes, rs_model **out);
+
 #ifdef __cplusplus
 }
 #endif

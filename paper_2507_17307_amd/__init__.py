@@ -12,6 +12,6 @@ from .binding import (  # noqa: F401
     rs_decode_step, rs_catchup_prefill, rs_route, rs_route_plus, RouterPlus, rs_route_static, rs_route_scratch_bytes, rs_set_phase_timer, rs_set_spin_limit, rs_set_sampling,
     rs_stitch_generate, STITCH_RUNNING, STITCH_DONE, STITCH_TRACE_FULL, STITCH_FLAGGED, STITCH_ABORTED,
     RS_F32, RS_BF16, ROPE_PLAIN, ROPE_LINEAR, ROPE_BY_PARTS, PagedCache, Rope, rs_rope_frequencies, rs_rope_rows, rs_paged_append,
-    rs_paged_attention, rs_paged_attention_scratch_bytes,
-    Model,
+    rs_paged_attention, rs_paged_attention_scratch_bytes, rs_paged_workspace_bytes, rs_create_model_paged,
+    Model, PagedModel,
 )

@@ -103,6 +103,10 @@ def _load() -> C.CDLL:
     lib.rs_paged_attention_scratch_bytes.argtypes = [C.POINTER(_RsPagedKv), i32, i32, i32]
     lib.rs_paged_attention.restype = i32
     lib.rs_paged_attention.argtypes = [C.POINTER(_RsPagedKv), i32, i32, vp, vp, vp, i32, i32, vp, i64, f32, i32, vp, i64, vp, vp, vp, sz, vp]
+    lib.rs_paged_workspace_bytes.restype = sz
+    lib.rs_paged_workspace_bytes.argtypes = [C.POINTER(RsConfig), C.POINTER(_RsPagedKv)]
+    lib.rs_create_model_paged.restype = i32
+    lib.rs_create_model_paged.argtypes = [C.POINTER(RsConfig), C.POINTER(_RsWeights), C.POINTER(_RsPagedKv), vp, sz, C.POINTER(vp)]
     lib.rs_set_spin_limit.restype = i32
     lib.rs_set_spin_limit.argtypes = [vp, C.c_uint32]
     lib.rs_set_phase_timer.restype = i32
@@ -151,20 +155,36 @@ def rs_kv_bytes(cfg: RsConfig) -> int:
     return lib.rs_kv_bytes(C.byref(cfg))
 
 
-def rs_create_model(cfg: RsConfig, weights, kv_k: torch.Tensor, kv_v: torch.Tensor,
-                    workspace: torch.Tensor) -> int:
-    """weights: object with embed, lm_head, final_norm and layers[*].{attn_norm,w_qkv,w_o,mlp_norm,
-    w_gate_up,w_down} as contiguous bf16 device tensors.  Returns the opaque handle."""
+def _marshal_weights(cfg: RsConfig, weights):
     n = cfg.n_layers
     arrs = {}
     for name in ("attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down"):
         arrs[name] = (C.c_void_p * n)(*[getattr(l, name).data_ptr() for l in weights.layers])
-    w = _RsWeights(weights.embed.data_ptr(), weights.lm_head.data_ptr(), weights.final_norm.data_ptr(),
-                   *[C.cast(arrs[k], C.POINTER(C.c_void_p)) for k in
-                     ("attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")])
+    return _RsWeights(weights.embed.data_ptr(), weights.lm_head.data_ptr(), weights.final_norm.data_ptr(),
+                      *[C.cast(arrs[k], C.POINTER(C.c_void_p)) for k in
+                        ("attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")])
+
+
+def rs_create_model(cfg: RsConfig, weights, kv_k: torch.Tensor, kv_v: torch.Tensor,
+                    workspace: torch.Tensor) -> int:
+    """weights: object with embed, lm_head, final_norm and layers[*].{attn_norm,w_qkv,w_o,mlp_norm,
+    w_gate_up,w_down} as contiguous bf16 device tensors.  Returns the opaque handle."""
+    w = _marshal_weights(cfg, weights)
     handle = C.c_void_p()
     _check(lib.rs_create_model(C.byref(cfg), C.byref(w), kv_k.data_ptr(), kv_v.data_ptr(), workspace.data_ptr(),
                                workspace.numel() * workspace.element_size(), C.byref(handle)))
+    return handle.value
+
+
+def rs_paged_workspace_bytes(cfg: RsConfig, cache: _RsPagedKv) -> int:
+    return lib.rs_paged_workspace_bytes(C.byref(cfg), C.byref(cache))
+
+
+def rs_create_model_paged(cfg: RsConfig, weights, cache: _RsPagedKv, workspace: torch.Tensor) -> int:
+    """cache: the marshalled pages of all layers (PagedModel.cache_struct)."""
+    w = _marshal_weights(cfg, weights)
+    handle = C.c_void_p()
+    _check(lib.rs_create_model_paged(C.byref(cfg), C.byref(w), C.byref(cache), workspace.data_ptr(), workspace.numel() * workspace.element_size(), C.byref(handle)))
     return handle.value
 
 
@@ -505,3 +525,56 @@ class Model:
             else:
                 res = self.catchup_prefill([chunk], [pos0 + s], tau, active, [scale], [slot], want_logits)
         return res
+
+
+class PagedModel(Model):
+    """A Model whose K/V cache is a pool of n_pages pages of page_size positions that its sequence slots draw from.
+
+    reserve(slot, positions) gives a slot the pages for its first `positions` positions (the calls do not do it by
+    themselves: the tokens a call feeds need their pages before it), release(slot) gives them back.  Both write the page table
+    on the current stream, after which calls on that stream see it."""
+
+    def __init__(self, weights, max_ctx: int, n_pages: int, page_size: int = 64, max_seqs: int = 1, max_rows: int = 64, device="cuda"):
+        self.handle = 0
+        self.shape = s = weights.shape
+        self.weights = weights
+        max_ctx = (max_ctx + 7) // 8 * 8
+        self.cfg = make_config(s, max_ctx, max_seqs, max_rows)
+        self.page_size, self.n_pages = page_size, n_pages
+        self.pages_k = torch.zeros(s.n_layers, n_pages, s.n_kv_heads, page_size, s.head_dim, dtype=torch.bfloat16, device=device)
+        self.pages_v = torch.zeros(s.n_layers, n_pages, s.n_kv_heads, s.head_dim, page_size, dtype=torch.bfloat16, device=device)
+        self.page_table = torch.full((max_seqs, (max_ctx + page_size - 1) // page_size), -1, dtype=torch.int32, device=device)
+        self.cache_struct = _RsPagedKv(self.pages_k.data_ptr(), self.pages_v.data_ptr(), self.page_table.data_ptr(), n_pages, page_size, max_seqs,
+                                       self.page_table.shape[1], s.n_kv_heads, s.head_dim)
+        wsb = rs_paged_workspace_bytes(self.cfg, self.cache_struct)
+        if wsb == 0:
+            raise RsError(-1, rs_last_error())
+        self.workspace = torch.zeros(wsb, dtype=torch.uint8, device=device)
+        self.device = device
+        self._free = list(range(n_pages - 1, -1, -1))
+        self._held: List[List[int]] = [[] for _ in range(max_seqs)]
+        self.handle = rs_create_model_paged(self.cfg, weights, self.cache_struct, self.workspace)
+
+    def reserve(self, slot: int, positions: int) -> None:
+        held, more = self._held[slot], (positions + self.page_size - 1) // self.page_size - len(self._held[slot])
+        if positions > self.cfg.max_ctx:
+            raise RsError(-2, f"{positions} positions do not fit max_ctx {self.cfg.max_ctx}")
+        if more <= 0:
+            return
+        if more > len(self._free):
+            raise RsError(-2, f"{more} pages wanted, {len(self._free)} are free")
+        at = len(held)
+        held.extend(self._free.pop() for _ in range(more))
+        self.page_table[slot, at:len(held)] = self._i32(held[at:])
+
+    def release(self, slot: int) -> None:
+        held = self._held[slot]
+        self.page_table[slot].fill_(-1)
+        self._free.extend(reversed(held))
+        held.clear()
+
+    def kv_view(self, which: str, slot: int = 0) -> torch.Tensor:
+        """[layer, kv_head, position, head_dim]: a copy of the positions of a slot's pages, in order."""
+        pages = torch.tensor(self._held[slot], dtype=torch.long, device=self.device)
+        t = self.pages_k[:, pages] if which == "k" else self.pages_v[:, pages].transpose(3, 4)
+        return t.transpose(1, 2).flatten(2, 3)

@@ -25,6 +25,9 @@ struct PrepArgs {
     const float *scale;
     const uint16_t *embed;
     int *row_slot, *row_pos, *row_bad, *out_row, *seq_bad;
+    // a cache in pages: page_table not null, row_slot gets the row's page and row_at its place there
+    const int *page_table; int n_pages, max_pages, page_shift;
+    int *row_at;
     int4 *seq_info;                // per sequence {first row, end row, cache slot, first row's position}; first row = -1 for an invalid one
     float *seq_scale;
     // walked attention (attn_plan.h); all null or zero in calls that do not take it
@@ -88,18 +91,23 @@ __device__ __forceinline__ void prepare_row(const PrepArgs &a, int r, int *sh) {
     const int top = sh[1];
     if (b == INT_MAX) { b = -1; bad = 1; lo = 0; hi = 0; }
     else if (a.span_off != nullptr) { lo = s_off[b]; hi = s_off[b + 1]; }
-    int bad2 = 0;
+    int bad2 = 0, page = 0;
     if (!bad) {
         const int slot = s_slot[b], p0 = s_pos[b];
         if (slot < 0 || slot >= a.max_seqs || p0 < 0 || p0 > a.max_ctx - (hi - lo)) bad2 = 1;
+        else if (a.page_table) {
+            page = a.page_table[(size_t)slot * a.max_pages + ((p0 + r - lo) >> a.page_shift)];
+            if (page < 0 || page >= a.n_pages) bad2 = 1;
+        }
         if (tid < ns && tid != b && s_slot[tid] == slot) bad2 = 1;       // slots must be distinct
         if (tid >= lo && tid < hi && (s_tok[tid] < 0 || s_tok[tid] >= a.vocab)) bad2 = 1;
     }
     bad |= __syncthreads_or(bad2);
     if (tid == 0) {
         a.row_bad[r] = bad;
-        a.row_slot[r] = bad ? 0 : s_slot[b];
+        a.row_slot[r] = bad ? 0 : a.page_table ? page : s_slot[b];
         a.row_pos[r] = bad ? 0 : s_pos[b] + (r - lo);
+        if (a.page_table) a.row_at[r] = bad ? 0 : (s_pos[b] + (r - lo)) & ((1 << a.page_shift) - 1);
         if (b >= 0 && r == hi - 1 && b < ns) {
             a.out_row[b] = r; a.seq_bad[b] = bad;
             a.seq_scale[b] = s_scale[b];
@@ -233,7 +241,7 @@ struct GemvArgs {
     float *qbuf; uint16_t *kcache, *vcache;               // QKV outputs (q rows [m][n_q*hd])
     const float *rope_cos, *rope_sin;                     // [max_ctx, head_dim/2]
     int n_q, n_kv, head_dim, max_ctx, max_seqs, layer, d_ffn;
-    const int *row_pos, *row_slot, *row_bad;
+    const int *row_pos, *row_slot, *row_bad, *row_at;     // row_at: place of the row's K/V in its slot (row_pos) or page
     const float *seq_scale; SoftPartial *parts; int n_parts; float *logits;   // LM head
     int sample_on; unsigned long long sample_key;         // LM head: also track the arg max of logit + Gumbel noise (needs row_pos)
 };
@@ -317,11 +325,11 @@ __device__ __forceinline__ void gemv_phase(const GemvArgs &a, unsigned char *sme
     }
 
     // row position / slot (QKV only), read once up front so that no epilogue waits on it
-    int row_bad[MP], row_pos[MP], row_slot[MP];
+    int row_bad[MP], row_pos[MP], row_slot[MP], row_at[MP];
 #pragma unroll
     for (int m = 0; m < MP; ++m) {
-        row_bad[m] = 1; row_pos[m] = 0; row_slot[m] = 0;
-        if (MODE == G_QKV && m < M) { row_bad[m] = a.row_bad[m]; row_pos[m] = a.row_pos[m]; row_slot[m] = a.row_slot[m]; }
+        row_bad[m] = 1; row_pos[m] = 0; row_slot[m] = 0; row_at[m] = 0;
+        if (MODE == G_QKV && m < M) { row_bad[m] = a.row_bad[m]; row_pos[m] = a.row_pos[m]; row_slot[m] = a.row_slot[m]; row_at[m] = a.row_at[m]; }
     }
 
     // ---- prologue: x (fp32) into LDS.  Norm phases: K = d_model fits one segment for every MP.
@@ -543,7 +551,7 @@ __device__ __forceinline__ void gemv_phase(const GemvArgs &a, unsigned char *sme
             if (m >= M) continue;
             if (MODE == G_QKV) {
                 if (row_bad[m]) continue;
-                const int pos = row_pos[m], slot = row_slot[m];
+                const int pos = row_at[m], slot = row_slot[m];
                 if (rot) {
 #pragma unroll
                     for (int j = 0; j < P; ++j) {
@@ -680,11 +688,11 @@ __global__ void __launch_bounds__(256) k_gemv_reg(GemvArgs a) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) pre[u][r] = load_stream(reinterpret_cast<const uint4 *>(a.W + (size_t)rows0[r] * K) + lane + 64 * u);
     }
-    int row_bad[MP], row_pos[MP], row_slot[MP];
+    int row_bad[MP], row_pos[MP], row_slot[MP], row_at[MP];
 #pragma unroll
     for (int m = 0; m < MP; ++m) {
-        row_bad[m] = 1; row_pos[m] = 0; row_slot[m] = 0;
-        if (MODE == G_QKV && m < M) { row_bad[m] = a.row_bad[m]; row_pos[m] = a.row_pos[m]; row_slot[m] = a.row_slot[m]; }
+        row_bad[m] = 1; row_pos[m] = 0; row_slot[m] = 0; row_at[m] = 0;
+        if (MODE == G_QKV && m < M) { row_bad[m] = a.row_bad[m]; row_pos[m] = a.row_pos[m]; row_slot[m] = a.row_slot[m]; row_at[m] = a.row_at[m]; }
     }
 
     // ---- x into registers: token row m, chunk u of this lane (a row past the call's count is a copy of row 0, never written)
@@ -803,7 +811,7 @@ __global__ void __launch_bounds__(256) k_gemv_reg(GemvArgs a) {
             if (m >= M) continue;
             if (MODE == G_QKV) {
                 if (row_bad[m]) continue;
-                const int pos = row_pos[m], slot = row_slot[m];
+                const int pos = row_at[m], slot = row_slot[m];
                 if (rot) {
 #pragma unroll
                     for (int j = 0; j < P; ++j) {

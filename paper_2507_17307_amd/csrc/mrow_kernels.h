@@ -106,7 +106,7 @@ struct RopeArgs {
     int ksplit; size_t part_stride;
     float *qbuf; uint16_t *kcache, *vcache;
     const float *rope_cos, *rope_sin;
-    const int *row_pos, *row_slot, *row_bad;
+    const int *row_pos, *row_slot, *row_bad, *row_at;     // row_at: place of the row's K/V in its slot (row_pos) or page
     int n_q, n_kv, head_dim, max_ctx, max_seqs, layer;
 };
 inline int rope_blocks(int n_q, int n_kv, int hd) { return ((n_q + n_kv) * (hd / 8) + n_kv * (hd / 4) + ROPE_THREADS - 1) / ROPE_THREADS; }
@@ -114,7 +114,7 @@ inline int rope_blocks(int n_q, int n_kv, int hd) { return ((n_q + n_kv) * (hd /
 __global__ void __launch_bounds__(ROPE_THREADS) k_rope_kv_rows(RopeArgs a) {
     const int r = blockIdx.x, hd = a.head_dim, half = hd >> 1, quads = half >> 2;
     const int n_rot = (a.n_q + a.n_kv) * quads, p4 = blockIdx.y * ROPE_THREADS + threadIdx.x;
-    const int bad = a.row_bad[r], pos = a.row_pos[r], slot = a.row_slot[r];
+    const int bad = a.row_bad[r], pos = a.row_pos[r], slot = a.row_slot[r], at = a.row_at[r];
     const size_t xo = (size_t)r * (a.n_q + 2 * a.n_kv) * hd;
     const int ks_n = a.ksplit > 1 ? a.ksplit : 1;
     if (p4 < n_rot) {
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_rope_kv_rows(RopeArgs a) {
         if (head < a.n_q) {
             *reinterpret_cast<float4 *>(q + i) = y0; *reinterpret_cast<float4 *>(q + i + half) = y1;
         } else {
-            const size_t base = ((((size_t)a.layer * a.max_seqs + slot) * a.n_kv + (head - a.n_q)) * a.max_ctx + pos) * hd;
+            const size_t base = ((((size_t)a.layer * a.max_seqs + slot) * a.n_kv + (head - a.n_q)) * a.max_ctx + at) * hd;
             *reinterpret_cast<uint2 *>(a.kcache + base + i) = make_uint2(pack_bf16x2(y0.x, y0.y), pack_bf16x2(y0.z, y0.w));
             *reinterpret_cast<uint2 *>(a.kcache + base + i + half) = make_uint2(pack_bf16x2(y1.x, y1.y), pack_bf16x2(y1.z, y1.w));
         }
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_rope_kv_rows(RopeArgs a) {
         const size_t e0 = xo + (a.n_q + a.n_kv) * hd + p;
         const float4 x = sum_splits4(a.qkv, e0, ks_n, a.part_stride, *reinterpret_cast<const float4 *>(a.qkv + e0));
         const size_t base = (((size_t)a.layer * a.max_seqs + slot) * a.n_kv + vh) * (size_t)a.max_ctx * hd;
-        uint16_t *vp = a.vcache + base + (size_t)e * a.max_ctx + pos;          // V is stored [hd][position]
+        uint16_t *vp = a.vcache + base + (size_t)e * a.max_ctx + at;          // V is stored [hd][position]
         vp[0] = f32_to_bf16(x.x); vp[a.max_ctx] = f32_to_bf16(x.y); vp[2 * (size_t)a.max_ctx] = f32_to_bf16(x.z); vp[3 * (size_t)a.max_ctx] = f32_to_bf16(x.w);
     }
 }

@@ -1,114 +1,7 @@
-// C entry points of the caches in pages (see include/rstitch.h): argument checks and launches.  Included by rstitch.hip.
+// C entry points of the operators on caches in pages (see include/rstitch.h).  Included by rstitch.hip.
 #pragma once
 
-#include "paged_attention.h"
-#include "paged_rope.h"
-
-namespace {
-
-const char *check_paged(const rs_paged_kv *c) {
-    if (!c) return "null cache";
-    if (!c->k || !c->v || !c->page_table) return "null cache pointer";
-    if (((uintptr_t)c->k | (uintptr_t)c->v) % 16) return "K and V pages must be 16-byte aligned";
-    if (c->n_pages < 1 || c->n_slots < 1 || c->max_pages < 1 || c->n_kv_heads < 1) return "cache with a count below 1";
-    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return "page_size must be a power of two in 16..1024";
-    if ((long long)c->page_size * c->max_pages > (1LL << 30)) return "page_size * max_pages must not exceed 2^30";
-    if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 32, 64 or 128";
-    if (c->n_kv_heads > 1024) return "more than 1024 KV heads";
-    return nullptr;
-}
-
-const char *check_rope(const rs_rope *r, int head_dim) {
-    if (r->rot_dim < 8 || r->rot_dim % 8 || r->rot_dim > head_dim) return "rot_dim must be a multiple of 8 in 8..head_dim";
-    if (r->interleaved != 0 && r->interleaved != 1) return "interleaved must be 0 or 1";
-    if (!r->d_inv_freq || (uintptr_t)r->d_inv_freq % 8) return "null or misaligned d_inv_freq";
-    if (!std::isfinite(r->amplitude)) return "amplitude must be finite";
-    return nullptr;
-}
-
-// Rows of `heads` heads, `stride` elements apart.
-const char *check_rows(const void *p, int64_t stride, int dtype, long long heads, int head_dim) {
-    const int size = dtype == RS_BF16 ? 2 : 4;
-    if (!p) return "null row pointer";
-    if ((uintptr_t)p % 16 || stride % (16 / size)) return "rows must be 16-byte aligned";
-    if (stride < heads * head_dim) return "a row stride is smaller than a row";
-    if (stride > ((int64_t)1 << 40)) return "a row stride is too large";
-    return nullptr;
-}
-
-rs_status check_spans(int32_t n_seqs, int32_t n_rows, const int32_t *slot, const int32_t *off, const int32_t *pos0, int dtype) {
-    if (n_seqs < 1 || n_rows < 1) return fail(RS_EINVAL, "n_seqs and n_rows must be at least 1");
-    if (n_seqs > PAGED_MAX_SEQS) return fail(RS_ECAPACITY, "n_seqs %d exceeds %d", n_seqs, PAGED_MAX_SEQS);
-    if (n_rows > (1 << 22)) return fail(RS_ECAPACITY, "n_rows %d exceeds 2^22", n_rows);
-    if (!slot || !pos0) return fail(RS_EINVAL, "null argument");
-    if (!off && n_rows < n_seqs) return fail(RS_EINVAL, "%d sequences of one row do not fit %d rows", n_seqs, n_rows);
-    if (dtype != RS_F32 && dtype != RS_BF16) return fail(RS_EINVAL, "dtype must be RS_F32 or RS_BF16");
-    return RS_OK;
-}
-
-PagedSpans paged_spans(const rs_paged_kv *c, int32_t n_seqs, int32_t n_rows, const int32_t *slot, const int32_t *off, const int32_t *pos0, uint32_t *flags) {
-    PagedSpans s{};
-    s.slot = slot; s.off = off; s.pos0 = pos0; s.table = c->page_table;
-    s.n_seqs = n_seqs; s.n_rows = n_rows; s.n_slots = c->n_slots; s.n_pages = c->n_pages; s.max_pages = c->max_pages; s.n_kv = c->n_kv_heads;
-    s.page_shift = __builtin_ctz((unsigned)c->page_size);
-    s.flags = flags;
-    return s;
-}
-
-// Which kernel takes a call: blocks of 16 or 32 columns where the spans have no more than that on average, else of 128.
-struct PagedShape { int cols, rows, runs; long long items; size_t of, odd, ml, o, total; };
-PagedShape paged_shape(int head_dim, int n_seqs, int n_rows, int group, int n_kv) {
-    PagedShape p{};
-    const long long slots = ((long long)n_rows * group + n_seqs - 1) / n_seqs;
-    p.cols = slots <= 16 ? 16 : slots <= 32 ? 32 : PAGED_COLS;
-    p.rows = p.cols / group;
-    p.runs = p.cols == PAGED_COLS ? PAGED_WIDE_RUNS : PAGED_NARROW_RUNS;
-    p.items = ((long long)n_rows / p.rows + n_seqs) * n_kv;                     // at most
-    p.of = align_up((size_t)p.runs * sizeof(int4));
-    p.odd = p.of + align_up((size_t)p.runs * sizeof(int2));
-    p.ml = p.odd + align_up((size_t)p.runs * 4);
-    p.o = p.ml + align_up((size_t)2 * p.runs * 2 * p.cols * 4);
-    p.total = p.o + align_up((size_t)2 * p.runs * p.cols * head_dim * 4);
-    return p;
-}
-
-template <int HD, int PL, int COLS>
-rs_status launch_paged(const PagedAttnArgs &a, const PagedShape &p, hipStream_t st) {
-    if constexpr (COLS == PAGED_COLS) hipLaunchKernelGGL((k_paged_wide<HD, PL>), dim3(a.runs), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_paged_narrow<HD, PL, COLS / 16>), dim3(a.runs), dim3(64), 0, st, a);
-    RS_LAUNCHED("paged_attention");
-    // about 2048 workgroups for the items that can be cut (one a run at most); the others end at once
-    constexpr int per = join_cols<HD, COLS>();
-    const int cut = p.items < a.runs ? (int)p.items : a.runs, most = (a.rows * a.group + per - 1) / per, want = (2048 + cut - 1) / cut;
-    hipLaunchKernelGGL((k_paged_join<HD, PL, COLS>), dim3(a.runs, want < most ? want : most), dim3(256), 0, st, a);
-    RS_LAUNCHED("paged_join");
-    return RS_OK;
-}
-template <int HD, int PL>
-rs_status launch_paged_cols(const PagedAttnArgs &a, const PagedShape &p, hipStream_t st) {
-    switch (p.cols) {
-        case 16: return launch_paged<HD, PL, 16>(a, p, st);
-        case 32: return launch_paged<HD, PL, 32>(a, p, st);
-        default: return launch_paged<HD, PL, PAGED_COLS>(a, p, st);
-    }
-}
-template <int PL>
-rs_status launch_paged_hd(int head_dim, const PagedAttnArgs &a, const PagedShape &p, hipStream_t st) {
-    switch (head_dim) {
-        case 32: return launch_paged_cols<32, PL>(a, p, st);
-        case 64: return launch_paged_cols<64, PL>(a, p, st);
-        default: return launch_paged_cols<128, PL>(a, p, st);
-    }
-}
-
-const char *check_paged_attention(const rs_paged_kv *c, int32_t n_q_heads) {
-    if (const char *why = check_paged(c)) return why;
-    if (n_q_heads < 1 || n_q_heads % c->n_kv_heads) return "n_kv_heads must divide n_q_heads";
-    if (n_q_heads / c->n_kv_heads > 16) return "more than 16 query heads per KV head";
-    return nullptr;
-}
-
-}  // namespace
+#include "paged_launch.h"
 
 extern "C" {
 
@@ -182,9 +75,13 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.q_out_stride = q_out_stride;
     if (rope) { a.inv_freq = rope->d_inv_freq; a.amplitude = rope->amplitude; a.half = rope->rot_dim / 2; a.interleaved = rope->interleaved; }
     a.n_q = n_q_heads; a.head_dim = hd;
-    a.heads_wg = 8; a.v_heads_wg = 1;
-    a.rope_wgs = (n_q_heads + cache->n_kv_heads + a.heads_wg - 1) / a.heads_wg;
-    const dim3 grid(append_blocks_most(n_seqs, n_rows), a.rope_wgs + (cache->n_kv_heads + a.v_heads_wg - 1) / a.v_heads_wg);
+    const int blocks = append_blocks_most(n_seqs, n_rows);
+    // eight q and k heads a workgroup, which share the sines and cosines of its rows, or fewer where that leaves under 512 workgroups (us, 128 rows of one
+    // position 6.2 with eight heads each, 9.0 with four; chunks of 8192 rows 47 with eight, 50 with six; 517 rows in 26 blocks 24 with eight, 12 with two)
+    const int heads = n_q_heads + cache->n_kv_heads, split = (512 + blocks - 1) / blocks, each = (heads + split - 1) / split;
+    a.heads_wg = each < 8 ? each : 8; a.v_heads_wg = 1;
+    a.rope_wgs = (heads + a.heads_wg - 1) / a.heads_wg;
+    const dim3 grid(blocks, a.rope_wgs + (cache->n_kv_heads + a.v_heads_wg - 1) / a.v_heads_wg);
     const size_t lds = append_lds_bytes(a.half, hd);
     hipStream_t st = (hipStream_t)stream;
     if (dtype == RS_F32) hipLaunchKernelGGL((k_paged_append<float, 4>), grid, dim3(256), lds, st, a);
@@ -197,7 +94,7 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
 size_t rs_paged_attention_scratch_bytes(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, int32_t n_q_heads) {
     if (const char *why = check_paged_attention(cache, n_q_heads)) { fail(RS_EINVAL, "%s", why); return 0; }
     if (n_seqs < 1 || n_rows < 1 || n_seqs > PAGED_MAX_SEQS || n_rows > (1 << 22)) { fail(RS_EINVAL, "n_seqs must be in 1..%d and n_rows in 1..2^22", PAGED_MAX_SEQS); return 0; }
-    return paged_shape(cache->head_dim, n_seqs, n_rows, n_q_heads / cache->n_kv_heads, cache->n_kv_heads).total;
+    return paged_shape(cache, n_seqs, n_rows, n_q_heads).total;
 }
 
 rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, const int32_t *d_seq_slot, const int32_t *d_span_offset,
@@ -214,16 +111,8 @@ rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n
     if (!d_scratch || (uintptr_t)d_scratch % ALIGN) return fail(RS_EINVAL, "scratch must be 256-byte aligned");
     const size_t need = rs_paged_attention_scratch_bytes(cache, n_seqs, n_rows, n_q_heads);
     if (scratch_bytes < need) return fail(RS_EINVAL, "scratch of %zu bytes is smaller than the %zu needed", scratch_bytes, need);
-    PagedAttnArgs a{};
-    const PagedShape p = paged_shape(hd, n_seqs, n_rows, n_q_heads / cache->n_kv_heads, cache->n_kv_heads);
-    a.s = paged_spans(cache, n_seqs, n_rows, d_seq_slot, d_span_offset, d_pos0, d_flags);
-    a.kc = (const uint16_t *)cache->k; a.vc = (const uint16_t *)cache->v;
-    a.q = d_q; a.out = d_out; a.lse = d_lse; a.q_stride = q_stride; a.out_stride = out_stride;
-    a.n_q = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.window = window; a.rows = p.rows;
-    a.runs = p.cols == PAGED_COLS && dtype == RS_F32 ? PAGED_WIDE_RUNS3 : p.runs;
-    a.c = scale * 1.44269504088896341f;
-    a.cuts = (int4 *)d_scratch; a.cut_of = (int2 *)((unsigned char *)d_scratch + p.of); a.odd = (unsigned int *)((unsigned char *)d_scratch + p.odd); a.part_ml = (float *)((unsigned char *)d_scratch + p.ml); a.part_o = (float *)((unsigned char *)d_scratch + p.o);
-    return dtype == RS_F32 ? launch_paged_hd<3>(hd, a, p, (hipStream_t)stream) : launch_paged_hd<1>(hd, a, p, (hipStream_t)stream);
+    return run_paged_attention(cache, paged_spans(cache, n_seqs, n_rows, d_seq_slot, d_span_offset, d_pos0, d_flags), dtype, n_q_heads, d_q, (size_t)q_stride, scale, window,
+                               d_out, (size_t)out_stride, -1, d_lse, (unsigned char *)d_scratch, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -34,6 +34,7 @@ struct PagedAttnArgs {
     size_t q_stride, out_stride;
     int n_q, group, window, rows, runs;        // rows: of a block of columns; runs: workgroups of the call
     float c;                                   // scale log2 e
+    int rsh;                                   // >= 0: fp32 output in operand order with blocks of 1 << rsh rows (frag_index) in the place of rows
     int4 *cuts;                                // per run: the cut item that ends in it {first row, KV head, columns, first run}, first row < 0: none
     int2 *cut_of;                              // ... and its {sequence, block}
     unsigned int *odd;                         // per run: bit k % 32: its item k is whole and its sums hold a NaN
@@ -217,11 +218,12 @@ template <int KIND>
 __device__ __forceinline__ bf16x8_t paged_pick(const uint4 &v) {
     return __builtin_bit_cast(bf16x8_t, make_uint4(paged_pick<KIND>(v.x), paged_pick<KIND>(v.y), paged_pick<KIND>(v.z), paged_pick<KIND>(v.w)));
 }
-// four consecutive channels of a row
-template <int PL>
-__device__ __forceinline__ void paged_store4(void *out, size_t at, float x, float y, float z, float w) {
-    if constexpr (PL == 1) *reinterpret_cast<uint2 *>((uint16_t *)out + at) = make_uint2(pack_bf16x2(x, y), pack_bf16x2(z, w));
-    else *reinterpret_cast<float4 *>((float *)out + at) = make_float4(x, y, z, w);
+// four consecutive channels of a row's head
+template <int HD, int PL>
+__device__ __forceinline__ void paged_store4(const PagedAttnArgs &a, int row, int head, int channel, float x, float y, float z, float w) {
+    const int k = head * HD + channel;
+    if constexpr (PL == 1) *reinterpret_cast<uint2 *>((uint16_t *)a.out + (size_t)row * a.out_stride + k) = make_uint2(pack_bf16x2(x, y), pack_bf16x2(z, w));
+    else *reinterpret_cast<float4 *>((float *)a.out + (a.rsh >= 0 ? frag_index(row, k, a.n_q * HD, a.rsh) : (size_t)row * a.out_stride + k)) = make_float4(x, y, z, w);
 }
 
 // What a lane of 32 columns holds: channels 32 d + 8 (i / 4) + 4 hh + i % 4 of its column; to the row (part < 0) or to a piece.
@@ -233,7 +235,7 @@ __device__ __forceinline__ void paged_store_cols(const PagedAttnArgs &a, int row
         for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                paged_store4<PL>(a.out, (size_t)row * a.out_stride + (size_t)head * HD + 32 * d + 2 * i + 4 * hh, o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv);
+                paged_store4<HD, PL>(a, row, head, 32 * d + 2 * i + 4 * hh, o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv);
         if (hh == 0 && a.lse) a.lse[(size_t)row * a.n_q + head] = (m * a.c + __log2f(l)) * 0.69314718055994531f;
     } else {
 #pragma unroll
@@ -320,7 +322,7 @@ __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const Page
             const float inv = 1.f / l;
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                paged_store4<PL>(a.out, at * a.out_stride + (size_t)head * HD + 32 * d + 2 * i + 4 * hh, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+                paged_store4<HD, PL>(a, (int)at, head, 32 * d + 2 * i + 4 * hh, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
             if (d == 0 && hh == 0 && a.lse) a.lse[at * a.n_q + head] = (m * a.c + __log2f(l)) * 0.69314718055994531f;
         }
     }
@@ -567,7 +569,7 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
                 for (int d = 0; d < ND; ++d) {
                     const f32x4_t x = o[nb][d];
                     poison += (x[0] + x[1]) + (x[2] + x[3]);
-                    if (whole) paged_store4<PL>(a.out, row * a.out_stride + (size_t)h * HD + 16 * d + 4 * hq, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+                    if (whole) paged_store4<HD, PL>(a, (int)row, h, 16 * d + 4 * hq, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
                     else *reinterpret_cast<float4 *>(a.part_o + ((size_t)part * COLS + c) * HD + 16 * d + 4 * hq) = make_float4(x[0], x[1], x[2], x[3]);
                 }
                 if (hq == 0) {
@@ -852,7 +854,7 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
             const size_t row = (size_t)(cut.x + r);
             const float inv = 1.f / L, all = (x[0] + x[1]) + (x[2] + x[3]);
             nan = all != all;
-            paged_store4<PL>(a.out, row * a.out_stride + (size_t)h * HD + d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+            paged_store4<HD, PL>(a, (int)row, h, d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
             if (d == 0 && a.lse) a.lse[row * a.n_q + h] = ((M == -INFINITY ? 0.f : M * a.c) + __log2f(L)) * 0.69314718055994531f;
         }
         if (__syncthreads_or(nan)) {

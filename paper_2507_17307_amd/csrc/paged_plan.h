@@ -10,6 +10,7 @@ constexpr int PAGED_MAX_SEQS = 1024;
 
 struct PagedSpans {
     const int *slot, *off, *pos0, *table;      // off null: one row a sequence
+    const int *info;                           // not null: in the place of those three, per sequence {first row, end row, slot, first row's position}, first row < 0: invalid
     int n_seqs, n_rows, n_slots, n_pages, max_pages, page_shift, n_kv;
     unsigned int *flags;                       // may be null
 };
@@ -19,9 +20,14 @@ struct Span { int first, m, slot, p0; };
 
 // Sequence b of the call; false: something of it is out of range (its rows are skipped).
 RS_HD bool paged_span(const PagedSpans &a, int b, Span &s) {
-    s.first = a.off ? a.off[b] : b;
-    const int end = a.off ? a.off[b + 1] : b + 1;
-    s.slot = a.slot[b]; s.p0 = a.pos0[b]; s.m = 0;
+    int end;
+    s.m = 0;
+    if (a.info) { s.first = a.info[4 * b]; end = a.info[4 * b + 1]; s.slot = a.info[4 * b + 2]; s.p0 = a.info[4 * b + 3]; }
+    else {
+        s.first = a.off ? a.off[b] : b;
+        end = a.off ? a.off[b + 1] : b + 1;
+        s.slot = a.slot[b]; s.p0 = a.pos0[b];
+    }
     if (s.first < 0 || end < s.first || end > a.n_rows) return false;
     s.m = end - s.first;
     if (s.slot < 0 || s.slot >= a.n_slots || s.p0 < 0) return false;

@@ -24,6 +24,8 @@
 #include "mrow_kernels.h"
 #include "gemm_ring.h"
 #include "persistent.h"
+#include "paged_attention.h"
+#include "paged_rope.h"
 
 namespace {
 
@@ -141,6 +143,8 @@ Layout make_layout(const rs_config &c) {
 struct rs_model {
     rs_config cfg;
     Layout lay;
+    rs_paged_kv paged{};                          // rs_create_model_paged: all layers' pages and the table; else page_table null
+    size_t paged_scratch = 0, paged_at = 0;       // of its workspace: what the attention needs, places of the rows
     int n_cu;
     int device = 0;                               // ordinal the model was created on
     const uint16_t *embed, *lm_head, *final_norm;
@@ -173,6 +177,10 @@ struct rs_model {
     unsigned int spin_limit = 1u << 22;
 
     template <typename T> T *at(size_t off) const { return reinterpret_cast<T *>(ws + off); }
+    bool in_pages() const { return paged.page_table != nullptr; }
+    // K/V of a layer lie in kv_units() units of kv_length() positions: slots, or pages
+    int kv_units() const { return in_pages() ? paged.n_pages : cfg.max_seqs; }
+    int kv_length() const { return in_pages() ? paged.page_size : cfg.max_ctx; }
 };
 
 namespace {
@@ -197,6 +205,12 @@ rs_status allow_lds(size_t bytes, const char *name) {
     raised.mark(dev);
     return RS_OK;
 }
+
+}  // namespace
+
+#include "paged_launch.h"
+
+namespace {
 
 // `blocks` workgroups share the phase; every workgroup takes a contiguous range of tiles
 template <int MODE, int RT, int KS, int UNR, int MP, int PRE = 0>
@@ -519,7 +533,7 @@ void fill_persist_args(rs_model *m, PersistArgs &p, const int *d_seq_slot, const
     g.m_rows = 1; g.ld_h = c.d_model; g.gather = nullptr;
     g.eps = c.rms_eps; g.n_q = c.n_q_heads; g.n_kv = c.n_kv_heads; g.head_dim = hd; g.max_ctx = c.max_ctx;
     g.max_seqs = c.max_seqs; g.d_ffn = c.d_ffn;
-    g.row_pos = p.prep.row_pos; g.row_slot = p.prep.row_slot; g.row_bad = p.prep.row_bad;
+    g.row_pos = p.prep.row_pos; g.row_slot = p.prep.row_slot; g.row_bad = p.prep.row_bad; g.row_at = p.prep.row_pos;
     g.rope_cos = m->at<float>(L.rope_cos); g.rope_sin = m->at<float>(L.rope_sin);
     g.qbuf = m->at<float>(L.qbuf); g.kcache = m->kv_k; g.vcache = m->kv_v;
     g.act = m->at<float>(L.act); g.h_out = p.prep.h;
@@ -556,6 +570,19 @@ rs_status forward_persistent(rs_model *m, const int *d_seq_slot, const int *d_to
     return RS_OK;
 }
 
+// Attention of a layer of a model whose cache is in pages: the spans of the row table over the layer's pages.  frag: the output in operand order.
+rs_status launch_attn_paged(const rs_model *m, int layer, int n_seqs, int n_rows, bool frag, int rsh, hipStream_t st) {
+    const rs_config &c = m->cfg;
+    rs_paged_kv kv = m->paged;
+    const size_t bytes = (size_t)kv.n_pages * kv.n_kv_heads * kv.page_size * kv.head_dim * 2;
+    kv.k = (unsigned char *)kv.k + layer * bytes; kv.v = (unsigned char *)kv.v + layer * bytes;
+    PagedSpans s = paged_spans(&kv, n_seqs, n_rows, nullptr, nullptr, nullptr, m->at<uint32_t>(m->lay.seq_bad));
+    s.info = m->at<int>(m->lay.seq_info);
+    const size_t qdim = (size_t)c.n_q_heads * c.head_dim;
+    return run_paged_attention(&kv, s, RS_F32, c.n_q_heads, m->at<float>(m->lay.qbuf), qdim, 1.f / sqrtf((float)c.head_dim), 0, m->at<float>(m->lay.attn_out), qdim, frag ? rsh : -1,
+                               nullptr, m->at<unsigned char>(m->paged_scratch), st);
+}
+
 // One decoder layer on the FMA kernels for a call of MP (1, 2 or 4) token-row slots: QKV, attention, O-proj,
 // gate/up, down.  Every phase reads the weights once and carries the rows side by side.
 template <int MP, typename Tic, typename Toc>
@@ -585,7 +612,8 @@ rs_status fma_layer(rs_model *m, int l, GemvArgs &g, AttnArgs &aa, const WalkPla
     if (rc) return rc;
     // attention
     tic(RS_PHASE_ATTN, l);
-    switch (hd) {
+    if (m->in_pages()) rc = launch_attn_paged(m, l, n_seqs, n_rows, false, 0, st);
+    else switch (hd) {
         case 32: rc = launch_attn<32>(aa, walk, n_splits, c.n_kv_heads, n_rows, n_seqs, m->n_cu, st); break;
         case 64: rc = launch_attn<64>(aa, walk, n_splits, c.n_kv_heads, n_rows, n_seqs, m->n_cu, st); break;
         default: rc = launch_attn<128>(aa, walk, n_splits, c.n_kv_heads, n_rows, n_seqs, m->n_cu, st); break;
@@ -672,10 +700,16 @@ rs_status forward_kernels(rs_model *m, int n_seqs, int n_rows, const int *d_seq_
     pa.out_row = m->at<int>(L.out_row); pa.seq_bad = m->at<int>(L.seq_bad); pa.seq_scale = m->at<float>(L.seq_scale);
     pa.seq_info = m->at<int4>(L.seq_info);
     pa.h = h;
+    int *row_at = row_pos;
+    if (m->in_pages()) {
+        row_at = m->at<int>(m->paged_at);
+        pa.page_table = m->paged.page_table; pa.n_pages = m->paged.n_pages; pa.max_pages = m->paged.max_pages; pa.page_shift = __builtin_ctz((unsigned)m->paged.page_size);
+        pa.row_at = row_at;
+    }
     // attention launch shape; calls in which some sequence brings several rows share K/V tiles between rows
     const int n_splits = attn_splits(c, L, n_rows);
     WalkPlan walk{};
-    if (walk_rows_fit(c.max_ctx, hd)) walk = plan_walk(n_rows, n_seqs, c.n_kv_heads, c.n_q_heads / c.n_kv_heads, c.max_ctx, n_splits, m->n_cu);
+    if (!m->in_pages() && walk_rows_fit(c.max_ctx, hd)) walk = plan_walk(n_rows, n_seqs, c.n_kv_heads, c.n_q_heads / c.n_kv_heads, c.max_ctx, n_splits, m->n_cu);
     if (walk.walk) pa.slice_len = m->at<int>(L.slice_len);
     if (walk.list) {
         pa.pieces = m->at<int4>(L.pieces); pa.n_pieces = walk.pieces; pa.list_slots = walk.slots; pa.list_slices = walk.slices;
@@ -714,9 +748,9 @@ rs_status forward_kernels(rs_model *m, int n_seqs, int n_rows, const int *d_seq_
         if (single) {
             GemvArgs g{};
             g.m_rows = n_rows; g.ld_h = c.d_model;
-            g.eps = c.rms_eps; g.n_q = c.n_q_heads; g.n_kv = c.n_kv_heads; g.head_dim = hd; g.max_ctx = c.max_ctx;
-            g.max_seqs = c.max_seqs; g.layer = l; g.d_ffn = c.d_ffn;
-            g.row_pos = row_pos; g.row_slot = row_slot; g.row_bad = row_bad;
+            g.eps = c.rms_eps; g.n_q = c.n_q_heads; g.n_kv = c.n_kv_heads; g.head_dim = hd; g.max_ctx = m->kv_length();
+            g.max_seqs = m->kv_units(); g.layer = l; g.d_ffn = c.d_ffn;
+            g.row_pos = row_pos; g.row_slot = row_slot; g.row_bad = row_bad; g.row_at = row_at;
             g.rope_cos = m->at<float>(L.rope_cos); g.rope_sin = m->at<float>(L.rope_sin);
             g.qbuf = m->at<float>(L.qbuf); g.kcache = m->kv_k; g.vcache = m->kv_v;
             g.act = m->at<float>(L.act); g.h_out = h;
@@ -747,14 +781,15 @@ rs_status forward_kernels(rs_model *m, int n_seqs, int n_rows, const int *d_seq_
             ra.qkv = g.part ? g.part : m->at<float>(L.qkv_raw); ra.ksplit = g.ksplit; ra.part_stride = g.part_stride;
             ra.qbuf = m->at<float>(L.qbuf); ra.kcache = m->kv_k; ra.vcache = m->kv_v;
             ra.rope_cos = m->at<float>(L.rope_cos); ra.rope_sin = m->at<float>(L.rope_sin);
-            ra.row_pos = row_pos; ra.row_slot = row_slot; ra.row_bad = row_bad;
-            ra.n_q = c.n_q_heads; ra.n_kv = c.n_kv_heads; ra.head_dim = hd; ra.max_ctx = c.max_ctx;
-            ra.max_seqs = c.max_seqs; ra.layer = l;
+            ra.row_pos = row_pos; ra.row_slot = row_slot; ra.row_bad = row_bad; ra.row_at = row_at;
+            ra.n_q = c.n_q_heads; ra.n_kv = c.n_kv_heads; ra.head_dim = hd; ra.max_ctx = m->kv_length();
+            ra.max_seqs = m->kv_units(); ra.layer = l;
             hipLaunchKernelGGL(k_rope_kv_rows, dim3(n_rows, rope_blocks(c.n_q_heads, c.n_kv_heads, hd)), dim3(ROPE_THREADS), 0, st, ra);
             RS_LAUNCHED("rope_kv_rows");
             aa.out_frag = 1; aa.rsh = rsh;
             tic(RS_PHASE_ATTN, l);
-            switch (hd) {
+            if (m->in_pages()) rc = launch_attn_paged(m, l, n_seqs, n_rows, true, rsh, st);
+            else switch (hd) {
                 case 32: rc = launch_attn<32>(aa, walk, n_splits, c.n_kv_heads, n_rows, n_seqs, m->n_cu, st); break;
                 case 64: rc = launch_attn<64>(aa, walk, n_splits, c.n_kv_heads, n_rows, n_seqs, m->n_cu, st); break;
                 default: rc = launch_attn<128>(aa, walk, n_splits, c.n_kv_heads, n_rows, n_seqs, m->n_cu, st); break;
@@ -905,8 +940,9 @@ size_t rs_kv_bytes(const rs_config *cfg) {
     return (size_t)cfg->n_layers * cfg->max_seqs * cfg->n_kv_heads * cfg->max_ctx * cfg->head_dim * 2;
 }
 
-rs_status rs_create_model(const rs_config *cfg, const rs_weights *w, void *kv_k, void *kv_v, void *workspace,
-                          size_t workspace_bytes, rs_model **out) {
+// kv: K and V by slots (paged null), or the pages of all layers
+static rs_status create_model(const rs_config *cfg, const rs_weights *w, void *kv_k, void *kv_v, const rs_paged_kv *paged, void *workspace,
+                              size_t workspace_bytes, rs_model **out) {
     if (!out) return fail(RS_EINVAL, "null output handle");
     *out = nullptr;
     if (const char *why = check_config(cfg)) return fail(RS_EINVAL, "%s", why);
@@ -916,7 +952,8 @@ rs_status rs_create_model(const rs_config *cfg, const rs_weights *w, void *kv_k,
     if (!kv_k || !kv_v || !workspace) return fail(RS_EINVAL, "null KV or workspace pointer");
     if (((uintptr_t)kv_k | (uintptr_t)kv_v | (uintptr_t)workspace) % ALIGN) return fail(RS_EINVAL, "KV/workspace must be 256-byte aligned");
     const Layout L = make_layout(*cfg);
-    if (workspace_bytes < L.total) return fail(RS_EINVAL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, L.total);
+    const size_t need = L.total + (paged ? paged_model_bytes(*cfg, *paged) : 0);
+    if (workspace_bytes < need) return fail(RS_EINVAL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
     for (int l = 0; l < cfg->n_layers; ++l)
         if (!w->attn_norm[l] || !w->w_qkv[l] || !w->w_o[l] || !w->mlp_norm[l] || !w->w_gate_up[l] || !w->w_down[l])
             return fail(RS_EINVAL, "null weight pointer in layer %d", l);
@@ -939,6 +976,7 @@ rs_status rs_create_model(const rs_config *cfg, const rs_weights *w, void *kv_k,
         m->w_gate_up.push_back((const uint16_t *)w->w_gate_up[l]); m->w_down.push_back((const uint16_t *)w->w_down[l]);
     }
     m->kv_k = (uint16_t *)kv_k; m->kv_v = (uint16_t *)kv_v; m->ws = (unsigned char *)workspace;
+    if (paged) { m->paged = *paged; m->paged_at = L.total; m->paged_scratch = L.total + align_up((size_t)cfg->max_rows * 4); }
 
     int dev = 0;
     hipDeviceProp_t prop;
@@ -980,7 +1018,7 @@ rs_status rs_create_model(const rs_config *cfg, const rs_weights *w, void *kv_k,
         const char *genv = getenv("RSTITCH_GRAPHS");
         m->use_graphs = !(genv && strcmp(genv, "0") == 0);
         const char *env = getenv("RSTITCH_DECODE");
-        m->use_persistent = coop != 0 && per_cu > 0 && env && strcmp(env, "persistent") == 0;
+        m->use_persistent = coop != 0 && per_cu > 0 && env && strcmp(env, "persistent") == 0 && !paged;
         if (m->use_persistent && m->persist_lds > 64 * 1024)
             e = hipFuncSetAttribute(persistent_kernel(cfg->head_dim), hipFuncAttributeMaxDynamicSharedMemorySize,
                                     (int)m->persist_lds);
@@ -993,6 +1031,31 @@ rs_status rs_create_model(const rs_config *cfg, const rs_weights *w, void *kv_k,
     if (e != hipSuccess) { delete m; return fail(RS_EHIP, "workspace initialisation: %s", hipGetErrorString(e)); }
     *out = m;
     return RS_OK;
+}
+
+rs_status rs_create_model(const rs_config *cfg, const rs_weights *w, void *kv_k, void *kv_v, void *workspace, size_t workspace_bytes, rs_model **out) {
+    return create_model(cfg, w, kv_k, kv_v, nullptr, workspace, workspace_bytes, out);
+}
+
+static const char *check_paged_model(const rs_config *cfg, const rs_paged_kv *cache) {
+    if (const char *why = check_config(cfg)) return why;
+    if (const char *why = check_paged_attention(cache, cfg->n_q_heads)) return why;
+    if (cache->n_kv_heads != cfg->n_kv_heads || cache->head_dim != cfg->head_dim) return "the cache's n_kv_heads and head_dim must be the model's";
+    if (cache->n_slots < cfg->max_seqs) return "the page table has fewer slots than max_seqs";
+    if ((long long)cache->page_size * cache->max_pages < cfg->max_ctx) return "page_size * max_pages is smaller than max_ctx";
+    return nullptr;
+}
+
+size_t rs_paged_workspace_bytes(const rs_config *cfg, const rs_paged_kv *cache) {
+    if (const char *why = check_paged_model(cfg, cache)) { fail(RS_EINVAL, "%s", why); return 0; }
+    return make_layout(*cfg).total + paged_model_bytes(*cfg, *cache);
+}
+
+rs_status rs_create_model_paged(const rs_config *cfg, const rs_weights *w, const rs_paged_kv *cache, void *workspace, size_t workspace_bytes, rs_model **out) {
+    if (!out) return fail(RS_EINVAL, "null output handle");
+    *out = nullptr;
+    if (const char *why = check_paged_model(cfg, cache)) return fail(RS_EINVAL, "%s", why);
+    return create_model(cfg, w, cache->k, cache->v, cache, workspace, workspace_bytes, out);
 }
 
 rs_status rs_destroy_model(rs_model *model) {
@@ -1064,6 +1127,7 @@ rs_status rs_stitch_generate(rs_model *slm, rs_model *llm, int32_t seq_slot, int
         if ((long long)n_prompt + n_new - 1 > m->cfg.max_ctx)
             return fail(RS_ECAPACITY, "%d + %d tokens do not fit max_ctx %d", n_prompt, n_new, m->cfg.max_ctx);
         if (m->sample_on) return fail(RS_ENOTIMPL, "the device-resident loop decodes greedily: disable sampling");
+        if (m->in_pages()) return fail(RS_ENOTIMPL, "the device-resident loop works on caches by slots");
     }
     if (slm->cfg.head_dim != llm->cfg.head_dim) return fail(RS_EINVAL, "the two models must have the same head_dim");
     if (slm->device != llm->device) return fail(RS_EINVAL, "the two models live on different devices");

@@ -12,7 +12,7 @@ CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
 WRAP = """
 #include "paged_plan.h"
 extern "C" int span(const int *slot, const int *off, const int *pos0, int n_seqs, int n_rows, int n_slots, int max_pages, int shift, int b, rs::Span *s) {
-    rs::PagedSpans a{slot, off, pos0, nullptr, n_seqs, n_rows, n_slots, 1, max_pages, shift, 1, nullptr};
+    rs::PagedSpans a{slot, off, pos0, nullptr, nullptr, n_seqs, n_rows, n_slots, 1, max_pages, shift, 1, nullptr};
     return rs::paged_span(a, b, *s);
 }
 extern "C" int blocks(int m, int p0) { return rs::append_blocks_of(rs::Span{0, m, 0, p0}); }
