@@ -6,8 +6,9 @@
 //   out[d, column]           = sum_j V[j, d] p[column, j]              A = V, which the pages hold by channel, B = p
 // The accumulators of the first product are the B operand of the second as they lie: which position a row of A stands for is free, and
 // is chosen so that the lane that needs k slots 8 h .. 8 h + 7 holds the scores of eight consecutive positions.  With fp32 q both q
-// and p are three bf16 planes (exact: 3 x 8 significant bits), with bf16 q they are one: p is rounded to bf16, an error of 2^-9 of each term at
-// most that is smaller in the sum, as the output's own rounding is 2^-9.
+// and p are three bf16 planes (exact: 3 x 8 significant bits).  With bf16 q, q is one plane and p two (k_paged_narrow) or one (k_paged_wide, where the
+// matrix cores are the bound): p is then rounded to bf16, half a step (2^-8 of a term) at most, as the output is.  Errors from 64 bits, 128 sequences / chunks of
+// 2048 rows: the output's rounding alone 1.7e-3 / 1.5e-3, with p of one plane 2.2e-3 / 2.0e-3.
 //
 // Positions that a row does not see have p = 0, whatever the page holds there.  0 does not take an infinity or a NaN away (and a low plane of p
 // may be negative, which turns a seen infinity into a NaN), but every such product is a NaN in the sum: an item whose sums hold one
@@ -196,9 +197,21 @@ __device__ __forceinline__ void paged_load_q(const void *q, size_t at, bool vali
 }
 template <int PL>
 __device__ __forceinline__ void paged_planes(const float (&p)[8], bf16x8_t (&out)[PL]) {
-    if constexpr (PL == 1)
-        out[0] = __builtin_bit_cast(bf16x8_t, make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
-    else split3(p, out);
+    if constexpr (PL == 3) split3(p, out);
+    else {
+        float rest[8];
+#pragma unroll
+        for (int pl = 0; pl < PL; ++pl) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float x = pl ? rest[2 * k] : p[2 * k], y = pl ? rest[2 * k + 1] : p[2 * k + 1];
+                w[k] = pack_bf16x2(x, y);
+                rest[2 * k] = x - bf16_lo(w[k]); rest[2 * k + 1] = y - bf16_hi(w[k]);
+            }
+            out[pl] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+    }
 }
 
 // ---------------------------------------------------------------- infinities and NaN among eight bf16 values
@@ -409,6 +422,7 @@ __device__ __forceinline__ void paged_fetch_v(const PagedAttnArgs &a, int t, int
 template <int HD, int PL, int NB>
 __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
     constexpr int NS = HD / 32, ND = HD / 16, COLS = 16 * NB, NL = HD / 8;             // NL: loads of a tile of K, and of V
+    constexpr int PP = PL == 1 ? 2 : PL;                              // planes of p: the matrix cores have time, and with one the error of p alone is that of the output's rounding
     __shared__ __align__(16) unsigned char kb[64 * HD * 2], vb[64 * HD * 2];
     const int lane = threadIdx.x, col = lane & 15, hq = lane >> 4, w = blockIdx.x, ps = 1 << a.s.page_shift;
     PagedRun run;
@@ -503,7 +517,7 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
         // ---- softmax
         const int first = 64 * t + 8 * hq;
         const bool all = 64 * t + 64 <= it.s.p0 + it.blk * a.rows + 1 && a.window == 0;             // every column sees the whole tile
-        bf16x8_t pb[NB][2][PL];
+        bf16x8_t pb[NB][2][PP];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             float p[16], mx = -INFINITY;
@@ -529,7 +543,7 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
                 float p8[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) p8[i] = p[8 * s + i];
-                paged_planes<PL>(p8, pb[nb][s]);
+                paged_planes<PP>(p8, pb[nb][s]);
             }
         }
         // ---- P V
@@ -548,7 +562,7 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int pl = PL - 1; pl >= 0; --pl)
+                    for (int pl = PP - 1; pl >= 0; --pl)
                         o[nb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v[s]), pb[nb][s][pl], o[nb][d], 0, 0, 0);
         }
         if (more) { paged_wait_reads(); fetch_v(nt, nit.kvh, page); }

@@ -45,6 +45,16 @@ template <> struct RowVec<uint16_t, 4> {
         *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
     }
 };
+template <> struct RowVec<uint16_t, 8> {
+    static __device__ __forceinline__ void load(const uint16_t *p, float (&x)[8]) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p);
+        x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
+        x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
+    }
+    static __device__ __forceinline__ void store(uint16_t *p, const float (&x)[8]) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+    }
+};
 template <typename T> struct RowVec<T, 8> {
     static __device__ __forceinline__ void load(const T *p, float (&x)[8]) {
         float lo[4], hi[4];
@@ -101,6 +111,25 @@ __device__ __forceinline__ void rope_unit(const TI *x, TO *y, int u, int half, b
     }
 }
 
+// The units of `rows` rows of `heads` heads, by a workgroup of 256: a thread keeps its unit of a head and walks the heads, row after row (no divisions on the way).
+// f(row, head, unit)
+template <typename F>
+__device__ __forceinline__ void rope_walk(int rows, int heads, int units, F f) {
+    const int at_once = 256 / units, slot = threadIdx.x / units, u = threadIdx.x - slot * units;
+    if (at_once > 0) {
+        if (slot >= at_once) return;
+        const int dr = at_once / heads, dh = at_once - dr * heads;
+        int r = slot / heads, h = slot - r * heads;
+        while (r < rows) {
+            f(r, h, u);
+            r += dr; h += dh;
+            if (h >= heads) { h -= heads; ++r; }
+        }
+    } else
+        for (int i = 0; i < rows * heads; ++i)
+            for (int v = threadIdx.x; v < units; v += 256) f(i / heads, i % heads, v);
+}
+
 // ---------------------------------------------------------------- rs_rope_rows
 struct RopeRowsArgs {
     const void *x; void *out; size_t x_stride, out_stride;
@@ -122,13 +151,11 @@ __global__ void __launch_bounds__(256) k_rope_rows(RopeRowsArgs a) {
         turns[i] = t;
     }
     __syncthreads();
-    const int nu = rope_units<VEC>(a.half, a.head_dim);
-    for (int i = tid; i < n * nh * nu; i += 256) {
-        const int rh = i / nu, u = i - rh * nu, r = rh / nh, h = h0 + rh - r * nh;
-        const T *x = (const T *)a.x + (size_t)(r0 + r) * a.x_stride + (size_t)h * a.head_dim;
-        T *y = (T *)a.out + (size_t)(r0 + r) * a.out_stride + (size_t)h * a.head_dim;
+    rope_walk(n, nh, rope_units<VEC>(a.half, a.head_dim), [&](int r, int h, int u) __attribute__((always_inline)) {
+        const T *x = (const T *)a.x + (size_t)(r0 + r) * a.x_stride + (size_t)(h0 + h) * a.head_dim;
+        T *y = (T *)a.out + (size_t)(r0 + r) * a.out_stride + (size_t)(h0 + h) * a.head_dim;
         rope_unit<T, T, VEC>(x, y, u, a.half, a.interleaved, turns + r * a.half);
-    }
+    });
 }
 
 // ---------------------------------------------------------------- rs_paged_append
@@ -201,10 +228,10 @@ __global__ void __launch_bounds__(256) k_paged_append(AppendArgs a) {
             turns[i] = rope_turn(lo + r, a.inv_freq[i - r * a.half], a.amplitude);
         }
         __syncthreads();
-        const int h0 = blockIdx.y * a.heads_wg, nh = min(a.heads_wg, a.n_q + a.s.n_kv - h0), nu = rope_units<VEC>(a.half, a.head_dim);
-        for (int i = tid; i < rows * nh * nu; i += 256) {
-            const int rh = i / nu, u = i - rh * nu, r = rh / nh, h = h0 + rh - r * nh, page = page_of[lo - base + r];
-            if (page < 0) continue;
+        const int h0 = blockIdx.y * a.heads_wg, nh = min(a.heads_wg, a.n_q + a.s.n_kv - h0);
+        rope_walk(rows, nh, rope_units<VEC>(a.half, a.head_dim), [&](int r, int hl, int u) __attribute__((always_inline)) {
+            const int h = h0 + hl, page = page_of[lo - base + r];
+            if (page < 0) return;
             if (h < a.n_q) {
                 const T *x = (const T *)a.q + (size_t)(r0 + r) * a.q_stride + (size_t)h * a.head_dim;
                 rope_unit<T, T, VEC>(x, (T *)a.q_out + (size_t)(r0 + r) * a.q_out_stride + (size_t)h * a.head_dim, u, a.half, a.interleaved, turns + r * a.half);
@@ -213,20 +240,21 @@ __global__ void __launch_bounds__(256) k_paged_append(AppendArgs a) {
                 uint16_t *y = a.kc + ((((size_t)page * a.s.n_kv + h - a.n_q) << a.s.page_shift) + ((lo + r) & (ps - 1))) * a.head_dim;
                 rope_unit<T, uint16_t, VEC>(x, y, u, a.half, a.interleaved, turns + r * a.half);
             }
-        }
+        });
         return;
     }
     // ---- V: a head's rows go to LDS and come back by channel
     uint16_t *tile = reinterpret_cast<uint16_t *>(smem);
-    const int pitch = a.head_dim + APPEND_V_PITCH, h0 = (blockIdx.y - a.rope_wgs) * a.v_heads_wg, h1 = min(h0 + a.v_heads_wg, a.s.n_kv), quads = a.head_dim / 4;
+    const int pitch = a.head_dim + APPEND_V_PITCH, h0 = (blockIdx.y - a.rope_wgs) * a.v_heads_wg, h1 = min(h0 + a.v_heads_wg, a.s.n_kv), pieces = a.head_dim / 8;
     for (int h = h0; h < h1; ++h) {
         __syncthreads();
-        for (int i = tid; i < rows * quads; i += 256) {
-            const int r = i / quads, c = 4 * (i - r * quads);
-            float x[4];
-            RowVec<T, 4>::load((const T *)a.v + (size_t)(r0 + r) * a.v_stride + (size_t)h * a.head_dim + c, x);
+        for (int i = tid; i < rows * pieces; i += 256) {
+            const int r = i / pieces, c = 8 * (i - r * pieces);
+            float x[8];
+            RowVec<T, 8>::load((const T *)a.v + (size_t)(r0 + r) * a.v_stride + (size_t)h * a.head_dim + c, x);
             uint32_t *t = reinterpret_cast<uint32_t *>(tile + (size_t)(lo - base + r) * pitch + c);
-            t[0] = pack_bf16x2(x[0], x[1]); t[1] = pack_bf16x2(x[2], x[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[k] = pack_bf16x2(x[2 * k], x[2 * k + 1]);
         }
         __syncthreads();
         for (int i = tid; i < a.head_dim * (APPEND_BLOCK / 8); i += 256) {
