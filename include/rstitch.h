@@ -419,8 +419,8 @@ rs_status rs_rope_frequencies(int32_t rot_dim, double theta, int32_t kind, doubl
  *              amplitude squared, what takes a rotation off again)
  *   d_out      DEVICE, rows out_stride elements apart; may be d_x itself if the strides are equal, and may not
  *              overlap it otherwise
- * head_dim is a multiple of 8, at most 1024; pointers are 16-byte aligned and strides multiples of 16 bytes.
- * Errors: RS_EINVAL, RS_EHIP. */
+ * head_dim is a multiple of 8, at most 1024; row pointers are 16-byte aligned and strides multiples of 16 bytes.
+ * Errors: RS_EINVAL, RS_ECAPACITY (n_rows > 2^22, n_heads > 65536), RS_EHIP. */
 rs_status rs_rope_rows(const rs_rope *rope, int32_t n_rows, const int32_t *d_pos, int32_t dtype,
                        int32_t n_heads, int32_t head_dim, const void *d_x, int64_t x_stride,
                        int32_t inverse, void *d_out, int64_t out_stride, void *stream);
@@ -431,7 +431,8 @@ rs_status rs_rope_rows(const rs_rope *rope, int32_t n_rows, const int32_t *d_pos
  *                   are neither read nor written
  *   d_seq_slot      DEVICE int32 [n_seqs]; spans of one slot must not share positions
  *   d_span_offset   DEVICE int32 [n_seqs + 1], non-decreasing, 0 <= entries <= n_rows (a span may be empty), or
- *                   NULL: one row for each sequence (n_rows >= n_seqs)
+ *                   NULL: one row for each sequence (n_rows >= n_seqs).  Where a table is not non-decreasing its broken
+ *                   spans are flagged, and it is not said which rows of the others are computed
  *   d_pos0          DEVICE int32 [n_seqs]
  *   rope            NULL: nothing is rotated
  *   dtype           RS_F32 or RS_BF16: type of q, k, v and q_out
@@ -441,8 +442,8 @@ rs_status rs_rope_rows(const rs_rope *rope, int32_t n_rows, const int32_t *d_pos
  *   d_flags         DEVICE uint32 [n_seqs] or NULL: RS_FLAG_BADARG is or-ed into the word of a sequence with a slot, span
  *                   or position out of range, whose rows are all skipped, or with a row whose page is no page of
  *                   the cache, which is skipped; nothing else is written (the caller clears the words)
- * pointers are 16-byte aligned and strides multiples of 16 bytes.
- * Errors: RS_EINVAL, RS_ECAPACITY (n_seqs), RS_EHIP. */
+ * Row pointers are 16-byte aligned and strides multiples of 16 bytes.
+ * Errors: RS_EINVAL, RS_ECAPACITY (n_seqs > 1024, n_rows > 2^22), RS_EHIP. */
 rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows,
                           const int32_t *d_seq_slot, const int32_t *d_span_offset, const int32_t *d_pos0,
                           const rs_rope *rope, int32_t dtype, int32_t n_q_heads,
@@ -459,7 +460,7 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
  *   dtype             type of d_q and d_out.  Sums are fp32.  RS_F32: products of fp32 q and fp32 probabilities with the
  *                     bf16 cache, exact to fp32; RS_BF16: probabilities may be rounded to bf16 for the matrix cores
  *   n_q_heads         a multiple of n_kv_heads, at most 16 times as many
- *   scale             > 0, finite
+ *   scale             > 0, below 2^127
  *   window            >= 0
  *   d_out             DEVICE [n_rows][n_q_heads][head_dim], rows out_stride elements apart; must not overlap d_q
  *   d_lse             DEVICE fp32 [n_rows][n_q_heads] or NULL
@@ -467,8 +468,9 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
  *                     whose page is no page of the cache is computed with some other page in its place
  *   d_scratch         DEVICE, 256-byte aligned, of at least rs_paged_attention_scratch_bytes (0 on a bad argument) for these
  *                     counts; any content.  Calls and graph replays that overlap must not share it
- * What lies in the pages at positions that no row sees may be anything, NaN too.
- * Errors: RS_EINVAL, RS_ECAPACITY (n_seqs), RS_EHIP. */
+ * What lies in the pages at positions that no row sees may be anything, NaN too, and what one row sees does not reach another: an infinity or
+ * a NaN in V at a position that only some rows of a span see is theirs alone (spans with such values take several times as long).
+ * Errors: RS_EINVAL, RS_ECAPACITY (n_seqs > 1024, n_rows > 2^22), RS_EHIP. */
 size_t    rs_paged_attention_scratch_bytes(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, int32_t n_q_heads);
 rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows,
                              const int32_t *d_seq_slot, const int32_t *d_span_offset, const int32_t *d_pos0,

@@ -346,9 +346,15 @@ def rs_rope_rows(rope: Rope, d_pos: torch.Tensor, x: torch.Tensor, out: torch.Te
 
 
 def _paged_rows(name: str, t: torch.Tensor, cache: PagedCache, n_rows: int, heads: int, dtype: torch.dtype):
-    shape = t.shape
-    if len(shape) != 3 or shape[0] < n_rows or shape[1] != heads or shape[2] != cache.head_dim or t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype} and at least [{n_rows}, {heads}, {cache.head_dim}], not {t.dtype} {tuple(shape)}")
+    """_rows of a tensor that a call on `cache` takes."""
+    if t.dtype is dtype and t.dim() == 3 and t.get_device() == cache.device:
+        rows, h, hd = t.shape
+        if rows >= n_rows and h == heads and hd == cache.head_dim:
+            stride = t.stride()
+            if stride[2] == 1 and stride[1] == hd:
+                return t.data_ptr(), stride[0]
+    if t.dtype != dtype or t.dim() != 3 or t.shape[0] < n_rows or t.shape[1] != heads or t.shape[2] != cache.head_dim:
+        raise ValueError(f"{name} must be {dtype} and at least [{n_rows}, {heads}, {cache.head_dim}], not {t.dtype} {tuple(t.shape)}")
     return _rows(name, t, cache.device)
 
 
@@ -556,6 +562,8 @@ class PagedModel(Model):
         self.handle = rs_create_model_paged(self.cfg, weights, self.cache_struct, self.workspace)
 
     def reserve(self, slot: int, positions: int) -> None:
+        if not 0 <= slot < len(self._held):
+            raise RsError(-1, f"slot {slot} out of range")
         held, more = self._held[slot], (positions + self.page_size - 1) // self.page_size - len(self._held[slot])
         if positions > self.cfg.max_ctx:
             raise RsError(-2, f"{positions} positions do not fit max_ctx {self.cfg.max_ctx}")
@@ -568,6 +576,8 @@ class PagedModel(Model):
         self.page_table[slot, at:len(held)] = self._i32(held[at:])
 
     def release(self, slot: int) -> None:
+        if not 0 <= slot < len(self._held):
+            raise RsError(-1, f"slot {slot} out of range")
         held = self._held[slot]
         self.page_table[slot].fill_(-1)
         self._free.extend(reversed(held))

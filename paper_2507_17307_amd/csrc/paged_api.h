@@ -31,6 +31,7 @@ rs_status rs_rope_frequencies(int32_t rot_dim, double theta, int32_t kind, doubl
 rs_status rs_rope_rows(const rs_rope *rope, int32_t n_rows, const int32_t *d_pos, int32_t dtype, int32_t n_heads, int32_t head_dim, const void *d_x,
                        int64_t x_stride, int32_t inverse, void *d_out, int64_t out_stride, void *stream) {
     if (!rope || !d_pos) return fail(RS_EINVAL, "null argument");
+    if ((uintptr_t)d_pos % 4) return fail(RS_EINVAL, "positions must be 4-byte aligned");
     if (n_rows < 1 || n_heads < 1) return fail(RS_EINVAL, "n_rows and n_heads must be at least 1");
     if (n_rows > (1 << 22) || n_heads > 65536) return fail(RS_ECAPACITY, "more than 2^22 rows or 65536 heads");
     if (head_dim < 8 || head_dim % 8 || head_dim > 1024) return fail(RS_EINVAL, "head_dim must be a multiple of 8 in 8..1024");
@@ -59,7 +60,7 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
                           const void *d_k, int64_t k_stride, const void *d_v, int64_t v_stride, void *d_q_out, int64_t q_out_stride, uint32_t *d_flags,
                           void *stream) {
     if (const char *why = check_paged(cache)) return fail(RS_EINVAL, "%s", why);
-    if (rs_status rc = check_spans(n_seqs, n_rows, d_seq_slot, d_span_offset, d_pos0, dtype)) return rc;
+    if (rs_status rc = check_spans(n_seqs, n_rows, d_seq_slot, d_span_offset, d_pos0, d_flags, dtype)) return rc;
     if (n_q_heads < 1 || n_q_heads > 16384) return fail(RS_EINVAL, "n_q_heads must be in 1..16384");
     const int hd = cache->head_dim;
     if (rope) if (const char *why = check_rope(rope, hd)) return fail(RS_EINVAL, "%s", why);
@@ -101,12 +102,13 @@ rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n
                              const int32_t *d_pos0, int32_t dtype, int32_t n_q_heads, const void *d_q, int64_t q_stride, float scale, int32_t window,
                              void *d_out, int64_t out_stride, float *d_lse, uint32_t *d_flags, void *d_scratch, size_t scratch_bytes, void *stream) {
     if (const char *why = check_paged_attention(cache, n_q_heads)) return fail(RS_EINVAL, "%s", why);
-    if (rs_status rc = check_spans(n_seqs, n_rows, d_seq_slot, d_span_offset, d_pos0, dtype)) return rc;
+    if (rs_status rc = check_spans(n_seqs, n_rows, d_seq_slot, d_span_offset, d_pos0, d_flags, dtype)) return rc;
     const int hd = cache->head_dim;
     if (const char *why = check_rows(d_q, q_stride, dtype, n_q_heads, hd)) return fail(RS_EINVAL, "q: %s", why);
     if (const char *why = check_rows(d_out, out_stride, dtype, n_q_heads, hd)) return fail(RS_EINVAL, "out: %s", why);
     if (d_q == d_out) return fail(RS_EINVAL, "out must not be q");
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(RS_EINVAL, "scale must be positive and finite");
+    if (!(scale > 0.f) || !std::isfinite(scale * 1.44269504088896341f)) return fail(RS_EINVAL, "scale must be positive and below 2^127");
+    if ((uintptr_t)d_lse % 4) return fail(RS_EINVAL, "lse must be 4-byte aligned");
     if (window < 0) return fail(RS_EINVAL, "window must be at least 0");
     if (!d_scratch || (uintptr_t)d_scratch % ALIGN) return fail(RS_EINVAL, "scratch must be 256-byte aligned");
     const size_t need = rs_paged_attention_scratch_bytes(cache, n_seqs, n_rows, n_q_heads);

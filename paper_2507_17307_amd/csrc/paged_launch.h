@@ -10,6 +10,7 @@ const char *check_paged(const rs_paged_kv *c) {
     if (!c) return "null cache";
     if (!c->k || !c->v || !c->page_table) return "null cache pointer";
     if (((uintptr_t)c->k | (uintptr_t)c->v) % 16) return "K and V pages must be 16-byte aligned";
+    if ((uintptr_t)c->page_table % 4) return "page_table must be 4-byte aligned";
     if (c->n_pages < 1 || c->n_slots < 1 || c->max_pages < 1 || c->n_kv_heads < 1) return "cache with a count below 1";
     if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return "page_size must be a power of two in 16..1024";
     if ((long long)c->page_size * c->max_pages > (1LL << 30)) return "page_size * max_pages must not exceed 2^30";
@@ -36,11 +37,12 @@ const char *check_rows(const void *p, int64_t stride, int dtype, long long heads
     return nullptr;
 }
 
-rs_status check_spans(int32_t n_seqs, int32_t n_rows, const int32_t *slot, const int32_t *off, const int32_t *pos0, int dtype) {
+rs_status check_spans(int32_t n_seqs, int32_t n_rows, const int32_t *slot, const int32_t *off, const int32_t *pos0, const uint32_t *flags, int dtype) {
     if (n_seqs < 1 || n_rows < 1) return fail(RS_EINVAL, "n_seqs and n_rows must be at least 1");
     if (n_seqs > PAGED_MAX_SEQS) return fail(RS_ECAPACITY, "n_seqs %d exceeds %d", n_seqs, PAGED_MAX_SEQS);
     if (n_rows > (1 << 22)) return fail(RS_ECAPACITY, "n_rows %d exceeds 2^22", n_rows);
     if (!slot || !pos0) return fail(RS_EINVAL, "null argument");
+    if (((uintptr_t)slot | (uintptr_t)off | (uintptr_t)pos0 | (uintptr_t)flags) % 4) return fail(RS_EINVAL, "slots, offsets, positions and flags must be 4-byte aligned");
     if (!off && n_rows < n_seqs) return fail(RS_EINVAL, "%d sequences of one row do not fit %d rows", n_seqs, n_rows);
     if (dtype != RS_F32 && dtype != RS_BF16) return fail(RS_EINVAL, "dtype must be RS_F32 or RS_BF16");
     return RS_OK;

@@ -115,19 +115,14 @@ __device__ __forceinline__ void rope_unit(const TI *x, TO *y, int u, int half, b
 // f(row, head, unit)
 template <typename F>
 __device__ __forceinline__ void rope_walk(int rows, int heads, int units, F f) {
-    const int at_once = 256 / units, slot = threadIdx.x / units, u = threadIdx.x - slot * units;
-    if (at_once > 0) {
-        if (slot >= at_once) return;
-        const int dr = at_once / heads, dh = at_once - dr * heads;
-        int r = slot / heads, h = slot - r * heads;
-        while (r < rows) {
-            f(r, h, u);
-            r += dr; h += dh;
-            if (h >= heads) { h -= heads; ++r; }
-        }
-    } else
-        for (int i = 0; i < rows * heads; ++i)
-            for (int v = threadIdx.x; v < units; v += 256) f(i / heads, i % heads, v);
+    const int at_once = 256 / units, slot = threadIdx.x / units, u = threadIdx.x - slot * units;         // (a head of 1024 channels has 128 units)
+    if (slot >= at_once) return;
+    const int dr = at_once / heads, dh = at_once - dr * heads;
+    for (int r = slot / heads, h = slot - r * heads; r < rows;) {
+        f(r, h, u);
+        r += dr; h += dh;
+        if (h >= heads) { h -= heads; ++r; }
+    }
 }
 
 // ---------------------------------------------------------------- rs_rope_rows

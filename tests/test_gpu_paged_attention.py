@@ -222,3 +222,65 @@ def test_a_run_of_chunks_and_single_tokens(dtype):
     # q itself may be off by the rotation's error, and in bf16 by a step where that crosses a rounding: one more rounding of every score
     eo = eo + (2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -20) * want.abs().amax() * 4
     paged.close(torch.cat([torch.cat(g) for g in got]), want, eo)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("spans,pos0,nq,nkv,hd", [([1] * 700, [(37 * i) % 190 for i in range(700)], 6, 2, 64), ([40] * 100, [(91 * i) % 230 for i in range(100)], 8, 2, 32),
+                                                  ([1] * 1024, [i % 3 for i in range(1024)], 2, 1, 32)])
+def test_many_sequences_some_with_infinities(spans, pos0, nq, nkv, hd, dtype):
+    """Workgroups that take several whole items, and some of an item's tiles: infinities and NaN in V of every ninth sequence."""
+    pg = paged.Pages(spans, pos0, nkv, hd, 16, seed=38, fill=float("inf"))
+    for b in range(0, len(spans), 9):
+        p = pos0[b] // 2
+        pg.v[pg.table[pg.slot[b], p // 16], 0, b % hd, p % 16] = (float("inf"), float("nan"), -float("inf"))[b % 3]
+    pg.gpu()
+    q = torch.randn(pg.rows, nq, hd, generator=pg.gen).to(dtype)
+    out, lse = call(pg, q, 0.2)
+    check(pg, q, 0.2, 0, out, lse)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_long_span_whose_first_pages_are_gone(dtype):
+    pg = paged.Pages([150, 33], [300, 70], 2, 128, 32, seed=39).gpu()
+    q = torch.randn(pg.rows, 6, 128, generator=pg.gen).to(dtype)
+    pg.dtable[pg.slot[0].item(), :7] = -1                                     # positions 0 .. 223; the first row sees 241 .. 300
+    flags = torch.zeros(2, dtype=torch.int32, device="cuda")
+    out, lse = call(pg, q, 0.1, window=60, flags=flags)
+    assert flags.tolist() == [0, 0]
+    check(pg, q, 0.1, 60, out, lse)
+    pg.dtable[pg.slot[0].item(), 8] = 10 ** 9                                 # 256 .. 287: seen
+    call(pg, q, 0.1, window=60, flags=flags)
+    assert flags.tolist() == [16, 0]
+
+
+def test_results_repeat_and_do_not_depend_on_the_scratch():
+    """Twice the same bits, with different scratch contents, whatever ran before in it."""
+    for spans, pos0 in (([1] * 20, [100 * i for i in range(20)]), ([90, 400, 1], [700, 30, 2000])):
+        pg = paged.Pages(spans, pos0, 2, 128, 64, seed=40).gpu()
+        q = torch.randn(pg.rows, 14, 128, generator=pg.gen).to(torch.bfloat16)
+        import paper_2507_17307_amd as P
+        n = P.rs_paged_attention_scratch_bytes(pg.cache, pg.n, pg.rows, 14)
+        dq, got = q.cuda(), []
+        for fill in (0, 255, 127):
+            out, lse = torch.empty_like(dq), torch.empty(pg.rows, 14, device="cuda")
+            s = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+            P.rs_paged_attention(pg.cache, pg.n, pg.rows, pg.dslot, pg.doff, pg.dpos, dq, 0.09, 0, out, lse, s)
+            P.rs_paged_attention(pg.cache, pg.n, pg.rows, pg.dslot, pg.doff, pg.dpos, dq, 0.09, 0, out, lse, s)
+            got.append((out.cpu(), lse.cpu()))
+        assert all(torch.equal(a, b) for g in got[1:] for a, b in zip(g, got[0]))
+
+
+def test_two_calls_at_once_with_scratch_of_their_own():
+    import paper_2507_17307_amd as P
+    pg = paged.Pages([60, 61], [900, 1000], 2, 128, 64, seed=41).gpu()
+    q = torch.randn(pg.rows, 8, 128, generator=pg.gen).to(torch.bfloat16).cuda()
+    n = P.rs_paged_attention_scratch_bytes(pg.cache, pg.n, pg.rows, 8)
+    want, _ = call(pg, q.cpu(), 0.09)
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(q) for _ in range(2)]
+    scr = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, o, c in zip(streams, outs, scr):
+            P.rs_paged_attention(pg.cache, pg.n, pg.rows, pg.dslot, pg.doff, pg.dpos, q, 0.09, 0, o, None, c, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o.cpu(), want) for o in outs)

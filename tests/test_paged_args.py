@@ -15,6 +15,14 @@ extern "C" int span(const int *slot, const int *off, const int *pos0, int n_seqs
     rs::PagedSpans a{slot, off, pos0, nullptr, nullptr, n_seqs, n_rows, n_slots, 1, max_pages, shift, 1, nullptr};
     return rs::paged_span(a, b, *s);
 }
+extern "C" int info_span(const int *info, int n_rows, int n_slots, int max_pages, int shift, int b, rs::Span *s) {
+    rs::PagedSpans a{nullptr, nullptr, nullptr, nullptr, info, 1, n_rows, n_slots, 1, max_pages, shift, 1, nullptr};
+    return rs::paged_span(a, b, *s);
+}
+extern "C" int n_blocks(int m, int rows) { return rs::paged_blocks(rs::Span{0, m, 0, 0}, rows); }
+extern "C" void tiles(int m, int p0, int rows, int window, int j, int *t) { rs::paged_tiles(rs::Span{0, m, 0, p0}, rows, window, 6, j, t[0], t[1]); }
+extern "C" long long run(long long T, int W, int w) { return rs::paged_run(T, W, w); }
+extern "C" int run_of(long long T, int W, long long t) { return rs::paged_run_of(T, W, t); }
 extern "C" int blocks(int m, int p0) { return rs::append_blocks_of(rs::Span{0, m, 0, p0}); }
 extern "C" int blocks_most(int n_seqs, int n_rows) { return rs::append_blocks_most(n_seqs, n_rows); }
 """
@@ -26,7 +34,9 @@ def plan(tmp_path_factory):
     src, so = d / "wrap.cpp", d / "libpaged_plan.so"
     src.write_text(WRAP)
     subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, str(src), "-o", str(so)], check=True)
-    return C.CDLL(str(so))
+    lib = C.CDLL(str(so))
+    lib.run.restype, lib.run.argtypes, lib.run_of.argtypes = C.c_longlong, [C.c_longlong, C.c_int, C.c_int], [C.c_longlong, C.c_int, C.c_longlong]
+    return lib
 
 
 def ints(*v):
@@ -48,6 +58,37 @@ def test_spans_out_of_range_are_told(plan):
     assert not span([0], [-2**31, 2**31 - 1], [0])
     assert span([0, 1], None, [0, 7], b=1) and list(s) == [1, 1, 1, 7]
     assert span([0], [0, 5], [2**30 - 5], max_pages=2**26) and not span([0], [0, 5], [2**30 - 4], max_pages=2**26)
+
+
+def test_spans_of_a_prepared_row_table(plan):
+    s = (C.c_int * 4)()
+    table = ints(3, 8, 2, 10, -1, 0, 0, 0, 0, 4, 9, 0)
+    assert plan.info_span(table, 10, 4, 3, 4, 0, s) and list(s) == [3, 5, 2, 10]
+    assert not plan.info_span(table, 10, 4, 3, 4, 1, s) and not plan.info_span(table, 10, 4, 3, 4, 2, s)
+
+
+def test_tiles_of_a_block_are_those_that_its_rows_see(plan):
+    rng, t = random.Random(2), (C.c_int * 2)()
+    for _ in range(3000):
+        m, p0, rows, window = rng.randint(1, 300), rng.choice([0, 1, 63, 64, rng.randint(0, 5000)]), rng.choice([1, 2, 5, 18, 25, 128]), rng.choice([0, 0, 1, 63, 64, 65, 1000, 2**31 - 1])
+        j = rng.randrange(plan.n_blocks(m, rows))
+        seen = [x for r in range(j * rows, min(m, (j + 1) * rows)) for x in (max(0, p0 + r - window + 1) if window else 0, p0 + r)]
+        plan.tiles(m, p0, rows, window, j, t)
+        assert (t[0], t[1]) == (min(seen) // 64, max(seen) // 64 + 1)
+    assert plan.n_blocks(0, 5) == 0 and plan.n_blocks(11, 5) == 3
+
+
+@pytest.mark.parametrize("T", [1, 7, 511, 512, 513, 100003, 2**31 - 1, 2**31, 2**40 + 12345])
+@pytest.mark.parametrize("W", [1, 8, 256, 512, 1024])
+def test_runs_share_the_tiles_evenly(plan, T, W):
+    W = min(W, T)
+    starts = [plan.run(T, W, w) for w in range(W + 1)]
+    assert starts[0] == 0 and starts[-1] == T
+    sizes = {b - a for a, b in zip(starts, starts[1:])}
+    assert max(sizes) - min(sizes) <= 1 and min(sizes) >= 1
+    for t in {0, T - 1, T // 2, T // 3} | {s for s in starts[1:-1][::37]} | {s - 1 for s in starts[1:][::41]}:
+        w = plan.run_of(T, W, t)
+        assert starts[w] <= t < starts[w + 1]
 
 
 def test_append_launches_a_workgroup_for_every_block_of_positions(plan):
@@ -92,7 +133,7 @@ def cache(P, **kw):
     return P.binding._RsPagedKv(*v.values())
 
 
-BAD_CACHES = [dict(k=None), dict(v=None), dict(page_table=None), dict(k=8), dict(v=264), dict(n_pages=0), dict(page_size=8), dict(page_size=48), dict(page_size=2048),
+BAD_CACHES = [dict(page_table=6), dict(k=None), dict(v=None), dict(page_table=None), dict(k=8), dict(v=264), dict(n_pages=0), dict(page_size=8), dict(page_size=48), dict(page_size=2048),
               dict(n_slots=0), dict(max_pages=0), dict(page_size=16, max_pages=2**26 + 1), dict(n_kv_heads=0), dict(n_kv_heads=3), dict(head_dim=96), dict(head_dim=0)]
 
 
@@ -117,13 +158,13 @@ def test_malformed_caches_are_refused_before_any_launch(bad):
 @pytest.mark.parametrize("bad,status", [
     (dict(n_seqs=0), -1), (dict(n_rows=0), -1), (dict(n_seqs=1025), -2), (dict(n_rows=2**22 + 1), -2), (dict(slot=None), -1), (dict(pos0=None), -1),
     (dict(n_seqs=5, off=None), -1), (dict(dtype=2), -1), (dict(n_q=0), -1), (dict(q=None), -1), (dict(q=8), -1), (dict(qs=252, dtype=1), -1), (dict(qs=192), -1),
-    (dict(out=None), -1), (dict(out=520), -1), (dict(outs=255), -1), (dict(outs=128), -1)])
+    (dict(slot=6), -1), (dict(off=5), -1), (dict(pos0=7), -1), (dict(out=None), -1), (dict(out=520), -1), (dict(outs=255), -1), (dict(outs=128), -1)])
 def test_malformed_rows_are_refused_before_any_launch(bad, status):
     import paper_2507_17307_amd as P
     assert attention(P, cache(P), **bad) == status and append(P, cache(P), **bad) == status
 
 
-@pytest.mark.parametrize("bad", [dict(n_q=5), dict(n_q=34, qs=4096, outs=4096), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(window=-1),
+@pytest.mark.parametrize("bad", [dict(n_q=5), dict(n_q=34, qs=4096, outs=4096), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38), dict(window=-1),
                                  dict(out=16), dict(scratch=None), dict(scratch=128), dict(size=0)])
 def test_malformed_attention_arguments_are_refused(bad):
     import paper_2507_17307_amd as P
