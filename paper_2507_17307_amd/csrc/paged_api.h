@@ -95,7 +95,8 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
 size_t rs_paged_attention_scratch_bytes(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, int32_t n_q_heads) {
     if (const char *why = check_paged_attention(cache, n_q_heads)) { fail(RS_EINVAL, "%s", why); return 0; }
     if (n_seqs < 1 || n_rows < 1 || n_seqs > PAGED_MAX_SEQS || n_rows > (1 << 22)) { fail(RS_EINVAL, "n_seqs must be in 1..%d and n_rows in 1..2^22", PAGED_MAX_SEQS); return 0; }
-    return paged_shape(cache, n_seqs, n_rows, n_q_heads).total;
+    const size_t f = paged_shape(cache, n_seqs, n_rows, n_q_heads, RS_F32).total, b = paged_shape(cache, n_seqs, n_rows, n_q_heads, RS_BF16).total;
+    return f > b ? f : b;
 }
 
 rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_rows, const int32_t *d_seq_slot, const int32_t *d_span_offset,

@@ -57,15 +57,30 @@ PagedSpans paged_spans(const rs_paged_kv *c, int32_t n_seqs, int32_t n_rows, con
     return s;
 }
 
-// Which kernel takes a call: blocks of 16 or 32 columns where the spans have no more than that on average, else of 128.
+// Which kernel takes a call, by the columns that a span brings on average (rows times query heads of a KV head) and by how many pairs of a sequence and a
+// KV head there are to share the CUs.  us a call in a graph, contexts of 4000 positions, blocks of 16 / 32 / 128 columns:
+//   fp32  28 query heads on 4, rows of each sequence 1 / 3 / 6 / 12:   1 sequence    15 18 21 30 / 18 19 23 28 / 22 25 26 31
+//                                                                   16 sequences   45 66 88 130 / 52 70 92 113 / 57 59 63 69
+//                                                                   64 sequences   117 181 313 477 / 122 138 220 335 / 174 179 184 200
+//   bf16  the same                                                   1 sequence    14 17 19 26 / 15 17 20 25 / 19 20 22 27
+//                                                                    8 sequences (8 rows at last)   31 43 - 56 / 35 52 - 64 / 27 32 - 42
+//                                                                   64 sequences   113 174 301 484 / 114 128 190 320 / 106 109 117 126
+// so that blocks grow with the columns, few pairs stay with narrow blocks longer, and with one plane of q and many pairs the wide kernel, in which
+// four waves fetch, is the fastest for single rows too.
+int paged_cols(int n_seqs, int n_rows, int group, int n_kv, int dtype) {
+    const long long cols = ((long long)n_rows * group + n_seqs - 1) / n_seqs;
+    const bool few = (long long)n_seqs * n_kv < 32;
+    if (dtype == RS_BF16 && !few) return PAGED_COLS;
+    return cols <= 16 ? 16 : cols <= (few ? 64 : 32) ? 32 : PAGED_COLS;
+}
+
 struct PagedShape { int cols, rows, runs; long long items; size_t of, odd, ml, o, total; };
-PagedShape paged_shape(const rs_paged_kv *cache, int n_seqs, int n_rows, int n_q_heads) {
+PagedShape paged_shape(const rs_paged_kv *cache, int n_seqs, int n_rows, int n_q_heads, int dtype) {
     const int n_kv = cache->n_kv_heads, head_dim = cache->head_dim, group = n_q_heads / n_kv;
     PagedShape p{};
-    const long long slots = ((long long)n_rows * group + n_seqs - 1) / n_seqs;
-    p.cols = slots <= 16 ? 16 : slots <= 32 ? 32 : PAGED_COLS;
+    p.cols = paged_cols(n_seqs, n_rows, group, n_kv, dtype);
     p.rows = p.cols / group;
-    p.runs = p.cols == PAGED_COLS ? PAGED_WIDE_RUNS : PAGED_NARROW_RUNS;
+    p.runs = p.cols != PAGED_COLS ? PAGED_NARROW_RUNS : dtype == RS_F32 ? PAGED_WIDE_RUNS3 : PAGED_WIDE_RUNS;
     // at most so many items, and so many tiles in all: short page tables need fewer workgroups
     p.items = ((long long)n_rows / p.rows + n_seqs) * n_kv;
     const double tiles = (double)p.items * (((long long)cache->page_size * cache->max_pages >> PAGED_TILE) + 1);
@@ -121,7 +136,7 @@ size_t paged_model_bytes(const rs_config &c, const rs_paged_kv &cache) {
     for (int slots : {16, 32, PAGED_COLS}) {                     // a row of each kernel's calls; every one of its runs
         rs_paged_kv kv = cache;
         kv.max_pages = (1 << 30) / kv.page_size;
-        const size_t n = paged_shape(&kv, 1, slots / group, c.n_q_heads).total;
+        const size_t n = paged_shape(&kv, 1, slots / group, c.n_q_heads, RS_F32).total;
         if (n > most) most = n;
     }
     return align_up((size_t)c.max_rows * 4) + most;
@@ -131,12 +146,12 @@ size_t paged_model_bytes(const rs_config &c, const rs_paged_kv &cache) {
 rs_status run_paged_attention(const rs_paged_kv *cache, const PagedSpans &spans, int dtype, int n_q_heads, const void *q, size_t q_stride, float scale, int window, void *out,
                               size_t out_stride, int out_rsh, float *lse, unsigned char *scratch, hipStream_t st) {
     PagedAttnArgs a{};
-    const PagedShape p = paged_shape(cache, spans.n_seqs, spans.n_rows, n_q_heads);
+    const PagedShape p = paged_shape(cache, spans.n_seqs, spans.n_rows, n_q_heads, dtype);
     a.s = spans;
     a.kc = (const uint16_t *)cache->k; a.vc = (const uint16_t *)cache->v;
     a.q = q; a.out = out; a.lse = lse; a.q_stride = q_stride; a.out_stride = out_stride; a.rsh = out_rsh;
     a.n_q = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.window = window; a.rows = p.rows;
-    a.runs = p.cols == PAGED_COLS && dtype == RS_F32 && p.runs > PAGED_WIDE_RUNS3 ? PAGED_WIDE_RUNS3 : p.runs;
+    a.runs = p.runs;
     a.c = scale * 1.44269504088896341f;
     a.cuts = (int4 *)scratch; a.cut_of = (int2 *)(scratch + p.of); a.odd = (unsigned int *)(scratch + p.odd);
     a.part_ml = (float *)(scratch + p.ml); a.part_o = (float *)(scratch + p.o);
