@@ -278,7 +278,7 @@ def _ints(name: str, t: Optional[torch.Tensor], n: int, device: int) -> Optional
     """Address of n 32-bit integers."""
     if t is None:
         return None
-    if t.dtype not in _INT_TYPES or not t.is_contiguous() or t.numel() < n or t.get_device() != device:
+    if t.dtype is not torch.int32 and t.dtype not in _INT_TYPES or not t.is_contiguous() or t.numel() < n or t.get_device() != device:
         raise ValueError(f"{name} must hold {n} contiguous 32-bit integers on {_device_name(device)}")
     return t.data_ptr()
 
@@ -289,6 +289,8 @@ def _device_name(device: int) -> str:
 
 def _device_stream(device: int, stream) -> Optional[int]:
     """The launch goes to the current device, which has to be the tensors' own."""
+    if stream is None and _raw_stream is not None and _raw_device is not None and 0 <= device == _raw_device():
+        return _raw_stream(device)
     if device < 0:
         raise ValueError("tensors must be on a GPU")
     if device != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):

@@ -451,58 +451,64 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
         --left; ++ft;
         if (left > 0 && ft == f_t1) { paged_next(a, fit); look(); ft = f_t0; }
     };
-    look();
-    int page = paged_page(a, fit.b, ask());
-    fetch_k(ft, fit.kvh, page);
-    fetch_v(ft, fit.kvh, page);
-    // ---- the tile that is multiplied
-    PagedItem it = fit;
-    int t = ft, t0 = f_t0, t1 = f_t1, hi = f_hi, ta = ft;
-    step();
-    int entry = left > 0 ? ask() : 0, n_items = 0;
-    unsigned int odd = 0;
     int see_lo[NB], see_hi[NB], n_col = 0;                                // positions that the lane's columns see
     bf16x8_t q[NB][NS][PL];
     float m[NB], l[NB];
     f32x4_t o[NB][ND];
-    bool begin = true;
-    while (true) {
-        if (begin) {
-            const int r0 = it.blk * a.rows;
-            n_col = min(a.rows, it.s.m - r0) * a.group;
+    auto begin = [&](const PagedItem &it) __attribute__((always_inline)) {
+        const int r0 = it.blk * a.rows;
+        n_col = min(a.rows, it.s.m - r0) * a.group;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const int c = 16 * nb + col, r = c / a.group, h = it.kvh * a.group + c - r * a.group;
-                const bool valid = c < n_col;
-                paged_seen(it.s, r0 + r, r0 + r + 1, a.window, see_lo[nb], see_hi[nb]);
-                if (!valid) see_hi[nb] = 0;
-                const size_t at = (size_t)(it.s.first + r0 + r) * a.q_stride + (size_t)h * HD + 8 * hq;
+        for (int nb = 0; nb < NB; ++nb) {
+            const int c = 16 * nb + col, r = c / a.group, h = it.kvh * a.group + c - r * a.group;
+            const bool valid = c < n_col;
+            paged_seen(it.s, r0 + r, r0 + r + 1, a.window, see_lo[nb], see_hi[nb]);
+            if (!valid) see_hi[nb] = 0;
+            const size_t at = (size_t)(it.s.first + r0 + r) * a.q_stride + (size_t)h * HD + 8 * hq;
 #pragma unroll
-                for (int s = 0; s < NS; ++s) paged_load_q<PL>(a.q, at + 32 * s, valid, q[nb][s]);
-                m[nb] = -INFINITY; l[nb] = 0.f;
+            for (int s = 0; s < NS; ++s) paged_load_q<PL>(a.q, at + 32 * s, valid, q[nb][s]);
+            m[nb] = -INFINITY; l[nb] = 0.f;
 #pragma unroll
-                for (int d = 0; d < ND; ++d) o[nb][d] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-            }
-            begin = false;
+            for (int d = 0; d < ND; ++d) o[nb][d] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
         }
+    };
+    look();
+    int entry = ask();
+    begin(fit);                                                           // (q on its way with the page, ahead of the tiles)
+    int page = paged_page(a, fit.b, entry);
+    fetch_k(ft, fit.kvh, page);
+    fetch_v(ft, fit.kvh, page);
+    // ---- the tile that is multiplied
+    PagedItem it = fit;
+    int t = ft, t0 = f_t0, t1 = f_t1, hi = f_hi, ta = ft, n_items = 0;
+    step();
+    if (left > 0) entry = ask();
+    unsigned int odd = 0;
+    while (true) {
         // ---- scores: register i of block 2 s32 + blk is position 64 t + 32 s32 + 8 hq + 4 blk + i of column col
         paged_wait_loads<NL>();                                           // all but V of this tile
+        // (operands first, then products that do not wait for each other)
         f32x4_t sc[NB][4];
+        bf16x8_t kf[4][NS];
 #pragma unroll
-        for (int kbk = 0; kbk < 4; ++kbk) {
-            const int r = 32 * (kbk >> 1) + 8 * (col >> 2) + 4 * (kbk & 1) + (col & 3);
-            bf16x8_t A[NS];
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int s = 0; s < NS; ++s) A[s] = *reinterpret_cast<const bf16x8_t *>(kb + r * (HD * 2) + ((4 * s + hq) ^ paged_k_swizzle<HD, 16>(r)) * 16);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                sc[nb][kbk] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s < NS; ++s)
-#pragma unroll
-                    for (int pl = PL - 1; pl >= 0; --pl) sc[nb][kbk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[s], q[nb][s][pl], sc[nb][kbk], 0, 0, 0);
+            for (int kbk = 0; kbk < 4; ++kbk) {
+                const int r = 32 * (kbk >> 1) + 8 * (col >> 2) + 4 * (kbk & 1) + (col & 3);
+                kf[kbk][s] = *reinterpret_cast<const bf16x8_t *>(kb + r * (HD * 2) + ((4 * s + hq) ^ paged_k_swizzle<HD, 16>(r)) * 16);
             }
-        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int kbk = 0; kbk < 4; ++kbk) sc[nb][kbk] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int pl = PL - 1; pl >= 0; --pl)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int kbk = 0; kbk < 4; ++kbk) sc[nb][kbk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kbk][s], q[nb][s][pl], sc[nb][kbk], 0, 0, 0);
         // ---- the next tile's K goes where this one's was
         const bool more = left > 0;
         PagedItem nit = fit;
@@ -549,22 +555,23 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
         // ---- P V
         if (more) paged_wait_loads<NL>(); else paged_wait_loads<0>();     // all but K of the next tile
         const bool end = 64 * t + 64 > hi;
+        uint4 v[ND][2];
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            uint4 v[2];
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                v[s] = *reinterpret_cast<const uint4 *>(vb + (16 * d + col) * 128 + ((4 * s + hq) ^ paged_v_swizzle(col)) * 16);
-                if (end) v[s] = paged_first(v[s], hi - first - 32 * s);
+            for (int d = 0; d < ND; ++d) {
+                v[d][s] = *reinterpret_cast<const uint4 *>(vb + (16 * d + col) * 128 + ((4 * s + hq) ^ paged_v_swizzle(col)) * 16);
+                if (end) v[d][s] = paged_first(v[d][s], hi - first - 32 * s);
             }
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+            for (int pl = PP - 1; pl >= 0; --pl)
 #pragma unroll
-                    for (int pl = PP - 1; pl >= 0; --pl)
-                        o[nb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v[s]), pb[nb][s][pl], o[nb][d], 0, 0, 0);
-        }
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+                        o[nb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v[d][s]), pb[nb][s][pl], o[nb][d], 0, 0, 0);
         if (more) { paged_wait_reads(); fetch_v(nt, nit.kvh, page); }
         // ---- the item's or the run's last tile
         if (t + 1 == t1 || !more) {
@@ -595,8 +602,8 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
             if (ta > t0 && t + 1 == t1) paged_note_cut(a, run, it, w, ta, t0);
             if (!more) break;
             ++n_items;
-            begin = true;
             ta = n_t0;
+            begin(nit);
         }
         it = nit; t = nt; t0 = n_t0; t1 = n_t1; hi = n_hi;
     }

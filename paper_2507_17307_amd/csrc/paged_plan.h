@@ -66,14 +66,17 @@ RS_HD void paged_tiles(const Span &s, int rows, int window, int tile_shift, int 
     t0 = lo >> tile_shift; t1 = ((hi - 1) >> tile_shift) + 1;
 }
 
-// First tile of run w of W over T tiles (no product beyond T).
+// First tile of run w of W over T tiles: T w / W, rounded down (no product beyond T).
 RS_HD long long paged_run(long long T, int W, int w) {
-    if (T >> 31 == 0) { const unsigned t = (unsigned)T, n = (unsigned)W, k = (unsigned)w; return t / n * k + t % n * k / n; }      // (W is at most 2^11)
+    if (T == W) return w;
+    if (T >> 31 == 0) { const unsigned t = (unsigned)T, n = (unsigned)W, k = (unsigned)w, q = t / n; return q * k + (t - q * n) * k / n; }      // (W is at most 2^11)
     return T / W * w + T % W * w / W;
 }
 
-// The run that tile t < T is in.
+// The run that tile t < T is in: the largest w with T w / W < t + 1.
 RS_HD int paged_run_of(long long T, int W, long long t) {
+    if (T < 1 << 20) return (int)((((unsigned)t + 1) * (unsigned)W - 1) / (unsigned)T);             // (below 2^31)
+    if (T >> 50 == 0) return (int)(((t + 1) * W - 1) / T);
     int lo = 0, hi = W - 1;
     while (lo < hi) { const int mid = (lo + hi) / 2; if (paged_run(T, W, mid + 1) > t) hi = mid; else lo = mid + 1; }
     return lo;
