@@ -36,14 +36,17 @@ struct PagedAttnArgs {
     int n_q, group, window, rows, runs;        // rows: of a block of columns; runs: workgroups of the call
     float c;                                   // scale log2 e
     int rsh;                                   // >= 0: fp32 output in operand order with blocks of 1 << rsh rows (frag_index) in the place of rows
-    int4 *cuts;                                // per run: the cut item that ends in it {first row, KV head, columns, first run}, first row < 0: none
-    int2 *cut_of;                              // ... and its {sequence, block}
-    unsigned int *odd;                         // per run: bit k % 32: its item k is whole and its sums hold a NaN
+    // What is left for k_paged_join: by item, if the call has no more of them than max_items, else by run, the cut item that ends in it.
+    int max_items;                             // 0: k_paged_narrow, or more items than runs
+    int *entries;                              // how many there are, by item; -1: by run
+    int4 *cuts;                                // {first row, KV head, columns, first run | runs << 16}, first row < 0: nothing to do; no runs: whole, with a NaN in its sums
+    int2 *cut_of;                              // its {sequence, block}
+    unsigned int *odd;                         // by run: bit k % 32: its item k is whole and its sums hold a NaN
     float *part_ml, *part_o;                   // [2 runs][2][columns], [2 runs][columns][head_dim]
 };
 
 struct PagedItem { int b, kvh, blk, n_blk; Span s; };
-struct PagedRun { PagedItem at; int ta; long long left, T; int W; };       // first item, first tile of it, tiles of the run
+struct PagedRun { PagedItem at; int ta, W, item, n_items; long long left, T; };       // first item, first tile of it; its number, items of the call (-1: too many to have entries); tiles of the run, of the call
 
 // Sum over this lane and those before it: in 32 bits without LDS where no sum passes them.
 __device__ __forceinline__ long long wave_prefix(long long v) {
@@ -66,7 +69,7 @@ __device__ __forceinline__ long long lane_value(long long v, int lane) {
     return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, lane));
 }
 
-constexpr int PAGED_RUN_LDS = 12;              // long long
+constexpr int PAGED_RUN_LDS = 16;              // long long
 
 // What run w has to do; false: nothing.  All NT threads of the workgroup get the same.  sh: PAGED_RUN_LDS long long (one wave: not used).
 template <int NT>
@@ -80,7 +83,7 @@ __device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int w, lo
     s.first = s.m = s.slot = s.p0 = 0;
     auto tiles = [&](int b, int from, int by) __attribute__((always_inline)) {
         long long sum = 0;
-        if (!paged_span(a.s, b, s)) { if (blockIdx.x == 0 && from == 0) paged_flag(a.s, b); }
+        if (!paged_span(a.s, b, s)) { s.m = 0; if (blockIdx.x == 0 && from == 0) paged_flag(a.s, b); }
         else {
             const int nb = paged_blocks(s, a.rows);
             for (int j = from; j < nb; j += by) { int t0, t1; paged_tiles(s, a.rows, a.window, PAGED_TILE, j, t0, t1); sum += t1 - t0; }
@@ -88,17 +91,23 @@ __device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int w, lo
         return sum;
     };
     long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tiles(b, sub, share);
+    int blocks = 0;
+    for (int b = b0; b < b1; ++b) { mine += tiles(b, sub, share); if (NT > 64) blocks += paged_blocks(s, a.rows); }
     for (int o = 1; o < share; o <<= 1) mine += __shfl_xor(mine, o, RS_WAVE);
     const long long own = sub == 0 ? mine * a.s.n_kv : 0;
+    const int own_items = sub == 0 && a.max_items > 0 ? blocks * a.s.n_kv : 0;     // (max_items bounds the rows of a call, so that these stay small)
     long long end = wave_prefix(own), T;
+    int items = 0;
     if constexpr (NT == 64) T = lane_value(end, 63);
     else {
-        if (lane == 63) sh[wave] = end;
+        if (a.max_items > 0) items = (int)wave_prefix(own_items);
+        if (lane == 63) { sh[wave] = end; sh[12 + wave] = items; }
         __syncthreads();
-        T = 0;
-        for (int i = 0; i < NT / 64; ++i) { if (i < wave) end += sh[i]; T += sh[i]; }
+        T = 0; run.n_items = 0;
+        for (int i = 0; i < NT / 64; ++i) { if (i < wave) { end += sh[i]; items += (int)sh[12 + i]; } T += sh[i]; run.n_items += (int)sh[12 + i]; }
     }
+    items -= own_items;
+    if (NT == 64 || a.max_items == 0 || run.n_items > a.max_items) run.n_items = -1;           // (spans that are no partition of the rows may bring more items than those do)
     const int W = T < a.runs ? (int)T : a.runs;              // (a tile a run at least)
     if (w >= W) return false;
     const long long t0 = paged_run(T, W, w);
@@ -114,6 +123,7 @@ __device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int w, lo
                 of = tiles(b, 0, 1);
                 if (rem < of * a.s.n_kv) break;
                 rem -= of * a.s.n_kv;
+                if (NT > 64) items += paged_blocks(s, a.rows) * a.s.n_kv;
             }
     }
     PagedItem &it = run.at;
@@ -123,11 +133,12 @@ __device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int w, lo
         it.s.first = __builtin_amdgcn_readlane(s.first, who); it.s.m = __builtin_amdgcn_readlane(s.m, who);
         it.s.slot = __builtin_amdgcn_readlane(s.slot, who); it.s.p0 = __builtin_amdgcn_readlane(s.p0, who);
     } else {
-        if (found) { sh[4] = b; sh[5] = rem; sh[6] = of; sh[7] = s.first; sh[8] = s.m; sh[9] = s.slot; sh[10] = s.p0; }
+        if (found) { sh[11] = items; sh[4] = b; sh[5] = rem; sh[6] = of; sh[7] = s.first; sh[8] = s.m; sh[9] = s.slot; sh[10] = s.p0; }
         __syncthreads();
         auto value = [&](int i) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane((int)sh[i]); };
         it.b = value(4); rem = lane_value(sh[5], 0); of = lane_value(sh[6], 0);
         it.s.first = value(7); it.s.m = value(8); it.s.slot = value(9); it.s.p0 = value(10);
+        run.item = value(11);
     }
     it.n_blk = paged_blocks(it.s, a.rows);
     it.kvh = rem >> 31 == 0 && of >> 31 == 0 ? (int)((unsigned)rem / (unsigned)of) : (int)(rem / of);
@@ -150,6 +161,7 @@ __device__ __forceinline__ bool paged_find_run(const PagedAttnArgs &a, int w, lo
     }
     it.blk = __builtin_amdgcn_readfirstlane(j);
     run.ta = __builtin_amdgcn_readfirstlane(u0 + (int)rem);
+    if (NT > 64) run.item += it.kvh * it.n_blk + it.blk;
     return true;
 }
 
@@ -163,12 +175,21 @@ __device__ __forceinline__ void paged_next(const PagedAttnArgs &a, PagedItem &it
     it.n_blk = paged_blocks(it.s, a.rows);
 }
 
-// If item `it`, of which this run w starts at tile ta > t0 and reaches the end, has been cut: what the joining kernel needs.
-__device__ __forceinline__ void paged_note_cut(const PagedAttnArgs &a, const PagedRun &run, const PagedItem &it, int w, int ta, int t0) {
+// Item `it`, number `item`, ends in run w, which has it from tile ta of t0 .. on: what is left for the joining kernel, if anything.  odd: its sums hold a NaN.
+__device__ __forceinline__ void paged_note_end(const PagedAttnArgs &a, const PagedRun &run, const PagedItem &it, int w, int item, int ta, int t0, bool odd) {
     if (threadIdx.x != 0) return;
-    const int r0 = it.blk * a.rows;
-    a.cuts[w] = make_int4(it.s.first + r0, it.kvh, min(a.rows, it.s.m - r0) * a.group, paged_run_of(run.T, run.W, paged_run(run.T, run.W, w) - (ta - t0)));
-    a.cut_of[w] = make_int2(it.b, it.blk);
+    const bool by_item = run.n_items >= 0;
+    const int at = by_item ? item : w, r0 = it.blk * a.rows;
+    if (ta == t0 && !(odd && by_item)) { if (by_item) a.cuts[at] = make_int4(-1, 0, 0, 0); return; }
+    const int first = ta > t0 ? paged_run_of(run.T, run.W, paged_run(run.T, run.W, w) - (ta - t0)) : 0, pieces = ta > t0 ? w - first + 1 : 0;
+    a.cuts[at] = make_int4(it.s.first + r0, it.kvh, min(a.rows, it.s.m - r0) * a.group, first | pieces << 16);
+    a.cut_of[at] = make_int2(it.b, it.blk);
+}
+// Before the first item of run w, also of one that has none.
+__device__ __forceinline__ void paged_note_start(const PagedAttnArgs &a, const PagedRun &run, int w) {
+    if (threadIdx.x != 0) return;
+    if (a.max_items > 0 && w == 0) *a.entries = run.n_items;
+    if (run.n_items < 0) { a.cuts[w] = make_int4(-1, 0, 0, 0); a.odd[w] = 0; }
 }
 
 // Page table entry of position pos, or of the position nearest to it among the needed ones, lo .. hi - 1; asked for ahead of its use, which checks it:
@@ -427,7 +448,7 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
     const int lane = threadIdx.x, col = lane & 15, hq = lane >> 4, w = blockIdx.x, ps = 1 << a.s.page_shift;
     PagedRun run;
     const bool some = paged_find_run<64>(a, w, nullptr, run);
-    if (lane == 0) { a.cuts[w] = make_int4(-1, 0, 0, 0); a.odd[w] = 0; }
+    paged_note_start(a, run, w);
     if (!some) return;
     // ---- the tile that is fetched next: `left` tiles of the run from it on, positions lo .. hi - 1 of its item are needed
     PagedItem fit = run.at;
@@ -598,8 +619,9 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
                     else if (a.lse) a.lse[row * a.n_q + h] = (m[nb] * a.c + __log2f(l[nb])) * 0.69314718055994531f;
                 }
             }
-            if (whole && __any(poison != poison)) odd |= 1u << (n_items & 31);
-            if (ta > t0 && t + 1 == t1) paged_note_cut(a, run, it, w, ta, t0);
+            const bool nan = __any(poison != poison);
+            if (whole && nan) odd |= 1u << (n_items & 31);
+            if (t + 1 == t1) paged_note_end(a, run, it, w, 0, ta, t0, nan);
             if (!more) break;
             ++n_items;
             ta = n_t0;
@@ -627,7 +649,7 @@ __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnAr
     const int w = (blockIdx.x & 7) * (a.runs / 8) + (blockIdx.x >> 3);         // (workgroups go round the eight XCDs)
     PagedRun run;
     const bool some = paged_find_run<256>(a, w, run_sh, run);
-    if (tid == 0) { a.cuts[w] = make_int4(-1, 0, 0, 0); a.odd[w] = 0; }
+    paged_note_start(a, run, w);
     if (!some) return;
     PagedItem it = run.at;
     int ta = run.ta;
@@ -789,21 +811,26 @@ __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnAr
 #pragma unroll
             for (int i = 0; i < 16; ++i) poison += o[d][i];
         const int part = ta == t0 && tb == t1 ? -1 : 2 * w + (ta == t0);
-        if (__syncthreads_or(valid && poison != poison) && part < 0) odd |= 1u << (n_items & 31);
+        const bool nan = __syncthreads_or(valid && poison != poison);
+        if (nan && part < 0) odd |= 1u << (n_items & 31);
         if (valid) paged_store_cols<HD, PL>(a, it.s.first + r0 + row, head, c, COLS, part, hh, m, l, o);
-        if (ta > t0 && tb == t1) paged_note_cut(a, run, it, w, ta, t0);
+        if (tb == t1) paged_note_end(a, run, it, w, run.item + n_items, ta, t0, nan);
         run.left -= tb - ta;
         if (run.left <= 0) break;
         paged_next(a, it);
         int n1;
         paged_tiles(it.s, a.rows, a.window, PAGED_TILE, it.blk, ta, n1);
     }
-    if (tid == 0) a.odd[w] = odd;
+    if (tid == 0 && run.n_items < 0) a.odd[w] = odd;
 }
 
 // ------------------------------------------------------------------------------------------------
-// k_paged_join: the pieces of a cut item, in the order of their runs.  grid (runs, column groups), block 256: HD / 4 threads a column.
-// And the items, whole or cut, whose sums hold a NaN, once more.
+// k_paged_join: the pieces of a cut item, in the order of their runs, and the items, whole or cut, whose sums hold a NaN, once more.
+// grid (runs, shares) or, by item, (entries * shares), block 256: HD / 4 threads a column and, with narrow blocks, whose pieces are many, four such groups that
+// share them (of two and four groups with wide blocks 26 and 45 us in the place of 19).  Every piece is read once, eight at a time; what bounds it are the loads'
+// time of flight (one fp32 token of 28 heads over 4096 positions: 4 us) and its workgroups, 2.7 ns for one that has no work.  Hence an entry per item where
+// a wide call has few: 61 rows of 40 query heads on 8 behind 3700 positions, 24 entries of 16 shares in the place of 256: 19.4 -> 6.0 us.
+// At least three waves a SIMD: chunks of 8192 rows 27 us, two (180 registers, the NaN's part) 34.
 // ------------------------------------------------------------------------------------------------
 template <int HD, int COLS>
 __host__ __device__ constexpr int join_groups() { return COLS == PAGED_COLS ? 1 : 4; }                     // threads that share a column's pieces between them: many pieces where blocks are small
@@ -811,23 +838,31 @@ template <int HD, int COLS>
 __host__ __device__ constexpr int join_cols() { return 1024 / HD / join_groups<HD, COLS>(); }            // columns a workgroup
 
 template <int HD, int PL, int COLS>
-__global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
+__global__ void __launch_bounds__(256, 3) k_paged_join(PagedAttnArgs a) {
     constexpr int TPC = HD / 4, G = join_groups<HD, COLS>(), CPW = join_cols<HD, COLS>(), BATCH = 8;
     __shared__ long long run_sh[PAGED_RUN_LDS];
     __shared__ float o_sh[G > 1 ? G : 1][CPW][HD + 4];
-    const int w = blockIdx.x, wave = threadIdx.x >> 6;
+    const int wave = threadIdx.x >> 6;
+    int w = blockIdx.x, part = blockIdx.y, share = gridDim.y, n_items = -1;               // workgroup `part` of `share` of entry w
+    if (COLS == PAGED_COLS && a.max_items > 0) {
+        n_items = *a.entries;
+        const unsigned entries = n_items < 0 ? a.runs : n_items;
+        if (entries == 0) return;
+        share = gridDim.x / entries; w = blockIdx.x % entries; part = blockIdx.x / entries;
+        if (part >= share) return;
+    }
     const int4 cut = a.cuts[w];
-    const unsigned int odd = blockIdx.y == 0 ? a.odd[w] : 0;
+    const unsigned int odd = part == 0 && n_items < 0 ? a.odd[w] : 0;
     if (cut.x < 0 && !odd) return;
     if (cut.x >= 0) {
-        const int kvh = cut.y, n_col = cut.z, n = w - cut.w + 1;
+        const int kvh = cut.y, n_col = cut.z, first = cut.w & 0xffff, n = cut.w >> 16;
         const int unit = threadIdx.x / TPC, g = unit / CPW, lc = unit % CPW, d = 4 * (threadIdx.x % TPC);
-        for (int from = blockIdx.y * CPW; from < n_col; from += gridDim.y * CPW) {
+        for (int from = part * CPW; from < n_col; from += share * CPW) {
         const int c = from + lc;
-        bool nan = false;
+        bool nan = n == 0;
         float M = -INFINITY, L = 0.f, x[4] = {};
         if (c < n_col) {
-            // piece i is the start of run cut.w + i, except the first one, which is the end of its run.  A batch's loads are under way together.
+            // piece i is the start of run first + i, except the first one, which is the end of its run.  A batch's loads are under way together.
             for (int i0 = g; i0 < n; i0 += G * BATCH) {
                 float m[BATCH], l[BATCH];
                 float4 y[BATCH];
@@ -836,9 +871,9 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
                     const int i = i0 + G * k;
                     m[k] = -INFINITY; l[k] = 0.f; y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (i >= n) continue;
-                    const size_t part = 2 * (size_t)(cut.w + i) + (i == 0);
-                    m[k] = a.part_ml[part * 2 * COLS + c]; l[k] = a.part_ml[(part * 2 + 1) * COLS + c];
-                    y[k] = *reinterpret_cast<const float4 *>(a.part_o + (part * COLS + c) * HD + d);
+                    const size_t at = 2 * (size_t)(first + i) + (i == 0);
+                    m[k] = a.part_ml[at * 2 * COLS + c]; l[k] = a.part_ml[(at * 2 + 1) * COLS + c];
+                    y[k] = *reinterpret_cast<const float4 *>(a.part_o + (at * COLS + c) * HD + d);
                 }
                 float top = M;
 #pragma unroll
@@ -870,7 +905,7 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedAttnArgs a) {
                 x[0] = fmaf(y.x, e, x[0]); x[1] = fmaf(y.y, e, x[1]); x[2] = fmaf(y.z, e, x[2]); x[3] = fmaf(y.w, e, x[3]);
             }
         }
-        if (c < n_col && g == 0) {
+        if (c < n_col && g == 0 && n > 0) {
             const int r = c / a.group, h = kvh * a.group + c - r * a.group;
             const size_t row = (size_t)(cut.x + r);
             const float inv = 1.f / L, all = (x[0] + x[1]) + (x[2] + x[3]);

@@ -74,7 +74,7 @@ int paged_cols(int n_seqs, int n_rows, int group, int n_kv, int dtype) {
     return cols <= 16 ? 16 : cols <= (few ? 64 : 32) ? 32 : PAGED_COLS;
 }
 
-struct PagedShape { int cols, rows, runs; long long items; size_t of, odd, ml, o, total; };
+struct PagedShape { int cols, rows, runs; long long items; size_t of, odd, entries, ml, o, total; };
 PagedShape paged_shape(const rs_paged_kv *cache, int n_seqs, int n_rows, int n_q_heads, int dtype) {
     const int n_kv = cache->n_kv_heads, head_dim = cache->head_dim, group = n_q_heads / n_kv;
     PagedShape p{};
@@ -87,7 +87,8 @@ PagedShape paged_shape(const rs_paged_kv *cache, int n_seqs, int n_rows, int n_q
     if (tiles < p.runs) p.runs = ((int)tiles + 7) / 8 * 8;                     // (whole rounds of the XCDs)
     p.of = align_up((size_t)p.runs * sizeof(int4));
     p.odd = p.of + align_up((size_t)p.runs * sizeof(int2));
-    p.ml = p.odd + align_up((size_t)p.runs * 4);
+    p.entries = p.odd + align_up((size_t)p.runs * 4);
+    p.ml = p.entries + align_up(4);
     p.o = p.ml + align_up((size_t)2 * p.runs * 2 * p.cols * 4);
     p.total = p.o + align_up((size_t)2 * p.runs * p.cols * head_dim * 4);
     return p;
@@ -98,10 +99,11 @@ rs_status launch_paged(const PagedAttnArgs &a, const PagedShape &p, hipStream_t 
     if constexpr (COLS == PAGED_COLS) hipLaunchKernelGGL((k_paged_wide<HD, PL>), dim3(a.runs), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_paged_narrow<HD, PL, COLS / 16>), dim3(a.runs), dim3(64), 0, st, a);
     RS_LAUNCHED("paged_attention");
-    // about 2048 workgroups for the items that can be cut (one a run at most); the others end at once
+    // about 2048 workgroups, as far as a block has columns for them; by item at least one a run too, should it come to that
     constexpr int per = join_cols<HD, COLS>();
-    const int cut = p.items < a.runs ? (int)p.items : a.runs, most = (a.rows * a.group + per - 1) / per, want = (2048 + cut - 1) / cut;
-    hipLaunchKernelGGL((k_paged_join<HD, PL, COLS>), dim3(a.runs, want < most ? want : most), dim3(256), 0, st, a);
+    const int entries = a.max_items > 0 ? a.max_items : a.runs, most = (a.rows * a.group + per - 1) / per, want = (2048 + entries - 1) / entries, shares = want < most ? want : most;
+    const dim3 grid = a.max_items > 0 ? dim3(entries * shares > a.runs ? entries * shares : a.runs) : dim3(entries, shares);
+    hipLaunchKernelGGL((k_paged_join<HD, PL, COLS>), grid, dim3(256), 0, st, a);
     RS_LAUNCHED("paged_join");
     return RS_OK;
 }
@@ -151,9 +153,9 @@ rs_status run_paged_attention(const rs_paged_kv *cache, const PagedSpans &spans,
     a.kc = (const uint16_t *)cache->k; a.vc = (const uint16_t *)cache->v;
     a.q = q; a.out = out; a.lse = lse; a.q_stride = q_stride; a.out_stride = out_stride; a.rsh = out_rsh;
     a.n_q = n_q_heads; a.group = n_q_heads / cache->n_kv_heads; a.window = window; a.rows = p.rows;
-    a.runs = p.runs;
+    a.runs = p.runs; a.max_items = p.cols == PAGED_COLS && p.items <= p.runs ? (int)p.items : 0;
     a.c = scale * 1.44269504088896341f;
-    a.cuts = (int4 *)scratch; a.cut_of = (int2 *)(scratch + p.of); a.odd = (unsigned int *)(scratch + p.odd);
+    a.cuts = (int4 *)scratch; a.cut_of = (int2 *)(scratch + p.of); a.odd = (unsigned int *)(scratch + p.odd); a.entries = (int *)(scratch + p.entries);
     a.part_ml = (float *)(scratch + p.ml); a.part_o = (float *)(scratch + p.o);
     return dtype == RS_F32 ? launch_paged_hd<3>(cache->head_dim, a, p, st) : launch_paged_hd<1>(cache->head_dim, a, p, st);
 }

@@ -115,6 +115,25 @@ def test_rows_out_of_range_are_skipped_and_flagged():
     paged.close(lse[12:], z[12:], ez[12:])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("odd", [False, True])
+def test_offsets_that_step_back_are_flagged_and_do_not_disturb_the_others(odd, dtype):
+    """Sequences 0, 2 and 4 are the same rows, which brings more blocks than n_rows rows have; sequence 5 is alone in its rows."""
+    pg = paged.Pages([400, 3], [100, 30], 2, 64, 16, seed=44)
+    if odd:
+        pg.v[pg.table[pg.slot[0], 3], 1, 5, 7] = math.nan
+    pg.gpu()
+    q = torch.randn(pg.rows, 10, 64, generator=pg.gen).to(dtype)
+    pg.n = 6
+    pg.doff = torch.tensor([0, 400, 0, 400, 0, 400, 403], dtype=torch.int32, device="cuda")
+    pg.dslot = pg.dslot[[0, 0, 0, 0, 0, 1]].contiguous()
+    pg.dpos = pg.dpos[[0, 0, 0, 0, 0, 1]].contiguous()
+    flags = torch.zeros(6, dtype=torch.int32, device="cuda")
+    out, lse = call(pg, q, 0.1, flags=flags)
+    assert flags.tolist() == [0, 16, 0, 16, 0, 0]
+    check(pg, q, 0.1, 0, out, lse)
+
+
 def test_a_page_that_the_window_has_left_behind_may_be_gone():
     pg = paged.Pages([3, 1], [100, 200], 2, 64, 16, seed=34).gpu()
     q = torch.randn(pg.rows, 6, 64, generator=pg.gen)
