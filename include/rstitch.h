@@ -375,7 +375,7 @@ typedef struct rs_paged_kv {
     int32_t page_size;           /* a power of two, 16 .. 1024                                */
     int32_t n_slots;             /* >= 1                                                      */
     int32_t max_pages;           /* >= 1; page_size * max_pages <= 2^30                       */
-    int32_t n_kv_heads;          /* >= 1                                                      */
+    int32_t n_kv_heads;          /* 1 .. 1024                                                 */
     int32_t head_dim;            /* 32, 64 or 128                                             */
 } rs_paged_kv;
 
@@ -437,7 +437,7 @@ rs_status rs_rope_rows(const rs_rope *rope, int32_t n_rows, const int32_t *d_pos
  *   rope            NULL: nothing is rotated
  *   dtype           RS_F32 or RS_BF16: type of q, k, v and q_out
  *   d_q, d_k, d_v   DEVICE [n_rows][heads][head_dim], rows a stride (elements) apart, heads back to back: three
- *                   buffers, or three places in the rows of one; n_q_heads >= 1 (any number), cache->n_kv_heads
+ *                   buffers, or three places in the rows of one; n_q_heads in 1 .. 16384, cache->n_kv_heads
  *   d_q_out         DEVICE; may be d_q itself if the strides are equal
  *   d_flags         DEVICE uint32 [n_seqs] or NULL: RS_FLAG_BADARG is or-ed into the word of a sequence with a slot, span
  *                   or position out of range, whose rows are all skipped, or with a row whose page is no page of

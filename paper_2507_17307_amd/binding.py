@@ -544,6 +544,8 @@ class PagedModel(Model):
 
     def __init__(self, weights, max_ctx: int, n_pages: int, page_size: int = 64, max_seqs: int = 1, max_rows: int = 64, device="cuda"):
         self.handle = 0
+        if n_pages < 1 or page_size < 1:
+            raise RsError(-1, "n_pages and page_size must be at least 1")
         self.shape = s = weights.shape
         self.weights = weights
         max_ctx = (max_ctx + 7) // 8 * 8

@@ -437,8 +437,10 @@ __device__ __forceinline__ void paged_fetch_v(const PagedAttnArgs &a, int t, int
 
 // ------------------------------------------------------------------------------------------------
 // k_paged_narrow: up to 16 NB columns a block (decode steps, spans of a few rows).  grid: runs, block 64: a wave by itself, four of them on a CU, each
-// with one tile of K and one of V in LDS.  Bound by the cache's bytes: K of the next tile is on its way while V of this one is multiplied, and the
-// other way round, also from one item to the next, so that a CU has about 100 KB under way.
+// with one tile of K and one of V in LDS.  Bound by the cache's bytes where there are many, by the chain of loads where there are few: K of the next tile
+// is on its way while V of this one is multiplied, and the other way round, also from one item to the next, so that a CU has about 100 KB under way.
+// One fp32 token: 12 heads on 2, 200 positions 8.5 us; 28 heads on 4, 4561 positions (9.4 MB) 9.3 us: a launch, the search for
+// the run, page table, K, V and the stores one after the other.
 // ------------------------------------------------------------------------------------------------
 template <int HD, int PL, int NB>
 __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
@@ -637,7 +639,12 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
 // once for all columns, by direct loads that are one tile ahead (two buffers); a wave has 32 columns.
 // Sharing the XCD's L2: neighbouring runs, which read the same K and V, are an XCD's, and they read the same tiles at the same time, because a run begins each item at
 // the tile that its count of tiles so far gives, modulo the item's, and goes round.  Begun at the first tile each, runs were spread over the whole context
-// and 11 % of the requests met in L2: 8.7 GB at 6 TB/s from beyond it for the four chunks of 2048 rows on up to 14000 positions.
+// and 11 % of the requests met in L2: 8.7 GB at 6 TB/s from beyond it for the four chunks of 2048 rows on up to 14000 positions.  Now 62 % do, which is 2 % of the time
+// (1243 -> 1219 us).
+// Those chunks (40 bf16 heads of 128 on 8, 1.09 TFLOP): 1210 us, 900 TFLOP/s, 73 % of the rate of a large bf16 product (1226); products and exponentials take turns
+// in a wave and two waves a SIMD fill each other's gaps.  With the scores of the next tile computed beside this one's exponentials the registers leave one
+// wave a SIMD, 2040 us, or spill, 3680.  128 bf16 tokens of 28 heads on 4, 512 .. 4607 positions each (707 MB): 132 us, 5.4 TB/s.  61 fp32 rows, three planes, one wave a
+// SIMD: 60 us.  701 bf16 rows of 33 sequences, head size 64, window 1000: 20 us.
 // ------------------------------------------------------------------------------------------------
 template <int HD, int PL>
 __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnArgs a) {
@@ -828,8 +835,8 @@ __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnAr
 // k_paged_join: the pieces of a cut item, in the order of their runs, and the items, whole or cut, whose sums hold a NaN, once more.
 // grid (runs, shares) or, by item, (entries * shares), block 256: HD / 4 threads a column and, with narrow blocks, whose pieces are many, four such groups that
 // share them (of two and four groups with wide blocks 26 and 45 us in the place of 19).  Every piece is read once, eight at a time; what bounds it are the loads'
-// time of flight (one fp32 token of 28 heads over 4096 positions: 4 us) and its workgroups, 2.7 ns for one that has no work.  Hence an entry per item where
-// a wide call has few: 61 rows of 40 query heads on 8 behind 3700 positions, 24 entries of 16 shares in the place of 256: 19.4 -> 6.0 us.
+// time of flight (one fp32 token of 28 heads over 4561 positions: 4 us) and its workgroups, 2.7 ns for one that has no work.  Hence an entry per item where
+// a wide call has few: 61 rows of 40 query heads on 8 behind 9001 positions, 24 entries of 16 shares in the place of 256: 19.4 -> 6.0 us.
 // At least three waves a SIMD: chunks of 8192 rows 27 us, two (180 registers, the NaN's part) 34.
 // ------------------------------------------------------------------------------------------------
 template <int HD, int COLS>

