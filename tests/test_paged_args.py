@@ -217,3 +217,11 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     for bad in ((r, one, q.half(), q.half()), (r, one, q, q.bfloat16()), (r, one[:1], q, q), (r, one, q, q[:, :2])):
         with pytest.raises(ValueError):
             P.rs_rope_rows(*bad)
+
+
+@pytest.mark.parametrize("n_pages,page_size", [(0, 64), (-1, 64), (4, 0), (4, -16)])
+def test_an_empty_pool_is_refused_before_anything_is_allocated(n_pages, page_size):
+    import paper_2507_17307_amd as P
+    with pytest.raises(P.RsError) as e:
+        P.PagedModel(None, 128, n_pages, page_size)
+    assert e.value.status == -1
