@@ -26,7 +26,8 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int PAGED_COLS = 128;                // columns of a workgroup of k_paged_wide
 constexpr int PAGED_TILE = 6;                  // log2 positions of a tile
-constexpr int PAGED_WIDE_RUNS = 512, PAGED_WIDE_RUNS3 = 256, PAGED_NARROW_RUNS = 1024;      // of a call, at most: what the CUs hold at a time (RUNS3: with three planes)
+constexpr int PAGED_WIDE_RUNS = 512, PAGED_WIDE_RUNS3 = 256, PAGED_NARROW_RUNS = 1024;      // of a call, at most: what the CUs hold at a time (RUNS3: with three planes).
+// Head sizes 32 and 64 leave room for more wide ones, which lose: 64 bf16 tokens, 8 KV heads of 64, 4000 positions, 512 / 768 / 1024: 102 / 125 / 111 us.
 
 struct PagedAttnArgs {
     PagedSpans s;
