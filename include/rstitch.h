@@ -458,7 +458,8 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
  *   out = sum_j softmax_j(scale q . k_j) v_j;  lse = ln sum_j exp(scale q . k_j)
  *   n_seqs .. d_pos0  as in rs_paged_append (slots may repeat: nothing is written to the cache)
  *   dtype             type of d_q and d_out.  Sums are fp32.  RS_F32: products of fp32 q and fp32 probabilities with the
- *                     bf16 cache, exact to fp32; RS_BF16: probabilities may be rounded to bf16 for the matrix cores
+ *                     bf16 cache, exact to fp32; RS_BF16: probabilities have 16 significant bits in the matrix cores, in spans
+ *                     whose rows times query heads of a KV head are more than 128 they may have 8, as the output has
  *   n_q_heads         a multiple of n_kv_heads, at most 16 times as many
  *   scale             > 0, below 2^127
  *   window            >= 0

@@ -6,9 +6,10 @@
 //   out[d, column]           = sum_j V[j, d] p[column, j]              A = V, which the pages hold by channel, B = p
 // The accumulators of the first product are the B operand of the second as they lie: which position a row of A stands for is free, and
 // is chosen so that the lane that needs k slots 8 h .. 8 h + 7 holds the scores of eight consecutive positions.  With fp32 q both q
-// and p are three bf16 planes (exact: 3 x 8 significant bits).  With bf16 q, q is one plane and p two (k_paged_narrow) or one (k_paged_wide, where the
-// matrix cores are the bound): p is then rounded to bf16, half a step (2^-8 of a term) at most, as the output is.  Errors from 64 bits, 128 sequences / chunks of
-// 2048 rows: the output's rounding alone 1.7e-3 / 1.5e-3, with p of one plane 2.2e-3 / 2.0e-3.
+// and p are three bf16 planes (exact: 3 x 8 significant bits).  With bf16 q, q is one plane and p two (16 bits: what is left out is 2^-16 of a term), except in spans
+// of several blocks of k_paged_wide (more than 128 columns), where the matrix cores are the bound: there p is rounded to bf16, half a step (2^-8 of a term) at most, as the
+// output is.  Errors from 64 bits: 128 sequences of a token 1.7e-3, as the output's rounding alone (with p of one plane 2.2e-3); chunks of 2048 rows, p of one plane, 2.0e-3
+// (the output's rounding alone 1.5e-3).
 //
 // Positions that a row does not see have p = 0, whatever the page holds there.  0 does not take an infinity or a NaN away (and a low plane of p
 // may be negative, which turns a seen infinity into a NaN), but every such product is a NaN in the sum: an item whose sums hold one
@@ -677,6 +678,10 @@ __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnAr
         int see_lo, see_hi;
         paged_seen(it.s, r0 + row, r0 + row + 1, a.window, see_lo, see_hi);
         if (!valid) see_hi = 0;
+        // bf16 rows: a second plane of p unless the span has several blocks, so that a row's bits depend on its span alone.  One block, us with two planes / one, in a graph: 128
+        // single tokens 144 / 140; 33 spans of up to 32 rows behind a window 28.6 / 27.1; 32 spans of 20 rows, 100 columns, 168 / 165; head size 64, 64 spans of 30 rows 98 / 84.
+        // Several: four chunks of 2048 rows 1620 / 1235 (with the choice 1253: the registers it takes).
+        const bool two_planes = PL == 1 && it.n_blk == 1;
         bf16x8_t q[NS][PL];
         {
             const size_t at = (size_t)(it.s.first + r0 + row) * a.q_stride + (size_t)head * HD + 8 * hh;
@@ -771,6 +776,12 @@ __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnAr
                 for (int d = 0; d < ND; ++d)
 #pragma unroll
                     for (int pl = PL - 1; pl >= 0; --pl) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s & 1][d], pb[pl], o[d], 0, 0, 0);
+                if (two_planes) {
+                    bf16x8_t both[2];
+                    paged_planes<2>(p, both);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s & 1][d], both[1], o[d], 0, 0, 0);
+                }
             }
         };
         auto compute = [&](int t, const unsigned char *kb, const unsigned char *vb) __attribute__((always_inline)) {
