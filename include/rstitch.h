@@ -491,8 +491,10 @@ rs_status rs_paged_attention(const rs_paged_kv *cache, int32_t n_seqs, int32_t n
  *           max_pages >= max_ctx
  *   workspace  as in rs_create_model, of at least rs_paged_workspace_bytes (0 on a
  *           bad argument)
- * A row whose page is no page of the cache is skipped and RS_FLAG_BADARG set in the
- * record of its sequence, and in that of one which sees such a page.
+ * A sequence without a page of the cache for some position up to its last row's is
+ * skipped like one whose position is out of range: RS_FLAG_BADARG is set in its
+ * record and nothing of it is written, so that the same call can be made again
+ * once the pages are there.
  * rs_stitch_generate does not take such a model (RS_ENOTIMPL).
  * Errors: as rs_create_model. */
 size_t    rs_paged_workspace_bytes(const rs_config *cfg, const rs_paged_kv *cache);

@@ -539,7 +539,8 @@ class PagedModel(Model):
     """A Model whose K/V cache is a pool of n_pages pages of page_size positions that its sequence slots draw from.
 
     reserve(slot, positions) gives a slot the pages for its first `positions` positions (the calls do not do it by
-    themselves: the tokens a call feeds need their pages before it), release(slot) gives them back.  Both write the page table
+    themselves: the tokens a call feeds need their pages before it, and a sequence without them is flagged and left as it
+    is), release(slot) gives them back.  Both write the page table
     on the current stream, after which calls on that stream see it."""
 
     def __init__(self, weights, max_ctx: int, n_pages: int, page_size: int = 64, max_seqs: int = 1, max_rows: int = 64, device="cuda"):

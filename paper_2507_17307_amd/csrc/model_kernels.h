@@ -96,8 +96,10 @@ __device__ __forceinline__ void prepare_row(const PrepArgs &a, int r, int *sh) {
         const int slot = s_slot[b], p0 = s_pos[b];
         if (slot < 0 || slot >= a.max_seqs || p0 < 0 || p0 > a.max_ctx - (hi - lo)) bad2 = 1;
         else if (a.page_table) {
-            page = a.page_table[(size_t)slot * a.max_pages + ((p0 + r - lo) >> a.page_shift)];
-            if (page < 0 || page >= a.n_pages) bad2 = 1;
+            // a page for every position up to the span's last, or none of the sequence is computed: its later rows would see what lies in other pages
+            const int *table = a.page_table + (size_t)slot * a.max_pages;
+            page = table[(p0 + r - lo) >> a.page_shift];
+            for (int i = tid; i <= (p0 + hi - lo - 1) >> a.page_shift; i += 256) { const int p = table[i]; if (p < 0 || p >= a.n_pages) bad2 = 1; }
         }
         if (tid < ns && tid != b && s_slot[tid] == slot) bad2 = 1;       // slots must be distinct
         if (tid >= lo && tid < hi && (s_tok[tid] < 0 || s_tok[tid] >= a.vocab)) bad2 = 1;
