@@ -1,7 +1,9 @@
 // Attention of new tokens over a cache in pages (rs_paged_attention).
 //
-// out = sum_j p_j v_j / sum_j p_j with p_j = 2^(c (q.k_j - m)), c = scale log2 e, over the positions that the row sees, in one
-// pass with a running maximum m.  Both products run on the matrix cores, transposed, so that a lane follows one (row, query head):
+// out = sum_j p_j v_j / sum_j p_j with p_j = 2^(c q.k_j - m), c = scale log2 e, over the positions that the row sees, in one
+// pass with m the running maximum of c q.k_j, rounded: m is the number itself that p is relative to, so that sums stay as they are where no larger score follows, and
+// are multiplied by 2^(m - m') where m' does.  (A running maximum of q.k_j does not do: its product with c is rounded in one place and not in the other, and every tile
+// brings that difference again.  lse of 16000 equal scores of 4000 was 0.02 off.)  Both products run on the matrix cores, transposed, so that a lane follows one (row, query head):
 //   scores[position, column] = sum_d K[position, d] q[column, d]       A = K, B = q
 //   out[d, column]           = sum_j V[j, d] p[column, j]              A = V, which the pages hold by channel, B = p
 // The accumulators of the first product are the B operand of the second as they lie: which position a row of A stands for is free, and
@@ -272,7 +274,7 @@ __device__ __forceinline__ void paged_store_cols(const PagedAttnArgs &a, int row
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
                 paged_store4<HD, PL>(a, row, head, 32 * d + 2 * i + 4 * hh, o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv);
-        if (hh == 0 && a.lse) a.lse[(size_t)row * a.n_q + head] = (m * a.c + __log2f(l)) * 0.69314718055994531f;
+        if (hh == 0 && a.lse) a.lse[(size_t)row * a.n_q + head] = (m + __log2f(l)) * 0.69314718055994531f;
     } else {
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d)
@@ -322,7 +324,7 @@ __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const Page
 #pragma unroll
             for (int i = 0; i < 16; ++i) { sc[i] = sees(i) ? sc[i] : -INFINITY; mx = fmaxf(mx, sc[i]); }
             mx = fmaxf(mx, __shfl_xor(mx, 32, RS_WAVE));
-            const float m_new = fmaxf(m, mx), mc = m_new == -INFINITY ? 0.f : m_new * a.c, alpha = __builtin_amdgcn_exp2f(fmaf(m, a.c, -mc));
+            const float m_new = fmaxf(m, mx * a.c), mc = m_new == -INFINITY ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m - mc);
             m = m_new;
             l *= alpha;
 #pragma unroll
@@ -359,7 +361,7 @@ __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const Page
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
                 paged_store4<HD, PL>(a, (int)at, head, 32 * d + 2 * i + 4 * hh, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
-            if (d == 0 && hh == 0 && a.lse) a.lse[at * a.n_q + head] = (m * a.c + __log2f(l)) * 0.69314718055994531f;
+            if (d == 0 && hh == 0 && a.lse) a.lse[at * a.n_q + head] = (m + __log2f(l)) * 0.69314718055994531f;
         }
     }
 }
@@ -560,8 +562,8 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
             }
             mx = fmaxf(mx, __shfl_xor(mx, 16, RS_WAVE));
             mx = fmaxf(mx, __shfl_xor(mx, 32, RS_WAVE));
-            const float m_new = fmaxf(m[nb], mx), mc = m_new == -INFINITY ? 0.f : m_new * a.c;
-            const float alpha = __builtin_amdgcn_exp2f(fmaf(m[nb], a.c, -mc));                // (no score so far: 0)
+            const float m_new = fmaxf(m[nb], mx * a.c), mc = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m[nb] - mc);                           // (no score so far: 0)
             m[nb] = m_new;
             float sum = 0.f;
 #pragma unroll
@@ -620,7 +622,7 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
                 }
                 if (hq == 0) {
                     if (!whole) { a.part_ml[(size_t)part * 2 * COLS + c] = m[nb]; a.part_ml[((size_t)part * 2 + 1) * COLS + c] = l[nb]; }
-                    else if (a.lse) a.lse[row * a.n_q + h] = (m[nb] * a.c + __log2f(l[nb])) * 0.69314718055994531f;
+                    else if (a.lse) a.lse[row * a.n_q + h] = (m[nb] + __log2f(l[nb])) * 0.69314718055994531f;
                 }
             }
             const bool nan = __any(poison != poison);
@@ -744,10 +746,10 @@ __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnAr
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[rb][i]);
-            mx = paged_max_halves(mx);
+            mx = paged_max_halves(mx) * a.c;
             // the maximum that p is relative to may lag behind by 2^8: the sums have room, and most tiles rescale nothing
-            if (__any((mx - m) * a.c > 8.f || (m == -INFINITY && mx > -INFINITY))) {
-                const float m_new = fmaxf(m, mx), alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * a.c);
+            if (__any(mx - m > 8.f)) {                     // (no score so far: the difference is infinite, or no number where this tile has none either)
+                const float m_new = fmaxf(m, mx), alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
                 m = m_new;
                 l *= alpha;
 #pragma unroll
@@ -755,7 +757,7 @@ __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnAr
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
             }
-            const float mc = m == -INFINITY ? 0.f : m * a.c;
+            const float mc = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -897,11 +899,11 @@ __global__ void __launch_bounds__(256, 3) k_paged_join(PagedAttnArgs a) {
                 float top = M;
 #pragma unroll
                 for (int k = 0; k < BATCH; ++k) top = fmaxf(top, m[k]);
-                const float tc = top == -INFINITY ? 0.f : top * a.c, e0 = __builtin_amdgcn_exp2f(fmaf(M, a.c, -tc));
+                const float tc = top == -INFINITY ? 0.f : top, e0 = __builtin_amdgcn_exp2f(M - tc);
                 M = top; L *= e0; x[0] *= e0; x[1] *= e0; x[2] *= e0; x[3] *= e0;
 #pragma unroll
                 for (int k = 0; k < BATCH; ++k) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(m[k], a.c, -tc));
+                    const float e = __builtin_amdgcn_exp2f(m[k] - tc);
                     L = fmaf(l[k], e, L);
                     x[0] = fmaf(y[k].x, e, x[0]); x[1] = fmaf(y[k].y, e, x[1]); x[2] = fmaf(y[k].z, e, x[2]); x[3] = fmaf(y[k].w, e, x[3]);
                 }
@@ -914,11 +916,11 @@ __global__ void __launch_bounds__(256, 3) k_paged_join(PagedAttnArgs a) {
             float top = -INFINITY;
 #pragma unroll
             for (int k = 0; k < G; ++k) top = fmaxf(top, o_sh[k][lc][HD]);
-            const float tc = top == -INFINITY ? 0.f : top * a.c;
+            const float tc = top == -INFINITY ? 0.f : top;
             M = top; L = 0.f; x[0] = x[1] = x[2] = x[3] = 0.f;
 #pragma unroll
             for (int k = 0; k < G; ++k) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(o_sh[k][lc][HD], a.c, -tc));
+                const float e = __builtin_amdgcn_exp2f(o_sh[k][lc][HD] - tc);
                 const float4 y = *reinterpret_cast<const float4 *>(&o_sh[k][lc][d]);
                 L = fmaf(o_sh[k][lc][HD + 1], e, L);
                 x[0] = fmaf(y.x, e, x[0]); x[1] = fmaf(y.y, e, x[1]); x[2] = fmaf(y.z, e, x[2]); x[3] = fmaf(y.w, e, x[3]);
@@ -930,7 +932,7 @@ __global__ void __launch_bounds__(256, 3) k_paged_join(PagedAttnArgs a) {
             const float inv = 1.f / L, all = (x[0] + x[1]) + (x[2] + x[3]);
             nan = all != all;
             paged_store4<HD, PL>(a, (int)row, h, d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-            if (d == 0 && a.lse) a.lse[row * a.n_q + h] = ((M == -INFINITY ? 0.f : M * a.c) + __log2f(L)) * 0.69314718055994531f;
+            if (d == 0 && a.lse) a.lse[row * a.n_q + h] = ((M == -INFINITY ? 0.f : M) + __log2f(L)) * 0.69314718055994531f;
         }
         if (__syncthreads_or(nan)) {
             const int c0 = (from & ~31) + 32 * wave;
