@@ -286,7 +286,8 @@ __device__ __forceinline__ void paged_store_cols(const PagedAttnArgs &a, int row
 }
 
 // Columns c_from .. c_to - 1 of c0 .. c0 + 31 of an item, by one wave, for items whose sums hold a NaN: V's
-// infinities and NaN stay out of the products and reach the columns that see them by being counted.  Operands come straight from the pages, 32
+// infinities and NaN stay out of the products and reach the columns that see them by being counted, at the end: a sum that had one would be multiplied by the 0 that a much
+// higher score makes of the factor, which is a NaN.  Operands come straight from the pages, 32
 // channels of the result at a time: few registers, so that the kernel it is part of starts fast when there is nothing of the kind.
 template <int HD, int PL>
 __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const PagedItem &it, int c0, int c_from, int c_to) {
@@ -303,6 +304,7 @@ __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const Page
     for (int d = 0; d < HD / 32; ++d) {
         float m = -INFINITY, l = 0.f;
         f32x16_t o;
+        unsigned int plus = 0, minus = 0, nan = 0;             // bit i: channel i's column sees one
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[i] = 0.f;
 #pragma unroll 1
@@ -348,9 +350,10 @@ __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const Page
 #pragma unroll
                     for (int i = 0; i < 16; ++i) n[i] = 0.f;
                     n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kind == 1 ? paged_pick<1>(v) : kind == 2 ? paged_pick<2>(v) : paged_pick<3>(v), sb[0], n, 0, 0, 0);
-                    const float special = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : __uint_as_float(0x7fc00000u);
+                    unsigned int hit = 0;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[i] += n[i] > 0.f ? special : 0.f;
+                    for (int i = 0; i < 16; ++i) hit |= n[i] > 0.f ? 1u << i : 0u;
+                    (kind == 1 ? plus : kind == 2 ? minus : nan) |= hit;
                 }
             }
         }
@@ -359,8 +362,11 @@ __device__ __forceinline__ void paged_careful(const PagedAttnArgs &a, const Page
             const size_t at = (size_t)(it.s.first + r0 + row);
             const float inv = 1.f / l;
 #pragma unroll
+            for (int i = 0; i < 16; ++i)
+                o[i] = o[i] * inv + (plus >> i & 1 ? INFINITY : 0.f) + (minus >> i & 1 ? -INFINITY : 0.f) + (nan >> i & 1 ? __uint_as_float(0x7fc00000u) : 0.f);
+#pragma unroll
             for (int i = 0; i < 16; i += 4)
-                paged_store4<HD, PL>(a, (int)at, head, 32 * d + 2 * i + 4 * hh, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+                paged_store4<HD, PL>(a, (int)at, head, 32 * d + 2 * i + 4 * hh, o[i], o[i + 1], o[i + 2], o[i + 3]);
             if (d == 0 && hh == 0 && a.lse) a.lse[at * a.n_q + head] = (m + __log2f(l)) * 0.69314718055994531f;
         }
     }
