@@ -266,12 +266,13 @@ _INT_TYPES = (torch.int32, torch.uint32)
 
 
 def _rows(name: str, t: torch.Tensor, device: int):
-    """(address, row stride) of a tensor [rows, heads, channels] whose heads lie back to back; the C side checks the rest."""
-    if t.dim() != 3 or not t.is_contiguous() and (t.stride(2) != 1 or t.stride(1) != t.shape[2]):
+    """(address, row stride) of a tensor [rows, heads, channels] whose heads lie back to back; the C side checks the rest.
+    (The stride of a dimension of one element says nothing: a single row's is its length.)"""
+    if t.dim() != 3 or not t.is_contiguous() and (t.stride(2) != 1 or t.stride(1) != t.shape[2] and t.shape[1] != 1):
         raise ValueError(f"{name} must be [rows, heads, head_dim] with the heads of a row back to back, not {tuple(t.shape)} with strides {t.stride()}")
     if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, the call's other tensors on {_device_name(device)}")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), t.stride(0) if t.shape[0] != 1 else t.shape[1] * t.shape[2]
 
 
 def _ints(name: str, t: Optional[torch.Tensor], n: int, device: int) -> Optional[int]:
@@ -354,7 +355,7 @@ def _paged_rows(name: str, t: torch.Tensor, cache: PagedCache, n_rows: int, head
         if rows >= n_rows and h == heads and hd == cache.head_dim:
             stride = t.stride()
             if stride[2] == 1 and stride[1] == hd:
-                return t.data_ptr(), stride[0]
+                return t.data_ptr(), stride[0] if rows != 1 else h * hd
     if t.dtype != dtype or t.dim() != 3 or t.shape[0] < n_rows or t.shape[1] != heads or t.shape[2] != cache.head_dim:
         raise ValueError(f"{name} must be {dtype} and at least [{n_rows}, {heads}, {cache.head_dim}], not {t.dtype} {tuple(t.shape)}")
     return _rows(name, t, cache.device)
