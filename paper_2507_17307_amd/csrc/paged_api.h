@@ -44,8 +44,8 @@ rs_status rs_rope_rows(const rs_rope *rope, int32_t n_rows, const int32_t *d_pos
     RopeRowsArgs a{};
     a.x = d_x; a.out = d_out; a.x_stride = x_stride; a.out_stride = out_stride; a.pos = d_pos; a.inv_freq = rope->d_inv_freq; a.amplitude = rope->amplitude;
     a.n_rows = n_rows; a.n_heads = n_heads; a.head_dim = head_dim; a.half = rope->rot_dim / 2; a.interleaved = rope->interleaved; a.inverse = inverse;
-    a.rows_wg = n_rows >= 2048 ? 4 : 1; a.heads_wg = n_heads;
-    const dim3 grid((n_rows + a.rows_wg - 1) / a.rows_wg, (n_heads + a.heads_wg - 1) / a.heads_wg);
+    a.rows_wg = n_rows >= 2048 ? 4 : 1;
+    const dim3 grid((n_rows + a.rows_wg - 1) / a.rows_wg);
     const size_t lds = (size_t)a.rows_wg * a.half * 8;
     hipStream_t st = (hipStream_t)stream;
     if (dtype == RS_F32) hipLaunchKernelGGL((k_rope_rows<float, 4>), grid, dim3(256), lds, st, a);
@@ -80,9 +80,9 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
     // eight q and k heads a workgroup, which share the sines and cosines of its rows, or fewer where that leaves under 512 workgroups (us, 128 rows of one
     // position 6.2 with eight heads each, 9.0 with four; chunks of 8192 rows 47 with eight, 50 with six; 517 rows in 26 blocks 24 with eight, 12 with two)
     const int heads = n_q_heads + cache->n_kv_heads, split = (512 + blocks - 1) / blocks, each = (heads + split - 1) / split;
-    a.heads_wg = each < 8 ? each : 8; a.v_heads_wg = 1;
+    a.heads_wg = each < 8 ? each : 8;
     a.rope_wgs = (heads + a.heads_wg - 1) / a.heads_wg;
-    const dim3 grid(blocks, a.rope_wgs + (cache->n_kv_heads + a.v_heads_wg - 1) / a.v_heads_wg);
+    const dim3 grid(blocks, a.rope_wgs + cache->n_kv_heads);
     const size_t lds = append_lds_bytes(a.half, hd);
     hipStream_t st = (hipStream_t)stream;
     if (dtype == RS_F32) hipLaunchKernelGGL((k_paged_append<float, 4>), grid, dim3(256), lds, st, a);

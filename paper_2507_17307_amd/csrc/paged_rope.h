@@ -129,10 +129,10 @@ __device__ __forceinline__ void rope_walk(int rows, int heads, int units, F f) {
 struct RopeRowsArgs {
     const void *x; void *out; size_t x_stride, out_stride;
     const int *pos; const double *inv_freq; float amplitude;
-    int n_rows, n_heads, head_dim, half, interleaved, inverse, rows_wg, heads_wg;
+    int n_rows, n_heads, head_dim, half, interleaved, inverse, rows_wg;
 };
 
-// grid (row blocks, head blocks), LDS rows_wg * half float2.  A workgroup has all heads of its rows, so that an angle is computed once.
+// grid row blocks, LDS rows_wg * half float2.  A workgroup has all heads of its rows, so that an angle is computed once.
 // Bound by bytes: 16384 bf16 rows of 40 heads of 128 (336 MB read and written) 65 us, 5.2 TB/s, as a large copy (5.1); 128 fp32 rows of 28 heads 3.4 us,
 // of which 1.7 are a launch.
 template <typename T, int VEC>
@@ -140,7 +140,6 @@ __global__ void __launch_bounds__(256) k_rope_rows(RopeRowsArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     float2 *turns = reinterpret_cast<float2 *>(smem);
     const int tid = threadIdx.x, r0 = blockIdx.x * a.rows_wg, n = min(a.rows_wg, a.n_rows - r0);
-    const int h0 = blockIdx.y * a.heads_wg, nh = min(a.heads_wg, a.n_heads - h0);
     for (int i = tid; i < n * a.half; i += 256) {
         const int r = i / a.half;
         float2 t = rope_turn(a.pos[r0 + r], a.inv_freq[i - r * a.half], a.amplitude);
@@ -148,9 +147,9 @@ __global__ void __launch_bounds__(256) k_rope_rows(RopeRowsArgs a) {
         turns[i] = t;
     }
     __syncthreads();
-    rope_walk(n, nh, rope_units<VEC>(a.half, a.head_dim), [&](int r, int h, int u) __attribute__((always_inline)) {
-        const T *x = (const T *)a.x + (size_t)(r0 + r) * a.x_stride + (size_t)(h0 + h) * a.head_dim;
-        T *y = (T *)a.out + (size_t)(r0 + r) * a.out_stride + (size_t)(h0 + h) * a.head_dim;
+    rope_walk(n, a.n_heads, rope_units<VEC>(a.half, a.head_dim), [&](int r, int h, int u) __attribute__((always_inline)) {
+        const T *x = (const T *)a.x + (size_t)(r0 + r) * a.x_stride + (size_t)h * a.head_dim;
+        T *y = (T *)a.out + (size_t)(r0 + r) * a.out_stride + (size_t)h * a.head_dim;
         rope_unit<T, T, VEC>(x, y, u, a.half, a.interleaved, turns + r * a.half);
     });
 }
@@ -162,7 +161,7 @@ struct AppendArgs {
     const void *q, *k, *v; void *q_out;
     size_t q_stride, k_stride, v_stride, q_out_stride;
     const double *inv_freq; float amplitude;
-    int n_q, head_dim, half, interleaved, heads_wg, rope_wgs, v_heads_wg;
+    int n_q, head_dim, half, interleaved, heads_wg, rope_wgs;
 };
 
 constexpr int APPEND_V_PITCH = 2;                                  // spare values of a row of V in LDS
@@ -171,7 +170,7 @@ __host__ __device__ __forceinline__ size_t append_lds_bytes(int half, int head_d
     return turns > v ? turns : v;
 }
 
-// grid (blocks of positions, at most; rope_wgs blocks of q and k heads and then those of V heads).  A block is 64 aligned positions of one sequence, so that V,
+// grid (blocks of positions, at most; rope_wgs blocks of q and k heads and then a V head each).  A block is 64 aligned positions of one sequence, so that V,
 // which turns from rows into channels in LDS, is written in pieces of 16 bytes and a channel's 128 bytes lie side by side; q and k pass through
 // registers.  Bound by bytes: chunks of 8192 bf16 rows of 40 + 8 + 8 heads (235 MB) 47 us, 5.0 TB/s, as a large copy; single calls by their launch and the
 // search for the block: one fp32 row 4.8 us, 128 sequences of one bf16 row 6.0, 517 fp32 rows of nine sequences 11.2.
@@ -245,30 +244,27 @@ __global__ void __launch_bounds__(256) k_paged_append(AppendArgs a) {
     }
     // ---- V: a head's rows go to LDS and come back by channel
     uint16_t *tile = reinterpret_cast<uint16_t *>(smem);
-    const int pitch = a.head_dim + APPEND_V_PITCH, h0 = (blockIdx.y - a.rope_wgs) * a.v_heads_wg, h1 = min(h0 + a.v_heads_wg, a.s.n_kv), pieces = a.head_dim / 8;
-    for (int h = h0; h < h1; ++h) {
-        __syncthreads();
-        for (int i = tid; i < rows * pieces; i += 256) {
-            const int r = i / pieces, c = 8 * (i - r * pieces);
-            float x[8];
-            RowVec<T, 8>::load((const T *)a.v + (size_t)(r0 + r) * a.v_stride + (size_t)h * a.head_dim + c, x);
-            uint32_t *t = reinterpret_cast<uint32_t *>(tile + (size_t)(lo - base + r) * pitch + c);
+    const int pitch = a.head_dim + APPEND_V_PITCH, h = blockIdx.y - a.rope_wgs, pieces = a.head_dim / 8;
+    for (int i = tid; i < rows * pieces; i += 256) {
+        const int r = i / pieces, c = 8 * (i - r * pieces);
+        float x[8];
+        RowVec<T, 8>::load((const T *)a.v + (size_t)(r0 + r) * a.v_stride + (size_t)h * a.head_dim + c, x);
+        uint32_t *t = reinterpret_cast<uint32_t *>(tile + (size_t)(lo - base + r) * pitch + c);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) t[k] = pack_bf16x2(x[2 * k], x[2 * k + 1]);
-        }
-        __syncthreads();
-        for (int i = tid; i < a.head_dim * (APPEND_BLOCK / 8); i += 256) {
-            const int c = i / (APPEND_BLOCK / 8), o = 8 * (i % (APPEND_BLOCK / 8)), page = page_of[min(max(o, lo - base), hi - 1 - base)];
-            if (page < 0 || base + o + 8 <= lo || base + o >= hi) continue;            // (eight places are one page's)
-            uint16_t *y = a.vc + ((((size_t)page * a.s.n_kv + h) * a.head_dim + c) << a.s.page_shift) + ((base + o) & (ps - 1));
-            if (base + o >= lo && base + o + 8 <= hi) {
-                uint32_t w[4];
+        for (int k = 0; k < 4; ++k) t[k] = pack_bf16x2(x[2 * k], x[2 * k + 1]);
+    }
+    __syncthreads();
+    for (int i = tid; i < a.head_dim * (APPEND_BLOCK / 8); i += 256) {
+        const int c = i / (APPEND_BLOCK / 8), o = 8 * (i % (APPEND_BLOCK / 8)), page = page_of[min(max(o, lo - base), hi - 1 - base)];
+        if (page < 0 || base + o + 8 <= lo || base + o >= hi) continue;                // (eight places are one page's)
+        uint16_t *y = a.vc + ((((size_t)page * a.s.n_kv + h) * a.head_dim + c) << a.s.page_shift) + ((base + o) & (ps - 1));
+        if (base + o >= lo && base + o + 8 <= hi) {
+            uint32_t w[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = tile[(size_t)(o + 2 * k) * pitch + c] | (uint32_t)tile[(size_t)(o + 2 * k + 1) * pitch + c] << 16;
-                *reinterpret_cast<uint4 *>(y) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-                for (int k = max(0, lo - base - o); k < min(8, hi - base - o); ++k) y[k] = tile[(size_t)(o + k) * pitch + c];
-            }
+            for (int k = 0; k < 4; ++k) w[k] = tile[(size_t)(o + 2 * k) * pitch + c] | (uint32_t)tile[(size_t)(o + 2 * k + 1) * pitch + c] << 16;
+            *reinterpret_cast<uint4 *>(y) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            for (int k = max(0, lo - base - o); k < min(8, hi - base - o); ++k) y[k] = tile[(size_t)(o + k) * pitch + c];
         }
     }
 }
