@@ -469,6 +469,7 @@ rs_status rs_paged_append(const rs_paged_kv *cache, int32_t n_seqs, int32_t n_ro
  *                     whose page is no page of the cache is computed with some other page in its place
  *   d_scratch         DEVICE, 256-byte aligned, of at least rs_paged_attention_scratch_bytes (0 on a bad argument) for these
  *                     counts; any content.  Calls and graph replays that overlap must not share it
+ * Sums of probabilities times V are fp32 before they are divided: |V| times the positions that a row sees has to stay below 2^119.
  * What lies in the pages at positions that no row sees may be anything, NaN too, and what one row sees does not reach another: an infinity or
  * a NaN in V at a position that only some rows of a span see is theirs alone (spans with such values take several times as long).
  * Errors: RS_EINVAL, RS_ECAPACITY (n_seqs > 1024, n_rows > 2^22), RS_EHIP. */

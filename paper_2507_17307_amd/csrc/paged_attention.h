@@ -29,8 +29,10 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int PAGED_COLS = 128;                // columns of a workgroup of k_paged_wide
 constexpr int PAGED_TILE = 6;                  // log2 positions of a tile
-constexpr int PAGED_WIDE_RUNS = 512, PAGED_WIDE_RUNS3 = 256, PAGED_NARROW_RUNS = 1024;      // of a call, at most: what the CUs hold at a time (RUNS3: with three planes).
-// Head sizes 32 and 64 leave room for more wide ones, which lose: 64 bf16 tokens, 8 KV heads of 64, 4000 positions, 512 / 768 / 1024: 102 / 125 / 111 us.
+// Runs of a call, at most: as many as the CUs hold at a time with head size 128, where a SIMD's 512 registers are two waves of k_paged_wide with one plane of q (252 each), or one
+// with three (390; RUNS3), or one of k_paged_narrow.  Smaller head sizes leave room for more wide ones: bf16, 64 tokens, 4000 positions, 8 KV heads, 512 / 768 / 1024 runs: 101 /
+// 130 / 111 us with 64 channels, 73 / 62 / 80 with 32; 701 rows of 33 spans, 64 channels, behind a window 30 / 35 / 38.
+constexpr int PAGED_WIDE_RUNS = 512, PAGED_WIDE_RUNS3 = 256, PAGED_NARROW_RUNS = 1024;
 
 struct PagedAttnArgs {
     PagedSpans s;
@@ -651,10 +653,10 @@ __global__ void __launch_bounds__(64, 1) k_paged_narrow(PagedAttnArgs a) {
 // the tile that its count of tiles so far gives, modulo the item's, and goes round.  Begun at the first tile each, runs were spread over the whole context
 // and 11 % of the requests met in L2: 8.7 GB at 6 TB/s from beyond it for the four chunks of 2048 rows on up to 14000 positions.  Now 62 % do, which is 2 % of the time
 // (1243 -> 1219 us).
-// Those chunks (40 bf16 heads of 128 on 8, 1.09 TFLOP): 1210 us, 900 TFLOP/s, 73 % of the rate of a large bf16 product (1226); products and exponentials take turns
+// Those chunks (40 bf16 heads of 128 on 8, 1.09 TFLOP): 1196 to 1246 us, 870 to 910 TFLOP/s, 73 % of the rate of a large bf16 product (1226); products and exponentials take turns
 // in a wave and two waves a SIMD fill each other's gaps.  With the scores of the next tile computed beside this one's exponentials the registers leave one
-// wave a SIMD, 2040 us, or spill, 3680.  128 bf16 tokens of 28 heads on 4, 512 .. 4607 positions each (707 MB): 132 us, 5.4 TB/s.  61 fp32 rows, three planes, one wave a
-// SIMD: 60 us.  701 bf16 rows of 33 sequences, head size 64, window 1000: 20 us.
+// wave a SIMD, 2040 us, or spill, 3680.  128 bf16 tokens of 28 heads on 4, 512 .. 4607 positions each (707 MB): 137 us, 5.2 TB/s.  61 fp32 rows, three planes, one wave a
+// SIMD: 60 us (its launch bound is one wave at every head size; of 32 and 64 channels two would fit).  701 bf16 rows of 33 sequences, head size 64, window 1000: 20 us.
 // ------------------------------------------------------------------------------------------------
 template <int HD, int PL>
 __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnArgs a) {
@@ -753,7 +755,7 @@ __global__ void __launch_bounds__(256, PL == 1 ? 2 : 1) k_paged_wide(PagedAttnAr
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[rb][i]);
             mx = paged_max_halves(mx) * a.c;
-            // the maximum that p is relative to may lag behind by 2^8: the sums have room, and most tiles rescale nothing
+            // the maximum that p is relative to may lag behind by 2^8, and most tiles rescale nothing: l has room, o while |V| times the positions is below 2^119
             if (__any(mx - m > 8.f)) {                     // (no score so far: the difference is infinite, or no number where this tile has none either)
                 const float m_new = fmaxf(m, mx), alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
                 m = m_new;

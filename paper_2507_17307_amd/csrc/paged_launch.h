@@ -58,15 +58,17 @@ PagedSpans paged_spans(const rs_paged_kv *c, int32_t n_seqs, int32_t n_rows, con
 }
 
 // Which kernel takes a call, by the columns that a span brings on average (rows times query heads of a KV head) and by how many pairs of a sequence and a
-// KV head there are to share the CUs.  us a call in a graph, contexts of 4000 positions, blocks of 16 / 32 / 128 columns:
-//   fp32  28 query heads on 4, rows of each sequence 1 / 3 / 6 / 12:   1 sequence    15 18 21 30 / 18 19 23 28 / 22 25 26 31
-//                                                                   16 sequences   45 66 88 130 / 52 70 92 113 / 57 59 63 69
-//                                                                   64 sequences   117 181 313 477 / 122 138 220 335 / 174 179 184 200
-//   bf16  the same                                                   1 sequence    14 17 19 26 / 15 17 20 25 / 19 20 22 27
-//                                                                    8 sequences (8 rows at last)   31 43 - 56 / 35 52 - 64 / 27 32 - 42
-//                                                                   64 sequences   113 174 301 484 / 114 128 190 320 / 106 109 117 126
-// so that blocks grow with the columns, few pairs stay with narrow blocks longer, and with one plane of q and many pairs the wide kernel, in which
-// four waves fetch, is the fastest for single rows too.
+// KV head there are to share the CUs.  us a call in a graph, 28 query heads on 4, contexts of 4000 positions, blocks of 16 / 32 / 128 columns, rows of each
+// sequence 1, 3, 6, 8, 12 (7 to 84 columns):
+//   fp32   1 sequence     15  18  24  26  30 /  18  23  28  31  38 /  20  21  23  24  27
+//         16 sequences    41  52  80 100 140 /  47  54  68  82 103 /  55  57  58  60  69
+//         64 sequences   113 156 299 348 490 / 118 135 199 263 360 / 179 181 182 183 193
+//   bf16   1 sequence     14  17  22  25  30 /  15  20  25  28  35 /  19  19  20  21  24
+//          8 sequences    32  37  50  57  80 /  34  40  45  50  59 /  25  27  29  29  35
+//         64 sequences   112 158 295 355 501 / 113 124 177 252 328 / 103 111 116 118 131
+// From 32 pairs on the rule takes the least of a line's three or is within 4 % of it: blocks grow with the columns, and with one plane of q the wide kernel, in which
+// four waves fetch, is the fastest for single rows too.  Below, 16 columns are right for single rows and 128 for more than 64 columns, but between them the rule is too
+// slow by up to 35 %: it takes 32 columns for 17 to 64, where 16 (up to 21 here) or 128 (from 42 on) are the least.
 int paged_cols(int n_seqs, int n_rows, int group, int n_kv, int dtype) {
     const long long cols = ((long long)n_rows * group + n_seqs - 1) / n_seqs;
     const bool few = (long long)n_seqs * n_kv < 32;
