@@ -75,6 +75,7 @@ typedef int32_t rs_status;
                                   the record is invalid and the model refuses further steps          */
 #define RS_FLAG_ROUTER_STAY 64u /* R-Stitch+: HI on the small model, but the learned router chose to
                                   stay: ACCEPT is set and NEXT_LLM cleared (rs_route_plus)            */
+#define RS_FLAG_NO_PAGE  128u  /* rs_pages_reserve, rs_pages_fork: fewer pages are free than the call needs */
 
 /* Shape rules (rs_workspace_bytes / rs_kv_bytes return 0 and rs_create_model returns
  * RS_EINVAL when one is violated; rs_last_error names it):
@@ -502,6 +503,116 @@ size_t    rs_paged_workspace_bytes(const rs_config *cfg, const rs_paged_kv *cach
 rs_status rs_create_model_paged(const rs_config *cfg, const rs_weights *weights,
                                 const rs_paged_kv *cache, void *workspace,
                                 size_t workspace_bytes, rs_model **out);
+
+/* ---------------------------------------------------------------------------
+ * Beam search on a model whose cache is in pages: the best continuations of several
+ * beams, and a pool of pages that sequences share.  A step is rs_decode_step with
+ * logits, rs_beam_select, rs_pages_fork (every beam takes over its parent's state) and
+ * rs_pages_reserve for the next position; the host reads nothing between them.
+ * Drawing several replies from one prompt, taking drafted tokens back and evicting
+ * positions behind a window use the same pool.
+ *
+ * rs_beam_select: of each group's n_beams beams and all tokens, the n_out best
+ * continuations, in order.  Row r = group * n_beams + beam of the logits belongs to one
+ * beam.  Token t continues it to the score d_score[r] + (x[t] - ln sum exp x), x =
+ * d_logit_scale[r] * logits; a logit of -inf is no candidate.  A beam whose last token is
+ * eos has ended: its logits are not read, it is its own only candidate, with token
+ * eos and its score and length unchanged.
+ *   d_logits        DEVICE [n_groups * n_beams][vocab], dtype RS_F32 or RS_BF16, rows row_stride elements apart
+ *   n_beams, n_out  1 .. 64;  n_groups * n_beams <= 65535
+ *   d_logit_scale   DEVICE fp32 [rows] or NULL (= 1): > 0 and finite
+ *   d_score         DEVICE fp32 [rows]: sum of log probabilities; -inf: the beam is not there (its logits are not read)
+ *   d_last          DEVICE int32 [rows] or NULL: the beams' last tokens;  eos: a token or -1 (no beam ends)
+ *   length_penalty  >= 0: candidates are ordered by score / length^length_penalty, length at least 1
+ *   d_len           DEVICE int32 [rows] or NULL (with length_penalty 0): tokens of the beams so far, >= 0; a continuation has one more
+ *   d_parent        DEVICE int32 [n_groups * n_out]: the candidate's beam, 0 .. n_beams - 1
+ *   d_token, d_score_out, d_len_out (or NULL)  its token, score (not divided) and length
+ *   d_flags         DEVICE uint32 [rows] or NULL: RS_FLAG_NONFINITE is or-ed in where a logit is NaN or +inf,
+ *                   RS_FLAG_BADARG where a score is NaN or +inf, a length negative or a scale not positive and finite; such rows
+ *                   have no candidates (the caller clears the words)
+ *   d_scratch       DEVICE, 256-byte aligned, of at least rs_beam_select_scratch_bytes (0 on a bad argument); any content.  Calls and
+ *                   graph replays that overlap must not share it
+ * Fewer candidates than n_out: the rest have parent -1, token -1, score -inf and length 0.  Equals (in double, in which sums are held
+ * and candidates compared) go to the lower beam, within a beam to the larger logit and then to the lower token.
+ * With n_out == n_beams outputs may be the inputs of the same kind (d_score_out = d_score, d_token = d_last, d_len_out = d_len).
+ * Errors: RS_EINVAL, RS_ECAPACITY (more than 65535 rows), RS_EHIP. */
+size_t    rs_beam_select_scratch_bytes(int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t n_out);
+rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype,
+                         int32_t n_groups, int32_t n_beams, int32_t vocab,
+                         const float *d_logit_scale, const float *d_score, const int32_t *d_last, int32_t eos,
+                         double length_penalty, const int32_t *d_len, int32_t n_out,
+                         int32_t *d_parent, int32_t *d_token, float *d_score_out, int32_t *d_len_out,
+                         uint32_t *d_flags, void *d_scratch, size_t scratch_bytes, void *stream);
+
+/* Pages that several sequences hold together: the pages of all layers as in
+ * rs_create_model_paged, the page table, and how many table entries name each page (0: free).  An
+ * entry outside 0 .. n_pages - 1 names none.  Calls that need pages take the free ones of
+ * the lowest indices, in order, so that a pool's state depends on its calls alone.
+ * Calls on one pool (and on caches over its pages) must be ordered; nothing reads the pool on the host. */
+typedef struct rs_page_pool {
+    void    *k;                  /* DEVICE bf16 [n_layers][n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned, or NULL      */
+    void    *v;                  /* DEVICE bf16 [n_layers][n_pages][n_kv_heads][head_dim][page_size], or NULL (reserve and release
+                                    do not look at k, v, n_layers, n_kv_heads and head_dim)       */
+    int32_t *page_table;         /* DEVICE int32 [n_slots][max_pages]                         */
+    int32_t *page_ref;           /* DEVICE int32 [n_pages]                                    */
+    int32_t n_layers;            /* 1 .. 65536                                                */
+    int32_t n_pages;             /* 1 .. 2^30                                                 */
+    int32_t page_size;           /* a power of two, 16 .. 1024                                */
+    int32_t n_slots;             /* >= 1                                                      */
+    int32_t max_pages;           /* >= 1; page_size * max_pages <= 2^30, n_slots * max_pages < 2^31 */
+    int32_t n_kv_heads;          /* 1 .. 1024                                                 */
+    int32_t head_dim;            /* 32, 64 or 128                                             */
+} rs_page_pool;
+
+/* DEVICE scratch of the calls below, 256-byte aligned, for n rows (n_groups * n_beams; 1 for rs_pages_compact); 0 on a bad
+ * argument.  Any content.  Calls and graph replays that overlap must not share it. */
+size_t    rs_pages_scratch_bytes(const rs_page_pool *pool, int32_t n);
+
+/* Pages for the positions d_from[r] .. d_to[r] - 1 of slot d_slot[r]: entries of the slot's row that some of them lie in and that name no page get one.
+ *   n        1 .. 1024 rows;  d_slot, d_from, d_to  DEVICE int32 [n], d_from may be NULL (= 0); 0 <= from <= to <= page_size * max_pages
+ *   d_flags  DEVICE uint32 [n] or NULL (the caller clears the words).  RS_FLAG_BADARG: the row is out of range, or a row before it has the same
+ *            slot; it is skipped.  RS_FLAG_NO_PAGE: the pages that this row and all before it lack are more than there are;
+ *            the row gets none
+ * Errors: RS_EINVAL, RS_ECAPACITY (n > 1024), RS_EHIP. */
+rs_status rs_pages_reserve(const rs_page_pool *pool, int32_t n, const int32_t *d_slot, const int32_t *d_from, const int32_t *d_to,
+                           uint32_t *d_flags, void *d_scratch, size_t scratch_bytes, void *stream);
+
+/* The other way round: entries all of whose positions lie in d_from[r] .. d_to[r] - 1 name no page any more (-1), and a
+ * page that no entry names is free.  From the number of positions to keep up to page_size * max_pages it takes
+ * tokens back, from 0 it frees what has left a window, or a sequence.  Rows as in rs_pages_reserve. */
+rs_status rs_pages_release(const rs_page_pool *pool, int32_t n, const int32_t *d_slot, const int32_t *d_from, const int32_t *d_to,
+                           uint32_t *d_flags, void *stream);
+
+/* Every row takes over the state of a row of its group: slot d_slot[r] holds the d_pos[q] first positions that slot d_slot[q] held
+ * before the call, q = group * n_beams + d_parent[r]; with d_parent[r] < 0 it holds none.
+ * What the slot held before goes, pages past the positions kept among it.  Whole pages are shared.  A last page
+ * in part filled stays with the first row that takes it if no other entry names it then, and is copied to a free page for every
+ * other, in all layers, by whole blocks of 8 positions (the places behind them keep what was there).  So
+ * the positions that follow can be written by every row for itself; with d_parent[r] = r's own beam throughout, a call makes the last pages of
+ * sequences their own.
+ *   n_groups, n_beams  n_groups * n_beams <= 1024 rows
+ *   d_slot, d_parent, d_pos  DEVICE int32 [rows]; slots distinct; parents below n_beams; 0 <= positions <= page_size * max_pages
+ *   d_pos_out          DEVICE int32 [rows] or NULL: the positions that each row holds now (may be d_pos)
+ *   d_flags            DEVICE uint32 [rows] or NULL (the caller clears the words): RS_FLAG_BADARG on rows out of range or
+ *                      whose slot a row before them has, RS_FLAG_NO_PAGE on all rows if the copies need more pages than are
+ *                      free after the call.  With either the call changes nothing else
+ * Errors: RS_EINVAL, RS_ECAPACITY, RS_EHIP. */
+rs_status rs_pages_fork(const rs_page_pool *pool, int32_t n_groups, int32_t n_beams, const int32_t *d_slot, const int32_t *d_parent,
+                        const int32_t *d_pos, int32_t *d_pos_out, uint32_t *d_flags, void *d_scratch, size_t scratch_bytes, void *stream);
+
+/* The contents of page d_src[i] of `from` go to page d_dst[i] of `to`, in all layers (tables and counts are
+ * not looked at).  The pools have the same layers, page size and heads, and may be one; pages named in d_dst must be distinct
+ * and, in one pool, none of d_src unless src = dst.
+ *   d_flags  DEVICE uint32 [n] or NULL: RS_FLAG_BADARG is or-ed in where a page is no page of its pool (the pair is skipped)
+ * Errors: RS_EINVAL, RS_ECAPACITY (n > 2^22), RS_EHIP. */
+rs_status rs_pages_copy(const rs_page_pool *to, const rs_page_pool *from, int32_t n, const int32_t *d_src, const int32_t *d_dst,
+                        uint32_t *d_flags, void *stream);
+
+/* Moves the used pages to the front: with U pages in use, those from U on go, in order, to the free ones below U, in order;
+ * all table entries and the counts follow.  Pages from U on are free afterwards.
+ *   d_used  DEVICE int32: U
+ * Errors: RS_EINVAL, RS_EHIP. */
+rs_status rs_pages_compact(const rs_page_pool *pool, int32_t *d_used, void *d_scratch, size_t scratch_bytes, void *stream);
 
 #ifdef __cplusplus
 }

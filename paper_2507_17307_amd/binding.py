@@ -16,7 +16,7 @@ from typing import List, Optional, Sequence
 import torch
 
 RS_SLM, RS_LLM = 0, 1
-FLAG_HI, FLAG_ACCEPT, FLAG_NEXT_LLM, FLAG_NONFINITE, FLAG_BADARG, FLAG_ABORTED, FLAG_ROUTER_STAY = 1, 2, 4, 8, 16, 32, 64
+FLAG_HI, FLAG_ACCEPT, FLAG_NEXT_LLM, FLAG_NONFINITE, FLAG_BADARG, FLAG_ABORTED, FLAG_ROUTER_STAY, FLAG_NO_PAGE = 1, 2, 4, 8, 16, 32, 64, 128
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -45,6 +45,11 @@ class _RsWeights(C.Structure):
 class _RsPagedKv(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p)] + [(n, C.c_int32) for n in (
         "n_pages", "page_size", "n_slots", "max_pages", "n_kv_heads", "head_dim")]
+
+
+class _RsPagePool(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("page_ref", C.c_void_p)] + [(n, C.c_int32) for n in (
+        "n_layers", "n_pages", "page_size", "n_slots", "max_pages", "n_kv_heads", "head_dim")]
 
 
 class _RsRope(C.Structure):
@@ -107,6 +112,23 @@ def _load() -> C.CDLL:
     lib.rs_paged_workspace_bytes.argtypes = [C.POINTER(RsConfig), C.POINTER(_RsPagedKv)]
     lib.rs_create_model_paged.restype = i32
     lib.rs_create_model_paged.argtypes = [C.POINTER(RsConfig), C.POINTER(_RsWeights), C.POINTER(_RsPagedKv), vp, sz, C.POINTER(vp)]
+    lib.rs_beam_select_scratch_bytes.restype = sz
+    lib.rs_beam_select_scratch_bytes.argtypes = [i32, i32, i32, i32]
+    lib.rs_beam_select.restype = i32
+    lib.rs_beam_select.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp, i32, f64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    pool = C.POINTER(_RsPagePool)
+    lib.rs_pages_scratch_bytes.restype = sz
+    lib.rs_pages_scratch_bytes.argtypes = [pool, i32]
+    lib.rs_pages_reserve.restype = i32
+    lib.rs_pages_reserve.argtypes = [pool, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.rs_pages_release.restype = i32
+    lib.rs_pages_release.argtypes = [pool, i32, vp, vp, vp, vp, vp]
+    lib.rs_pages_fork.restype = i32
+    lib.rs_pages_fork.argtypes = [pool, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.rs_pages_copy.restype = i32
+    lib.rs_pages_copy.argtypes = [pool, pool, i32, vp, vp, vp, vp]
+    lib.rs_pages_compact.restype = i32
+    lib.rs_pages_compact.argtypes = [pool, vp, vp, sz, vp]
     lib.rs_set_spin_limit.restype = i32
     lib.rs_set_spin_limit.argtypes = [vp, C.c_uint32]
     lib.rs_set_phase_timer.restype = i32
@@ -401,6 +423,103 @@ def rs_paged_attention(cache: PagedCache, n_seqs: int, n_rows: int, d_seq_slot, 
                                   _ints("d_span_offset", d_span_offset, n_seqs + 1, dev), _ints("d_pos0", d_pos0, n_seqs, dev), kind, nq, pq, sq,
                                   scale, window, po, so, _ptr(d_lse), _ints("d_flags", d_flags, n_seqs, dev), d_scratch.data_ptr(),
                                   d_scratch.numel() * d_scratch.element_size(), _device_stream(dev, stream)))
+
+
+# ------------------------------------------------------------------ beam search
+def rs_beam_select_scratch_bytes(n_groups: int, n_beams: int, vocab: int, n_out: int) -> int:
+    return lib.rs_beam_select_scratch_bytes(n_groups, n_beams, vocab, n_out)
+
+
+def _floats(name: str, t: Optional[torch.Tensor], n: int, device: int) -> Optional[int]:
+    """Address of n fp32 numbers."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.numel() < n or t.get_device() != device:
+        raise ValueError(f"{name} must hold {n} contiguous fp32 numbers on {_device_name(device)}")
+    return t.data_ptr()
+
+
+def _scratch(t: torch.Tensor, device: int):
+    """(address, bytes)"""
+    if t is None or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"d_scratch must be a contiguous tensor on {_device_name(device)}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def rs_beam_select(d_logits: torch.Tensor, n_groups: int, n_beams: int, d_logit_scale, d_score, d_last, eos: int, length_penalty: float, d_len, n_out: int,
+                   d_parent, d_token, d_score_out, d_len_out, d_scratch, d_flags=None, stream=None) -> None:
+    """d_logits: fp32 or bf16 [rows, vocab] with the values of a row side by side, at least n_groups * n_beams rows; d_score, d_logit_scale (or None): fp32;
+    d_last, d_len (or None): int32 of a row each; d_parent, d_token, d_len_out (or None): int32, d_score_out: fp32 of n_groups * n_out."""
+    dev, rows, n = d_logits.get_device(), n_groups * n_beams, n_groups * n_out
+    if d_logits.dtype not in _ROW_TYPES or d_logits.dim() != 2 or d_logits.shape[0] < rows or d_logits.stride(1) != 1 and d_logits.shape[1] != 1:
+        raise ValueError(f"d_logits must be fp32 or bf16 [{rows}, vocab] with the values of a row side by side, not {d_logits.dtype} {tuple(d_logits.shape)}")
+    vocab = d_logits.shape[1]
+    stride = d_logits.stride(0) if d_logits.shape[0] != 1 else vocab
+    _check(lib.rs_beam_select(d_logits.data_ptr(), stride, _ROW_TYPES[d_logits.dtype], n_groups, n_beams, vocab, _floats("d_logit_scale", d_logit_scale, rows, dev),
+                              _floats("d_score", d_score, rows, dev), _ints("d_last", d_last, rows, dev), eos, length_penalty, _ints("d_len", d_len, rows, dev), n_out,
+                              _ints("d_parent", d_parent, n, dev), _ints("d_token", d_token, n, dev), _floats("d_score_out", d_score_out, n, dev),
+                              _ints("d_len_out", d_len_out, n, dev), _ints("d_flags", d_flags, rows, dev), *_scratch(d_scratch, dev), _device_stream(dev, stream)))
+
+
+class PagePool:
+    """Marshalled rs_page_pool over its tensors, which it keeps alive: page_table int32 [slots, pages], page_ref int32 [pages] and, for the
+    calls that move what is in the pages, k [layers, pages, KV heads, positions, channels] and v [layers, pages, KV heads, channels, positions]
+    bf16; all contiguous on one device."""
+
+    def __init__(self, page_table: torch.Tensor, page_ref: torch.Tensor, page_size: int, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_ref.dtype != torch.int32 or page_ref.dim() != 1:
+            raise ValueError("page_table must be int32 [slots, pages], page_ref int32 [pages]")
+        if (k is None) != (v is None):
+            raise ValueError("give both k and v or neither")
+        tensors = [page_table, page_ref] + ([] if k is None else [k, v])
+        if any(not t.is_contiguous() or t.device != page_table.device for t in tensors):
+            raise ValueError("page_table, page_ref, k and v must be contiguous and on one device")
+        layers = heads = hd = 0
+        if k is not None:
+            if k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 or k.dim() != 5 or k.shape[1] != page_ref.shape[0] or k.shape[3] != page_size \
+                    or v.shape != (k.shape[0], k.shape[1], k.shape[2], k.shape[4], k.shape[3]):
+                raise ValueError("k must be bf16 [layers, pages, KV heads, page_size, channels], v bf16 [layers, pages, KV heads, channels, page_size]")
+            layers, heads, hd = k.shape[0], k.shape[2], k.shape[4]
+        self.page_table, self.page_ref, self.page_size, self.k, self.v, self.device = page_table, page_ref, page_size, k, v, page_table.get_device()
+        self.struct = _RsPagePool(_ptr(k), _ptr(v), page_table.data_ptr(), page_ref.data_ptr(), layers, page_ref.shape[0], page_size, page_table.shape[0],
+                                  page_table.shape[1], heads, hd)
+        self._ref = C.byref(self.struct)
+
+
+def rs_pages_scratch_bytes(pool: PagePool, n: int) -> int:
+    return lib.rs_pages_scratch_bytes(pool._ref, n)
+
+
+def rs_pages_reserve(pool: PagePool, n: int, d_slot, d_from, d_to, d_scratch, d_flags=None, stream=None) -> None:
+    dev = pool.device
+    _check(lib.rs_pages_reserve(pool._ref, n, _ints("d_slot", d_slot, n, dev), _ints("d_from", d_from, n, dev), _ints("d_to", d_to, n, dev),
+                                _ints("d_flags", d_flags, n, dev), *_scratch(d_scratch, dev), _device_stream(dev, stream)))
+
+
+def rs_pages_release(pool: PagePool, n: int, d_slot, d_from, d_to, d_flags=None, stream=None) -> None:
+    dev = pool.device
+    _check(lib.rs_pages_release(pool._ref, n, _ints("d_slot", d_slot, n, dev), _ints("d_from", d_from, n, dev), _ints("d_to", d_to, n, dev),
+                                _ints("d_flags", d_flags, n, dev), _device_stream(dev, stream)))
+
+
+def rs_pages_fork(pool: PagePool, n_groups: int, n_beams: int, d_slot, d_parent, d_pos, d_pos_out, d_scratch, d_flags=None, stream=None) -> None:
+    dev, n = pool.device, n_groups * n_beams
+    _check(lib.rs_pages_fork(pool._ref, n_groups, n_beams, _ints("d_slot", d_slot, n, dev), _ints("d_parent", d_parent, n, dev), _ints("d_pos", d_pos, n, dev),
+                             _ints("d_pos_out", d_pos_out, n, dev), _ints("d_flags", d_flags, n, dev), *_scratch(d_scratch, dev), _device_stream(dev, stream)))
+
+
+def rs_pages_copy(to: PagePool, source: PagePool, n: int, d_src, d_dst, d_flags=None, stream=None) -> None:
+    """Pages d_src of `source` to pages d_dst of `to`."""
+    dev = to.device
+    if source.device != dev:
+        raise ValueError(f"the pools are on {_device_name(source.device)} and {_device_name(dev)}")
+    _check(lib.rs_pages_copy(to._ref, source._ref, n, _ints("d_src", d_src, n, dev), _ints("d_dst", d_dst, n, dev), _ints("d_flags", d_flags, n, dev),
+                             _device_stream(dev, stream)))
+
+
+def rs_pages_compact(pool: PagePool, d_used, d_scratch, stream=None) -> None:
+    dev = pool.device
+    _check(lib.rs_pages_compact(pool._ref, _ints("d_used", d_used, 1, dev), *_scratch(d_scratch, dev), _device_stream(dev, stream)))
 
 
 PHASE_QKV, PHASE_OPROJ, PHASE_GATEUP, PHASE_DOWN, PHASE_LMHEAD, PHASE_ATTN = range(6)

@@ -1333,3 +1333,4 @@ extern "C" rs_status rs_route_static(const float *d_logits, int32_t n, int32_t v
 }
 
 #include "paged_api.h"
+#include "beam_api.h"
