@@ -70,6 +70,17 @@ rs_status launch_copy(const CopyArgs &a, long long moves_most, hipStream_t st) {
     return RS_OK;
 }
 
+constexpr int BEAM_SLOTS = 1024;                                   // workgroups of k_beam_scan that run at once: four a CU
+struct BeamScratch { BeamPlan plan; size_t sums, total; };
+BeamScratch beam_scratch(int n_groups, int n_beams, int vocab, int n_out) {
+    BeamScratch s{};
+    s.plan = beam_plan(n_groups * n_beams, n_beams, vocab, n_out, BEAM_SLOTS);
+    const size_t parts = (size_t)n_groups * n_beams * s.plan.parts;
+    s.sums = align_up(parts * n_out * 8);
+    s.total = s.sums + align_up(parts * sizeof(BeamSum));
+    return s;
+}
+
 }  // namespace
 
 extern "C" {
@@ -77,8 +88,7 @@ extern "C" {
 size_t rs_beam_select_scratch_bytes(int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t n_out) {
     if (n_groups < 1 || n_beams < 1 || n_beams > 64 || n_out < 1 || n_out > 64 || vocab < 1) { fail(RS_EINVAL, "need n_groups >= 1, n_beams and n_out in 1..64, vocab >= 1"); return 0; }
     if ((long long)n_groups * n_beams > 65535) { fail(RS_ECAPACITY, "more than 65535 rows"); return 0; }
-    const size_t rows = (size_t)n_groups * n_beams;
-    return align_up(rows * n_out * 8) + align_up(rows * 8);
+    return beam_scratch(n_groups, n_beams, vocab, n_out).total;
 }
 
 rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype, int32_t n_groups, int32_t n_beams, int32_t vocab,
@@ -100,18 +110,21 @@ rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype
     if ((uintptr_t)d_scratch % ALIGN) return fail(RS_EINVAL, "scratch must be 256-byte aligned");
     if (scratch_bytes < need) return fail(RS_EINVAL, "scratch of %zu bytes is smaller than the %zu needed", scratch_bytes, need);
     const int rows = n_groups * n_beams;
+    const BeamScratch p = beam_scratch(n_groups, n_beams, vocab, n_out);
+    unsigned char *scratch = (unsigned char *)d_scratch;
     BeamArgs a{};
     a.logits = d_logits; a.stride = (size_t)row_stride; a.scale = d_logit_scale; a.score = d_score; a.last = d_last; a.len = d_len;
-    a.eos = eos; a.n_groups = n_groups; a.n_beams = n_beams; a.vocab = vocab; a.n_out = n_out; a.alpha = length_penalty;
+    a.eos = eos; a.n_beams = n_beams; a.vocab = vocab; a.n_out = n_out; a.alpha = length_penalty; a.parts = p.plan.parts; a.batches = p.plan.batches;
     a.parent = d_parent; a.token = d_token; a.len_out = d_len_out; a.score_out = d_score_out; a.flags = d_flags;
-    a.keys = (unsigned long long *)d_scratch;
-    a.log_z = (double *)((unsigned char *)d_scratch + align_up((size_t)rows * n_out * 8));
+    a.keys = (unsigned long long *)scratch; a.sums = (BeamSum *)(scratch + p.sums);
     hipStream_t st = (hipStream_t)stream;
-    if (dtype == RS_F32) hipLaunchKernelGGL((k_beam_row<float>), dim3(rows), dim3(1024), 0, st, a);
-    else hipLaunchKernelGGL((k_beam_row<uint16_t>), dim3(rows), dim3(1024), 0, st, a);
-    RS_LAUNCHED("beam_row");
-    hipLaunchKernelGGL(k_beam_group, dim3(n_groups), dim3(256), 0, st, a);
-    RS_LAUNCHED("beam_group");
+    const dim3 grid(a.parts, rows);
+    if (dtype == RS_F32) hipLaunchKernelGGL((k_beam_scan<float>), grid, dim3(BEAM_THREADS), 0, st, a);
+    else hipLaunchKernelGGL((k_beam_scan<uint16_t>), grid, dim3(BEAM_THREADS), 0, st, a);
+    RS_LAUNCHED("beam_scan");
+    const int keys = n_beams * a.parts * n_out;
+    hipLaunchKernelGGL(k_beam_join, dim3(n_groups), dim3(keys <= 256 * JOIN_EACH ? 256 : keys <= 512 * JOIN_EACH ? 512 : 1024), 0, st, a);
+    RS_LAUNCHED("beam_join");
     return RS_OK;
 }
 

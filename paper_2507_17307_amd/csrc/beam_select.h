@@ -3,178 +3,561 @@
 // The continuation of beam b by token t is worth score_b + (x_t - ln Z_b), x = scale * logits, Z = sum e^x.  Neighbours in the order of a vocabulary,
 // and more so across beams, may be nearer than fp32 sums can tell, so the sum of exponentials and all that is compared across beams are double; within a
 // row the order is that of the logits themselves.
+//
+// k_beam_scan makes one pass over the logits.  A wave takes 1024 of them at a time, 16 a lane: their exponentials go into its sum, the largest of each lane's 16
+// into LDS.  After eight batches it sets a border that n_out of its values at least reach, from what the lanes had as their largest, and only lanes
+// with something at or above it read their 16 values again (from the cache) and put those into a short list of the wave in LDS; a list that fills up is cut to
+// its n_out best.  The workgroup joins its waves' lists and leaves n_out keys and a sum; k_beam_join joins those of a group.  Lists are ordered
+// by counting, for each member, how many come before it.
 #pragma once
 
+#include <cfloat>
+
+#include "beam_plan.h"
 #include "device_utils.h"
 #include "../../include/rstitch.h"
 
 namespace rs {
 
+struct BeamSum { double z; float m; int bad; };                    // sum of 2^((x - m) c) over what was seen, its largest logit, NaN or +inf seen
+
 struct BeamArgs {
     const void *logits; size_t stride;
     const float *scale, *score;
     const int *last, *len;
-    int eos, n_groups, n_beams, vocab, n_out;
+    int eos, n_beams, vocab, n_out, parts, batches;                // parts * n_beams * n_out <= BEAM_KEYS
     double alpha;
     int *parent, *token, *len_out;
     float *score_out;
     unsigned int *flags;
-    unsigned long long *keys;                                      // [row][n_out] best logits of a row, in order
-    double *log_z;                                                 // [row]
+    unsigned long long *keys;                                      // [row][part][n_out]; 0: none
+    BeamSum *sums;                                                 // [row][part]
 };
 
-// 2^d for d <= 0, to 1.1e-12: 2^n p(d - n), n the nearest integer, p of degree eight through 2^f at the Chebyshev nodes of [-1/2, 1/2].
-// Below 2^-1000 it is 2^-1000.
-__device__ __forceinline__ double exp2_sum(double d) {
-    d = fmax(d, -1000.0);
-    const double n = __builtin_rint(d), f = d - n;
+// 2^f for |f| <= 1/2, to 1.1e-12: degree eight through 2^f at the Chebyshev nodes.
+__device__ __forceinline__ double exp2_part(double f) {
     double p = 1.3255224887502117e-06;
     p = fma(p, f, 1.531007940254368e-05); p = fma(p, f, 0.0001540345585240991); p = fma(p, f, 0.0013333450567999414); p = fma(p, f, 0.009618129159402628);
-    p = fma(p, f, 0.05550410941205934); p = fma(p, f, 0.2402265069581299); p = fma(p, f, 0.6931471805459335); p = fma(p, f, 1.0);
-    return __builtin_ldexp(p, (int)n);
+    p = fma(p, f, 0.05550410941205934); p = fma(p, f, 0.2402265069581299); p = fma(p, f, 0.6931471805459335); return fma(p, f, 1.0);
+}
+// p 2^n, p in [0.7, 1.5] and |n| <= 1020: n goes into the exponent
+__device__ __forceinline__ double scale_exp(double p, int n) { return __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p)); }
+// Adding this to a number below 2^30 leaves the nearest integer in the low word of the sum.
+constexpr double TO_INT = 6755399441055744.0;                      // 1.5 2^52
+
+// 2^d for d <= 1; below 2^-1000 it is 2^-1000.
+__device__ __forceinline__ double exp2_sum(double d) {
+    d = fmax(d, -1000.0);
+    const double s = d + TO_INT;
+    return scale_exp(exp2_part(d - (s - TO_INT)), __double2loint(s));
 }
 
 // A logit and its token as one number: larger for a larger logit, and for a lower token among equals (-0 and 0 are equal).  0: no candidate.
+__device__ __forceinline__ uint32_t beam_order(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
 __device__ __forceinline__ unsigned long long beam_key(float x, int token) {
-    const uint32_t u = __float_as_uint(x + 0.f), o = u >> 31 ? ~u : u | 0x80000000u;
-    return x > -INFINITY ? (unsigned long long)o << 32 | (uint32_t)~token : 0;
+    return x > -INFINITY ? (unsigned long long)beam_order(x) << 32 | (uint32_t)~token : 0;
 }
-__device__ __forceinline__ float key_logit(unsigned long long key) {
-    const uint32_t o = (uint32_t)(key >> 32);
-    return __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o);
-}
+constexpr uint32_t ORDER_OF_MINUS_INF = 0x007fffffu;
+__device__ __forceinline__ float order_logit(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ float key_logit(unsigned long long key) { return order_logit((uint32_t)(key >> 32)); }
 __device__ __forceinline__ int key_token(unsigned long long key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ unsigned long long double_order(double x) {
+    const unsigned long long u = (unsigned long long)__double_as_longlong(x + 0.0);
+    return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double order_double(unsigned long long o) { return __longlong_as_double((long long)(o >> 63 ? o & ~(1ull << 63) : ~o)); }
 
-__device__ __forceinline__ float beam_logit(const float *x, int i) { return x[i]; }
-__device__ __forceinline__ float beam_logit(const uint16_t *x, int i) { return bf16_to_f32(x[i]); }
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, RS_WAVE);
+    return v;
+}
 
 // What a row takes part with: its vocabulary, its end, or nothing.
 enum { BEAM_NONE, BEAM_ENDED, BEAM_RUNS };
-__device__ __forceinline__ int beam_row(const BeamArgs &a, int row, unsigned int &flag) {
-    const float score = a.score[row], scale = a.scale ? a.scale[row] : 1.f;
+struct BeamRow { float score, scale; int last, len; };
+__device__ __forceinline__ BeamRow beam_row(const BeamArgs &a, int row) {
+    return {a.score[row], a.scale ? a.scale[row] : 1.f, a.last ? a.last[row] : -2, a.len ? a.len[row] : 0};
+}
+__device__ __forceinline__ int beam_kind(const BeamRow &r, int eos, unsigned int &flag) {
     flag = 0;
-    if (!(score < INFINITY) || (a.len && a.len[row] < 0)) { flag = RS_FLAG_BADARG; return BEAM_NONE; }
-    if (score == -INFINITY) return BEAM_NONE;
-    if (a.last && a.eos >= 0 && a.last[row] == a.eos) return BEAM_ENDED;
-    if (!(scale > 0.f && scale < INFINITY)) { flag = RS_FLAG_BADARG; return BEAM_NONE; }
+    if (!(r.score < INFINITY) || r.len < 0) { flag = RS_FLAG_BADARG; return BEAM_NONE; }
+    if (r.score == -INFINITY) return BEAM_NONE;
+    if (eos >= 0 && r.last == eos) return BEAM_ENDED;
+    if (!(r.scale > 0.f && r.scale < INFINITY)) { flag = RS_FLAG_BADARG; return BEAM_NONE; }
     return BEAM_RUNS;
 }
 
-// ---------------------------------------------------------------- one row
-// grid rows, block 1024: ln Z, then the n_out best logits one after the other
+// A number that at least `keep` of 128 reach, two a lane (0 if so many are not above 0).  keep <= 64.
+// The lanes in 2^k >= keep groups: the least of the groups' largest, 6 steps across lanes.  Of random numbers keep (ln keep + 0.6) reach that;
+// halving the way to the largest brings it nearer to keep.
+template <bool MIN>
+__device__ __forceinline__ uint32_t row_step(uint32_t v, int step) {
+    uint32_t o;
+    if (step == 0) o = __builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false);
+    else if (step == 1) o = __builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false);
+    else if (step == 2) o = __builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false);
+    else o = __builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false);
+    return MIN ? min(v, o) : max(v, o);
+}
+__device__ __forceinline__ uint32_t wave_border(uint32_t x, uint32_t y, int keep, int halvings) {
+    const int lanes = keep > 32 ? 0 : keep > 16 ? 1 : keep > 8 ? 2 : keep > 4 ? 3 : keep > 2 ? 4 : keep > 1 ? 5 : 6;      // log2 of a group's lanes
+    uint32_t t = max(x, y), m = t;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        t = s < lanes ? row_step<false>(t, s) : row_step<true>(t, s);
+        m = row_step<false>(m, s);
+    }
+    auto join = [](uint32_t v, bool sixteen, bool thirty_two) {    // (four rows of 16 lanes; true: the larger)
+        const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16), c = __builtin_amdgcn_readlane(v, 32), d = __builtin_amdgcn_readlane(v, 48);
+        const uint32_t e = sixteen ? max(a, b) : min(a, b), f = sixteen ? max(c, d) : min(c, d);
+        return thirty_two ? max(e, f) : min(e, f);
+    };
+    uint32_t lo = join(t, lanes > 4, lanes > 5);
+    if (halvings > 0) {
+        uint32_t hi = join(m, true, true);
+#pragma unroll 1
+        for (int k = 0; k < halvings; ++k) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            const bool enough = (int)__popcll(__ballot(x >= mid)) + (int)__popcll(__ballot(y >= mid)) >= keep;
+            lo = enough ? mid : lo; hi = enough ? hi : mid;
+        }
+    }
+    return lo;
+}
+
+// Lane's place among the wave's lanes with `in`, behind *count, which it moves on: one addition for the wave.
+__device__ __forceinline__ int wave_place(bool in, int *count) {
+    const unsigned long long who = __ballot(in);
+    if (!who) return 0;
+    int base = 0;
+    if ((threadIdx.x & 63) == 0) base = atomicAdd(count, (int)__popcll(who));
+    return __builtin_amdgcn_readfirstlane(base) + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+}
+
+// ---------------------------------------------------------------- a wave's list
+constexpr int BEAM_LIST = 256;
+
+// Keys above `floor`, of which it has to keep so many (once it was cut, floor is the last of those).
+struct WaveList {
+    unsigned long long *keys, floor;
+    int n, keep;
+
+    __device__ __forceinline__ void cut() {
+        const int lane = threadIdx.x & 63;
+        unsigned long long mine[BEAM_LIST / 64];
+        int rank[BEAM_LIST / 64];
+#pragma unroll
+        for (int k = 0; k < BEAM_LIST / 64; ++k) { mine[k] = lane + 64 * k < n ? keys[lane + 64 * k] : 0; rank[k] = 0; }
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+            const unsigned long long other = keys[j];
+#pragma unroll
+            for (int k = 0; k < BEAM_LIST / 64; ++k) rank[k] += other > mine[k];
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int k = 0; k < BEAM_LIST / 64; ++k) if (mine[k] && rank[k] < keep) keys[rank[k]] = mine[k];
+        __builtin_amdgcn_wave_barrier();
+        if (n > keep) n = keep;
+        if (n == keep) floor = keys[keep - 1];
+    }
+    __device__ __forceinline__ void push(unsigned long long key) {
+        bool in = key > floor;
+        unsigned long long who = __ballot(in);
+        if (!who) return;
+        if (n + (int)__popcll(who) > BEAM_LIST) {
+            cut();
+            in = key > floor;
+            who = __ballot(in);
+        }
+        if (in) keys[n + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key;
+        n += (int)__popcll(who);
+    }
+};
+
+// ---------------------------------------------------------------- a wave's sum
+// Batches whose logits are of an ordinary size are added up as sum 2^(x c - r) for one integer r of the wave, near the largest of its first batch: x c is
+// rounded to n, which goes into the exponent, and x c - n is exact in one operation (14 double instructions a logit; from the largest logit met so
+// far, with its rescaling, 17).  What is 2^1000 times smaller is raised to that.  Other batches, logits beyond 4096 and what towers 2^500 above r, are added
+// up by the lanes from their largest.
+struct WaveSum {
+    double c, z, lane_z;                                           // z: with r; lane_z: with lane_m
+    float lane_m, low, high;
+    int r;
+    bool bad, ready;
+
+    __device__ __forceinline__ void init(float scale) {
+        c = (double)scale * 1.4426950408889634074;
+        z = lane_z = 0.0; lane_m = low = high = -INFINITY; r = 0; bad = ready = false;
+    }
+    __device__ __forceinline__ void add(const float (&v)[16], float top) {
+        if (!ready) {
+            const float m = wave_max(top);
+            const double x = (double)m * c;
+            if (fabs(x) < 4096.0) {
+                r = (int)__builtin_rint(x);
+                low = (float)((double)(r - 1000) / c); high = (float)((double)(r + 500) / c);
+                ready = true;
+            }
+        }
+        if (ready && !__any(top > high)) {
+            const double shift = TO_INT - (double)r;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const double x = (double)fmaxf(v[k], low), s = fma(x, c, shift);
+                z += scale_exp(exp2_part(fma(x, c, shift - s)), __double2loint(s));
+            }
+        } else {
+            if (top > lane_m) { lane_z = lane_m > -INFINITY ? lane_z * exp2_sum(((double)lane_m - (double)top) * c) : 0.0; lane_m = top; }
+            const double from = lane_m > -INFINITY ? (double)lane_m : 0.0;         // (nothing but masked logits so far: their 2^-1000 are dropped)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) lane_z += exp2_sum(((double)v[k] - from) * c);
+        }
+    }
+    // the wave's largest logit among those added, given the largest of each lane; z then counts from it
+    __device__ __forceinline__ float finish(float lane_top) {
+        const float top = wave_max(lane_top);
+        double all = lane_m > -INFINITY ? lane_z * exp2_sum(((double)lane_m - (double)top) * c) : 0.0;
+        if (ready && top > -INFINITY) all += z * exp2_sum((double)r - (double)top * c);
+        z = wave_sum_f64(all);
+        return top;
+    }
+};
+
+// How many of m numbers are above `mine`, and how many equal it.  x: in LDS, 16-byte aligned, with zeros up to a multiple of eight.
+__device__ __forceinline__ void count_before(const uint32_t *x, int m, uint32_t mine, int &above, int &equal) {
+#pragma unroll 1
+    for (int j = 0; j < m; j += 8) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(x + j), b = *reinterpret_cast<const uint4 *>(x + j + 4);
+        const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { above += v[k] > mine; equal += v[k] == mine; }
+    }
+}
+
+// f(j) for those that equal it.
+template <typename F>
+__device__ __forceinline__ void for_equal(const uint32_t *x, int m, uint32_t mine, F f) {
+#pragma unroll 1
+    for (int j = 0; j < m; j += 8) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(x + j), b = *reinterpret_cast<const uint4 *>(x + j + 4);
+        const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        uint32_t which = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) which |= (uint32_t)(v[k] == mine) << k;
+        for (; which; which &= which - 1) f(j + __ffs(which) - 1);
+    }
+}
+
+// ---------------------------------------------------------------- a wave's batch
+template <typename T> struct BeamUnit;                             // a piece of 16 bytes
+template <> struct BeamUnit<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void load(const float *p, float (&v)[4]) {
+        const float4 q = *reinterpret_cast<const float4 *>(p);
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    }
+    static __device__ __forceinline__ float one(const float *p) { return *p; }
+};
+template <> struct BeamUnit<uint16_t> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[8]) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(p);
+        v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
+        v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
+    }
+    static __device__ __forceinline__ float one(const uint16_t *p) { return bf16_to_f32(*p); }
+};
+
+constexpr int BEAM_ROUND = 8;                                      // batches between two looks for candidates
+
+struct ScanShared {
+    union {
+        unsigned long long list[BEAM_WAVES][BEAM_LIST];
+        struct { uint32_t order[BEAM_WAVES * BEAM_LIST + 8], rest[BEAM_WAVES * BEAM_LIST]; } kept;
+    };
+    float top[BEAM_WAVES][BEAM_ROUND][64];
+    double z[BEAM_WAVES];
+    float m[BEAM_WAVES];
+    uint32_t border[BEAM_WAVES];
+    int bad[BEAM_WAVES], n;
+};
+
+// grid (parts, rows), block BEAM_THREADS
 template <typename T>
-__global__ void __launch_bounds__(1024) k_beam_row(BeamArgs a) {
-    __shared__ float sh_m[16];
-    __shared__ double sh_z[16];
-    __shared__ unsigned long long sh_key[16];
-    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    unsigned long long *keys = a.keys + (size_t)row * a.n_out;
+__global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
+    constexpr int UNIT = BeamUnit<T>::N, PIECES = 16 / UNIT, WAVE_UNITS = 64 * PIECES;
+    __shared__ ScanShared sh;
+    const int row = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const BeamRow r = beam_row(a, row);
     unsigned int flag;
-    const int what = beam_row(a, row, flag);
-    if (flag && tid == 0 && a.flags) atomicOr(a.flags + row, flag);
-    if (what != BEAM_RUNS) {
-        for (int k = tid; k < a.n_out; k += 1024) keys[k] = 0;
-        return;
-    }
+    const int kind = beam_kind(r, a.eos, flag);
+    if (flag && part == 0 && tid == 0 && a.flags) atomicOr(a.flags + row, flag);
+    if (kind != BEAM_RUNS) return;
     const T *x = (const T *)a.logits + (size_t)row * a.stride;
-    const double c = (a.scale ? a.scale[row] : 1.f) * 1.4426950408889634074;
-    float m = -INFINITY;
-    int bad = 0;
-    for (int i = tid; i < a.vocab; i += 1024) {
-        const float v = beam_logit(x, i);
-        bad |= !(v < INFINITY);
-        m = fmaxf(m, v);
+    // values before the first 16-byte border, whole pieces from there, values behind the last piece
+    const int before = min(a.vocab, (int)((16 - (uintptr_t)x % 16) % 16 / sizeof(T))), pieces = (a.vocab - before) / UNIT, behind = a.vocab - before - pieces * UNIT;
+    // the values before are the first part's, those behind the last one's: a batch of their own, one a lane
+    const int head = part == 0 ? before : 0, ends = wave == 0 ? head + (part == a.parts - 1 ? behind : 0) : 0;
+    const T *px = x + before;
+    WaveSum sum;
+    sum.init(r.scale);
+    WaveList list{sh.list[wave], 0, 0, a.n_out};
+    uint32_t border = 0;
+    float v[16], least = -FLT_MAX, lo_top = -INFINITY, hi_top = -INFINITY;
+    const int unit_a = (part * a.batches * BEAM_WAVES + wave) * WAVE_UNITS + lane;
+    const int wave_pieces = pieces - unit_a + lane;                // pieces from the wave's first one on
+    int whole = wave_pieces <= 0 ? 0 : (wave_pieces + BEAM_WAVES * WAVE_UNITS - 1) / (BEAM_WAVES * WAVE_UNITS);
+    whole = min(whole, a.batches);
+    const int n_batches = whole + (ends > 0);
+    // this lane's values of batch b
+    auto fetch = [&](int b, float (&w)[16]) __attribute__((always_inline)) {
+        if (b < whole) {
+            const int u0 = unit_a + b * (BEAM_WAVES * WAVE_UNITS);
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) {
+                float t[UNIT];
+#pragma unroll
+                for (int e = 0; e < UNIT; ++e) t[e] = -INFINITY;
+                if (u0 + 64 * j < pieces) BeamUnit<T>::load(px + (size_t)(u0 + 64 * j) * UNIT, t);
+#pragma unroll
+                for (int e = 0; e < UNIT; ++e) w[j * UNIT + e] = t[e];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = -INFINITY;
+            if (lane < ends) w[0] = BeamUnit<T>::one(x + (lane < head ? lane : a.vocab - behind + (lane - head)));
+        }
+    };
+    if (n_batches > 0) fetch(0, v);
+    for (int b0 = 0; b0 < n_batches; b0 += BEAM_ROUND) {
+        const int n_round = min(BEAM_ROUND, n_batches - b0);
+        float best = -INFINITY;
+        for (int b = b0;;) {
+            float next[16];
+            if (b + 1 < n_batches) fetch(b + 1, next);
+            float lo = v[0], hi = v[8];
+#pragma unroll
+            for (int k = 1; k < 8; ++k) { lo = fmaxf(lo, v[k]); hi = fmaxf(hi, v[8 + k]); }
+            const float top = fmaxf(lo, hi);
+            lo_top = fmaxf(lo_top, lo); hi_top = fmaxf(hi_top, hi); best = fmaxf(best, top);
+            sh.top[wave][b - b0][lane] = top;
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) sum.bad |= __builtin_isunordered(v[k], v[k + 1]);
+            sum.add(v, top);
+            ++b;
+            if (b == b0 + n_round) break;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = next[k];
+        }
+        if (__any(best >= least)) {
+            border = max(border, wave_border(beam_order(lo_top), beam_order(hi_top), a.n_out, a.n_out > 8 ? 8 : 0));
+            least = border > ORDER_OF_MINUS_INF ? order_logit(border) : -FLT_MAX;
+            uint32_t in = 0;                                       // the lane's batches with something to take
+            for (int k = 0; k < n_round; ++k) in |= (uint32_t)(sh.top[wave][k][lane] >= least) << k;
+#pragma unroll 1
+            while (__any(in != 0)) {
+                const int b = b0 + __ffs(in) - 1;                  // (the last one is still there)
+                float w[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) w[k] = v[k];
+                if (in && b != b0 + n_round - 1) fetch(b, w);
+                uint32_t which = 0;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) which |= (uint32_t)(w[k] >= least) << k;
+                if (!in) which = 0;
+                const int first = b < whole ? before + (unit_a + b * (BEAM_WAVES * WAVE_UNITS)) * UNIT : lane < head ? lane : a.vocab - behind + (lane - head);
+#pragma unroll 1
+                while (__any(which != 0)) {                        // a lane's next one
+                    const int k = __ffs(which) - 1;
+                    // (chosen by bits: a choice between two elements of an array becomes one between their addresses)
+                    const uint32_t eight = 0u - (k >> 3 & 1), four = 0u - (k >> 2 & 1), two = 0u - (k >> 1 & 1), one = 0u - (k & 1);
+                    uint32_t q[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) q[e] = (__float_as_uint(w[8 + e]) & eight) | (__float_as_uint(w[e]) & ~eight);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q[e] = (q[4 + e] & four) | (q[e] & ~four);
+                    q[0] = (q[2] & two) | (q[0] & ~two); q[1] = (q[3] & two) | (q[1] & ~two);
+                    list.push(which ? beam_key(__uint_as_float((q[1] & one) | (q[0] & ~one)), first + (k / UNIT) * (64 * UNIT) + k % UNIT) : 0);
+                    which &= which - 1;
+                }
+                in &= in - 1;
+            }
+        }
+        if (b0 + BEAM_ROUND < n_batches) fetch(b0 + BEAM_ROUND, v);
     }
-    m = wave_max(m);
-    if (lane == 0) sh_m[wave] = m;
-    bad = __syncthreads_or(bad);
-    for (int w = 0; w < 16; ++w) m = fmaxf(m, sh_m[w]);
-    if (bad || !(m > -INFINITY)) {
-        if (bad && tid == 0 && a.flags) atomicOr(a.flags + row, RS_FLAG_NONFINITE);
-        for (int k = tid; k < a.n_out; k += 1024) keys[k] = 0;
-        return;
-    }
-    double z = 0.0;
-    for (int i = tid; i < a.vocab; i += 1024) z += exp2_sum(((double)beam_logit(x, i) - (double)m) * c);
-    for (int o = 32; o; o >>= 1) z += __shfl_xor(z, o, RS_WAVE);
-    if (lane == 0) sh_z[wave] = z;
+    const float lane_top = fmaxf(lo_top, hi_top);
+    // ---- the waves' sums and lists
+    const float top = sum.finish(lane_top);
+    const int bad = __any(sum.bad || !(lane_top < INFINITY));
+    if (lane == 0) { sh.z[wave] = sum.z; sh.m[wave] = top; sh.bad[wave] = bad; sh.border[wave] = border; }
+    if (tid == 0) sh.n = 0;
     __syncthreads();
     if (tid == 0) {
-        z = 0.0;
-        for (int w = 0; w < 16; ++w) z += sh_z[w];
-        a.log_z[row] = log(z) + (double)m * (a.scale ? a.scale[row] : 1.f);
+        float m = sh.m[0];
+        int any = sh.bad[0];
+#pragma unroll
+        for (int w = 1; w < BEAM_WAVES; ++w) { m = fmaxf(m, sh.m[w]); any |= sh.bad[w]; }
+        double all = 0.0;
+#pragma unroll 1
+        for (int w = 0; w < BEAM_WAVES; ++w) all += sh.m[w] > -INFINITY && !any ? sh.z[w] * exp2_sum(((double)sh.m[w] - (double)m) * sum.c) : 0.0;
+        a.sums[(size_t)row * a.parts + part] = {all, m, any};
     }
-    unsigned long long before = ~0ull;
-    for (int k = 0; k < a.n_out; ++k) {
-        unsigned long long best = 0;
-        for (int i = tid; i < a.vocab; i += 1024) {
-            const unsigned long long key = beam_key(beam_logit(x, i), i);
-            if (key < before && key > best) best = key;
-        }
-        for (int o = 32; o; o >>= 1) { const unsigned long long u = __shfl_xor(best, o, RS_WAVE); best = u > best ? u : best; }
-        __syncthreads();
-        if (lane == 0) sh_key[wave] = best;
-        __syncthreads();
-        for (int w = 0; w < 16; ++w) best = sh_key[w] > best ? sh_key[w] : best;
-        if (tid == 0) keys[k] = best;
-        before = best;
-        if (!best) { for (int j = k + 1 + tid; j < a.n_out; j += 1024) keys[j] = 0; break; }
+    // (n_out keys at least reach each of the waves' borders: those below the highest border are out)
+    uint32_t highest = 0;
+#pragma unroll
+    for (int w = 0; w < BEAM_WAVES; ++w) highest = max(highest, sh.border[w]);
+    unsigned long long mine[BEAM_LIST / 64];
+#pragma unroll
+    for (int k = 0; k < BEAM_LIST / 64; ++k) mine[k] = lane + 64 * k < list.n ? list.keys[lane + 64 * k] : 0;
+    __syncthreads();
+    unsigned long long *to = a.keys + ((size_t)row * a.parts + part) * a.n_out;
+#pragma unroll
+    for (int k = 0; k < BEAM_LIST / 64; ++k) {
+        const bool in = mine[k] && (uint32_t)(mine[k] >> 32) >= highest;
+        const int at = wave_place(in, &sh.n);
+        if (in) { sh.kept.order[at] = (uint32_t)(mine[k] >> 32); sh.kept.rest[at] = (uint32_t)mine[k]; }
     }
+    __syncthreads();
+    const int m = sh.n;
+    if (tid < 8) sh.kept.order[m + tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < m; i += BEAM_THREADS) {
+        const uint32_t order = sh.kept.order[i], rest = sh.kept.rest[i];
+        int rank = 0, equal = 0;
+        count_before(sh.kept.order, m, order, rank, equal);
+        if (equal > 1) for_equal(sh.kept.order, m, order, [&](int j) { rank += sh.kept.rest[j] > rest; });
+        if (rank < a.n_out) to[rank] = (unsigned long long)order << 32 | rest;
+    }
+    for (int k = m + tid; k < a.n_out; k += BEAM_THREADS) to[k] = 0;
 }
 
-// ---------------------------------------------------------------- one group
-struct BeamCandidate { double rank, value; int beam, at, token, len; };
-__device__ __forceinline__ bool beam_before(const BeamCandidate &a, const BeamCandidate &b) {      // a is taken before b; beam < 0: none
-    if (b.beam < 0) return a.beam >= 0;
-    if (a.beam < 0) return false;
-    return a.rank > b.rank || (a.rank == b.rank && (a.beam < b.beam || (a.beam == b.beam && a.at < b.at)));
+// ---------------------------------------------------------------- the join of a group
+constexpr int JOIN_EACH = 4;                                       // keys a thread
+constexpr int JOIN_KEPT = 1024;                                    // items that are kept for ordering
+
+struct JoinShared {
+    uint32_t high[JOIN_KEPT + 8];                                  // upper halves of the values
+    unsigned long long value[JOIN_KEPT], key[JOIN_KEPT], edge_value, edge_key;
+    uint32_t beam[JOIN_KEPT], edge_beam, border[16];
+    double row_z[BEAM_MAX], row_div[BEAM_MAX];
+    float row_score[BEAM_MAX], row_scale[BEAM_MAX];
+    int row_kind[BEAM_MAX], row_len[BEAM_MAX], n;
+};
+
+// The order of items: larger values first, of equals the lower beam, in one beam the larger key.
+__device__ __forceinline__ bool item_before(unsigned long long v, uint32_t b, unsigned long long k, unsigned long long v2, uint32_t b2, unsigned long long k2) {
+    return v > v2 || (v == v2 && (b < b2 || (b == b2 && k > k2)));
 }
 
-// grid groups, block 256
-__global__ void __launch_bounds__(256) k_beam_group(BeamArgs a) {
-    __shared__ BeamCandidate sh[256];
-    const int g = blockIdx.x, tid = threadIdx.x;
-    BeamCandidate last{INFINITY, 0.0, 0, -1, 0, 0};
-    float out_score = 0.f;
-    int out_parent = -1, out_token = -1, out_len = 0;
-    for (int k = 0; k < a.n_out; ++k) {
-        BeamCandidate best{0.0, 0.0, -1, 0, 0, 0};
-        for (int i = tid; i < a.n_beams * a.n_out; i += 256) {
-            const int b = i / a.n_out, at = i - b * a.n_out, row = g * a.n_beams + b;
-            unsigned int flag;
-            const int what = beam_row(a, row, flag);
-            BeamCandidate c{0.0, 0.0, -1, at, 0, 0};
-            const int len = a.len ? a.len[row] : 0;
-            if (what == BEAM_ENDED && at == 0) { c.beam = b; c.token = a.eos; c.value = a.score[row]; c.len = len; }
-            const unsigned long long key = what == BEAM_RUNS ? a.keys[(size_t)row * a.n_out + at] : 0;
-            if (key) {
-                c.beam = b; c.token = key_token(key); c.len = len + 1;
-                c.value = (double)a.score[row] + ((double)key_logit(key) * (a.scale ? a.scale[row] : 1.f) - a.log_z[row]);
-            }
-            if (c.beam < 0) continue;
-            c.rank = a.alpha > 0.0 ? c.value / pow((double)max(c.len, 1), a.alpha) : c.value;
-            if (beam_before(last, c) && beam_before(c, best)) best = c;
+// grid groups, block 256, 512 or 1024: JOIN_EACH keys a thread
+__global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
+    __shared__ JoinShared sh;
+    const int g = blockIdx.x, tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, wave = tid >> 6, parts = a.parts;
+    const int per_row = parts * a.n_out, n = a.n_beams * per_row, waves = min(threads, n + 63) >> 6;      // those that have keys
+    const unsigned long long *keys = a.keys + (size_t)g * a.n_beams * per_row;
+    unsigned long long value[JOIN_EACH], key[JOIN_EACH];
+#pragma unroll
+    for (int k = 0; k < JOIN_EACH; ++k) key[k] = tid + threads * k < n ? keys[tid + threads * k] : 0;      // (of rows that do not run: anything)
+    // ---- ln Z of the rows: as many lanes a row as it has parts, up to the next power of two
+    const int shift = parts <= 1 ? 0 : 32 - __clz(parts - 1), rows_at_once = threads >> shift, sub = lane & ((1 << shift) - 1);
+    for (int b0 = 0; b0 < a.n_beams; b0 += rows_at_once) {
+        const int b = b0 + (tid >> shift), row = g * a.n_beams + min(b, a.n_beams - 1);
+        const BeamRow r = beam_row(a, row);
+        unsigned int flag;
+        int kind = beam_kind(r, a.eos, flag), bad = 0;
+        double z = 0.0;
+        float m = -INFINITY;
+        if (kind == BEAM_RUNS && sub < parts) {
+            const BeamSum s = a.sums[(size_t)row * parts + sub];
+            z = s.z; m = s.m; bad = s.bad;
         }
-        __syncthreads();
-        sh[tid] = best;
-        __syncthreads();
-        for (int o = 128; o; o >>= 1) {
-            if (tid < o && beam_before(sh[tid + o], sh[tid])) sh[tid] = sh[tid + o];
-            __syncthreads();
+        float top = m;
+        for (int o = 1; o < 1 << shift; o <<= 1) { top = fmaxf(top, __shfl_xor(top, o, RS_WAVE)); bad |= __shfl_xor(bad, o, RS_WAVE); }
+        z = m > -INFINITY ? z * exp2_sum(((double)m - (double)top) * ((double)r.scale * 1.4426950408889634074)) : 0.0;
+        for (int o = 1; o < 1 << shift; o <<= 1) z += __shfl_xor(z, o, RS_WAVE);
+        if (sub == 0 && b < a.n_beams) {
+            if (bad && a.flags) atomicOr(a.flags + row, RS_FLAG_NONFINITE);
+            if (kind == BEAM_RUNS && (bad || !(top > -INFINITY))) kind = BEAM_NONE;
+            const int len = r.len + (kind == BEAM_RUNS);
+            sh.row_kind[b] = kind; sh.row_len[b] = len; sh.row_score[b] = r.score; sh.row_scale[b] = r.scale;
+            sh.row_z[b] = kind == BEAM_RUNS ? log(z) + (double)top * (double)r.scale : 0.0;
+            sh.row_div[b] = a.alpha > 0.0 ? pow((double)max(len, 1), a.alpha) : 1.0;
         }
-        best = sh[0];
-        if (tid == k) {
-            out_parent = best.beam; out_token = best.beam < 0 ? -1 : best.token; out_len = best.len;
-            out_score = best.beam < 0 ? -INFINITY : (float)best.value;
-        }
-        if (best.beam < 0) { if (tid > k && tid < a.n_out) out_score = -INFINITY; break; }
-        last = best;
     }
-    __syncthreads();                                               // (outputs may be the inputs' places)
-    if (tid < a.n_out) {
-        const size_t o = (size_t)g * a.n_out + tid;
-        a.parent[o] = out_parent; a.token[o] = out_token; a.score_out[o] = out_score;
-        if (a.len_out) a.len_out[o] = out_len;
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    // ---- the items' values
+    unsigned long long best = 0;
+#pragma unroll
+    for (int k = 0; k < JOIN_EACH; ++k) {
+        const int i = tid + threads * k, b = min(i / per_row, a.n_beams - 1), kind = i < n ? sh.row_kind[b] : BEAM_NONE;
+        value[k] = 0;
+        double v = sh.row_score[b];
+        if (kind == BEAM_RUNS) v += (double)key_logit(key[k]) * (double)sh.row_scale[b] - sh.row_z[b];
+        if (kind == BEAM_ENDED) key[k] = i == b * per_row ? 1ull << 32 | (uint32_t)~a.eos : 0;
+        if (kind != BEAM_NONE && key[k]) value[k] = double_order(a.alpha > 0.0 ? v / sh.row_div[b] : v);
+        best = value[k] > best ? value[k] : best;
+    }
+    // a share of them in each wave: all of these reach the least of the waves' borders
+    const uint32_t wave_least = wave_border((uint32_t)(best >> 32), 0, (a.n_out + waves - 1) / waves, 12);
+    if (lane == 0) sh.border[wave] = wave_least;
+    __syncthreads();
+    uint32_t border = sh.border[0];
+    for (int w = 1; w < waves; ++w) border = min(border, sh.border[w]);
+    auto keep = [&](int k, bool in) __attribute__((always_inline)) {
+        const int at = wave_place(in, &sh.n);
+        if (in && at < JOIN_KEPT) { sh.high[at] = (uint32_t)(value[k] >> 32); sh.value[at] = value[k]; sh.key[at] = key[k]; sh.beam[at] = (tid + threads * k) / per_row; }
+    };
+#pragma unroll
+    for (int k = 0; k < JOIN_EACH; ++k) keep(k, value[k] && (uint32_t)(value[k] >> 32) >= border);
+    __syncthreads();
+    if (sh.n > JOIN_KEPT) {
+        // too many (equals, or a wave with next to nothing): the border is the n_out-th of the threads' first items, which leaves items of n_out threads
+        unsigned long long v = 0, x = 0;
+        uint32_t b = 0;
+#pragma unroll
+        for (int k = 0; k < JOIN_EACH; ++k) {
+            const uint32_t bk = (tid + threads * k) / per_row;
+            if (value[k] && (!v || item_before(value[k], bk, key[k], v, b, x))) { v = value[k]; x = key[k]; b = bk; }
+        }
+        __syncthreads();
+        sh.value[tid] = v; sh.key[tid] = x; sh.beam[tid] = b;
+        if (tid == 0) { sh.n = 0; sh.edge_value = 0; sh.edge_key = 0; sh.edge_beam = 0; }
+        __syncthreads();
+        int rank = 0;
+        for (int j = 0; j < threads; ++j) rank += item_before(sh.value[j], sh.beam[j], sh.key[j], v, b, x);
+        if (v && rank == a.n_out - 1) { sh.edge_value = v; sh.edge_key = x; sh.edge_beam = b; }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < JOIN_EACH; ++k)
+            keep(k, value[k] && !item_before(sh.edge_value, sh.edge_beam, sh.edge_key, value[k], (tid + threads * k) / per_row, key[k]));
+        __syncthreads();
+    }
+    // ---- in order (all rows were read: outputs may be their places)
+    const size_t o = (size_t)g * a.n_out;
+    const int m = sh.n;
+    if (tid < 8) sh.high[m + tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < m; i += threads) {
+        const unsigned long long v = sh.value[i], x = sh.key[i];
+        const uint32_t b = sh.beam[i], high = sh.high[i];
+        int rank = 0, equal = 0;
+        count_before(sh.high, m, high, rank, equal);
+        if (equal > 1)
+            for_equal(sh.high, m, high, [&](int j) { rank += item_before(sh.value[j], sh.beam[j], sh.key[j], v, b, x); });
+        if (rank < a.n_out) {
+            a.parent[o + rank] = (int)b; a.token[o + rank] = key_token(x); a.score_out[o + rank] = (float)(order_double(v) * sh.row_div[b]);
+            if (a.len_out) a.len_out[o + rank] = sh.row_len[b];
+        }
+    }
+    for (int k = m + tid; k < a.n_out; k += threads) {
+        a.parent[o + k] = -1; a.token[o + k] = -1; a.score_out[o + k] = -INFINITY;
+        if (a.len_out) a.len_out[o + k] = 0;
     }
 }
 
