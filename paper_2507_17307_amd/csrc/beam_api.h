@@ -61,11 +61,13 @@ rs_status check_pool_rows(int32_t n, const void *a, const void *b, const void *c
     return RS_OK;
 }
 
-rs_status launch_copy(const CopyArgs &a, long long moves_most, hipStream_t st) {
-    const size_t page_values = (size_t)a.to.n_kv * a.to.head_dim << a.to.page_shift;
-    const double pieces = (double)((page_values / 8 + 256 * COPY_UNITS - 1) / (256 * COPY_UNITS)) * a.to.n_layers * 2 * (double)moves_most;
-    const int grid = pieces < 2048 ? (pieces < 1 ? 1 : (int)pieces) : 2048;
-    hipLaunchKernelGGL(k_pool_copy, dim3(grid), dim3(256), 0, st, a);
+constexpr int COPY_WGS = 4096;                                     // workgroups of k_pool_copy, about
+rs_status launch_copy(CopyArgs a, int moves_most, hipStream_t st) {
+    const long long units = (long long)a.to.n_kv * a.to.head_dim << a.to.page_shift >> 3, halves = 2LL * a.to.n_layers;
+    a.pieces = (int)((units + 256 * COPY_UNITS - 1) / (256 * COPY_UNITS));
+    const long long x = a.pieces * halves, y = (COPY_WGS + x - 1) / x;
+    if (x > 0xffffff) return fail(RS_EINVAL, "a page of all layers is too large");
+    hipLaunchKernelGGL(k_pool_copy, dim3((unsigned)x, (unsigned)(y < moves_most ? y : moves_most < 1 ? 1 : moves_most)), dim3(256), 0, st, a);
     RS_LAUNCHED("pool_copy");
     return RS_OK;
 }

@@ -70,6 +70,11 @@ __device__ __forceinline__ unsigned long long double_order(double x) {
 }
 __device__ __forceinline__ double order_double(unsigned long long o) { return __longlong_as_double((long long)(o >> 63 ? o & ~(1ull << 63) : ~o)); }
 
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, RS_WAVE));
+    return v;
+}
 __device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, RS_WAVE);
@@ -143,26 +148,23 @@ constexpr int BEAM_LIST = 256;
 
 // Keys above `floor`, of which it has to keep so many (once it was cut, floor is the last of those).
 struct WaveList {
-    unsigned long long *keys, floor;
+    unsigned long long *keys, *spare, floor;                       // spare: room for `keep` keys
     int n, keep;
 
     __device__ __forceinline__ void cut() {
         const int lane = threadIdx.x & 63;
-        unsigned long long mine[BEAM_LIST / 64];
-        int rank[BEAM_LIST / 64];
-#pragma unroll
-        for (int k = 0; k < BEAM_LIST / 64; ++k) { mine[k] = lane + 64 * k < n ? keys[lane + 64 * k] : 0; rank[k] = 0; }
 #pragma unroll 1
-        for (int j = 0; j < n; ++j) {
-            const unsigned long long other = keys[j];
-#pragma unroll
-            for (int k = 0; k < BEAM_LIST / 64; ++k) rank[k] += other > mine[k];
+        for (int i = lane; i < n; i += 64) {
+            const unsigned long long mine = keys[i];
+            int rank = 0;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) rank += keys[j] > mine;
+            if (rank < keep) spare[rank] = mine;
         }
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int k = 0; k < BEAM_LIST / 64; ++k) if (mine[k] && rank[k] < keep) keys[rank[k]] = mine[k];
-        __builtin_amdgcn_wave_barrier();
         if (n > keep) n = keep;
+        if (lane < n) keys[lane] = spare[lane];
+        __builtin_amdgcn_wave_barrier();
         if (n == keep) floor = keys[keep - 1];
     }
     __device__ __forceinline__ void push(unsigned long long key) {
@@ -280,7 +282,7 @@ struct ScanShared {
         unsigned long long list[BEAM_WAVES][BEAM_LIST];
         struct { uint32_t order[BEAM_WAVES * BEAM_LIST + 8], rest[BEAM_WAVES * BEAM_LIST]; } kept;
     };
-    float top[BEAM_WAVES][BEAM_ROUND][64];
+    union { float of[BEAM_ROUND][64]; unsigned long long spare[BEAM_MAX]; } top[BEAM_WAVES];
     double z[BEAM_WAVES];
     float m[BEAM_WAVES];
     uint32_t border[BEAM_WAVES];
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     const T *px = x + before;
     WaveSum sum;
     sum.init(r.scale);
-    WaveList list{sh.list[wave], 0, 0, a.n_out};
+    WaveList list{sh.list[wave], sh.top[wave].spare, 0, 0, a.n_out};
     uint32_t border = 0;
     float v[16], least = -FLT_MAX, lo_top = -INFINITY, hi_top = -INFINITY;
     const int unit_a = (part * a.batches * BEAM_WAVES + wave) * WAVE_UNITS + lane;
@@ -345,7 +347,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
             for (int k = 1; k < 8; ++k) { lo = fmaxf(lo, v[k]); hi = fmaxf(hi, v[8 + k]); }
             const float top = fmaxf(lo, hi);
             lo_top = fmaxf(lo_top, lo); hi_top = fmaxf(hi_top, hi); best = fmaxf(best, top);
-            sh.top[wave][b - b0][lane] = top;
+            sh.top[wave].of[b - b0][lane] = top;
 #pragma unroll
             for (int k = 0; k < 16; k += 2) sum.bad |= __builtin_isunordered(v[k], v[k + 1]);
             sum.add(v, top);
@@ -358,7 +360,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
             border = max(border, wave_border(beam_order(lo_top), beam_order(hi_top), a.n_out, a.n_out > 8 ? 8 : 0));
             least = border > ORDER_OF_MINUS_INF ? order_logit(border) : -FLT_MAX;
             uint32_t in = 0;                                       // the lane's batches with something to take
-            for (int k = 0; k < n_round; ++k) in |= (uint32_t)(sh.top[wave][k][lane] >= least) << k;
+            for (int k = 0; k < n_round; ++k) in |= (uint32_t)(sh.top[wave].of[k][lane] >= least) << k;
 #pragma unroll 1
             while (__any(in != 0)) {
                 const int b = b0 + __ffs(in) - 1;                  // (the last one is still there)
@@ -440,10 +442,14 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
 constexpr int JOIN_EACH = 4;                                       // keys a thread
 constexpr int JOIN_KEPT = 1024;                                    // items that are kept for ordering
 
+constexpr int JOIN_SLACK = 24;                                      // ... beyond n_out that are not worth another halving
+constexpr int JOIN_STEPS = 9 + 32;
+
 struct JoinShared {
     uint32_t high[JOIN_KEPT + 8];                                  // upper halves of the values
     unsigned long long value[JOIN_KEPT], key[JOIN_KEPT], edge_value, edge_key;
-    uint32_t beam[JOIN_KEPT], edge_beam, border[16];
+    uint32_t beam[JOIN_KEPT], edge_beam, most;
+    int reach[JOIN_STEPS];
     double row_z[BEAM_MAX], row_div[BEAM_MAX];
     float row_score[BEAM_MAX], row_scale[BEAM_MAX];
     int row_kind[BEAM_MAX], row_len[BEAM_MAX], n;
@@ -457,8 +463,8 @@ __device__ __forceinline__ bool item_before(unsigned long long v, uint32_t b, un
 // grid groups, block 256, 512 or 1024: JOIN_EACH keys a thread
 __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
     __shared__ JoinShared sh;
-    const int g = blockIdx.x, tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, wave = tid >> 6, parts = a.parts;
-    const int per_row = parts * a.n_out, n = a.n_beams * per_row, waves = min(threads, n + 63) >> 6;      // those that have keys
+    const int g = blockIdx.x, tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, parts = a.parts;
+    const int per_row = parts * a.n_out, n = a.n_beams * per_row;
     const unsigned long long *keys = a.keys + (size_t)g * a.n_beams * per_row;
     unsigned long long value[JOIN_EACH], key[JOIN_EACH];
 #pragma unroll
@@ -489,7 +495,8 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
             sh.row_div[b] = a.alpha > 0.0 ? pow((double)max(len, 1), a.alpha) : 1.0;
         }
     }
-    if (tid == 0) sh.n = 0;
+    if (tid == 0) { sh.n = 0; sh.most = 0; }
+    if (tid < JOIN_STEPS) sh.reach[tid] = 0;
     __syncthreads();
     // ---- the items' values
     unsigned long long best = 0;
@@ -503,12 +510,37 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
         if (kind != BEAM_NONE && key[k]) value[k] = double_order(a.alpha > 0.0 ? v / sh.row_div[b] : v);
         best = value[k] > best ? value[k] : best;
     }
-    // a share of them in each wave: all of these reach the least of the waves' borders
-    const uint32_t wave_least = wave_border((uint32_t)(best >> 32), 0, (a.n_out + waves - 1) / waves, 12);
-    if (lane == 0) sh.border[wave] = wave_least;
+    // ---- a border, on the upper halves, that n_out items and few more reach: down from the largest in growing steps, then halving
+    const uint32_t wave_most = wave_max_u32((uint32_t)(best >> 32));
+    if (lane == 0) atomicMax(&sh.most, wave_most);
     __syncthreads();
-    uint32_t border = sh.border[0];
-    for (int w = 1; w < waves; ++w) border = min(border, sh.border[w]);
+    const uint32_t most = sh.most;
+    int step = 0;
+    auto reach = [&](uint32_t t) __attribute__((always_inline)) {
+        int c = 0;
+#pragma unroll
+        for (int k = 0; k < JOIN_EACH; ++k) c += (int)__popcll(__ballot((uint32_t)(value[k] >> 32) >= t));
+        if (lane == 0) atomicAdd(&sh.reach[step], c);
+        __syncthreads();
+        return sh.reach[step++];
+    };
+    uint32_t border = 1, above = most;
+    int reached = 0;
+    if (most > 0) {
+#pragma unroll 1
+        for (int d = 16;; d += 2) {
+            border = d < 32 && most > 1u << d ? most - (1u << d) : 1;
+            reached = reach(border);
+            if (reached >= a.n_out || border == 1) break;
+            above = border;
+        }
+#pragma unroll 1
+        while (reached > a.n_out + JOIN_SLACK && above - border > 1) {
+            const uint32_t mid = border + (above - border) / 2;
+            const int r = reach(mid);
+            if (r >= a.n_out) { border = mid; reached = r; } else above = mid;
+        }
+    }
     auto keep = [&](int k, bool in) __attribute__((always_inline)) {
         const int at = wave_place(in, &sh.n);
         if (in && at < JOIN_KEPT) { sh.high[at] = (uint32_t)(value[k] >> 32); sh.value[at] = value[k]; sh.key[at] = key[k]; sh.beam[at] = (tid + threads * k) / per_row; }
@@ -517,7 +549,7 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
     for (int k = 0; k < JOIN_EACH; ++k) keep(k, value[k] && (uint32_t)(value[k] >> 32) >= border);
     __syncthreads();
     if (sh.n > JOIN_KEPT) {
-        // too many (equals, or a wave with next to nothing): the border is the n_out-th of the threads' first items, which leaves items of n_out threads
+        // more than a thousand equals: the border is the n_out-th of the threads' first items, which leaves items of n_out threads
         unsigned long long v = 0, x = 0;
         uint32_t b = 0;
 #pragma unroll

@@ -51,19 +51,55 @@ __device__ __forceinline__ int block_scan(int v, int *sh, int &total) {
     return before;
 }
 
-// test(i) of i = 0 .. n - 1 in order; found(i, rank) for those that pass, until at least `enough` have.  Returns how many have.
-template <typename T, typename F>
-__device__ __forceinline__ int ordered(int n, int enough, int *sh, T test, F found) {
+// found(i, rank) for those i of 0 .. n - 1, in order, whose number load(i) passes test(), until at least `enough` have.  Returns how many have.
+// ORDERED_EACH numbers a thread at once, POOL_THREADS apart, so that they are requested together and side by side.
+constexpr int ORDERED_EACH = 8, ORDERED_COUNTS = ORDERED_EACH * POOL_WAVES;
+static_assert(ORDERED_COUNTS == 128, "two counts a lane");
+template <typename L, typename T, typename F>
+__device__ __forceinline__ int ordered(int n, int enough, int *sh, L load, T test, F found) {       // sh: ORDERED_COUNTS ints of LDS
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int rank = 0;
-    for (int i0 = 0; i0 < n && rank < enough; i0 += POOL_THREADS) {
-        const int i = i0 + threadIdx.x;
-        const bool yes = i < n && test(i);
-        int total;
-        const int at = block_scan(yes, sh, total);
-        if (yes) found(i, rank + at);
-        rank += total;
+    for (int i0 = 0; i0 < n && rank < enough; i0 += POOL_THREADS * ORDERED_EACH) {
+        int x[ORDERED_EACH];
+#pragma unroll
+        for (int u = 0; u < ORDERED_EACH; ++u) x[u] = load(min(i0 + POOL_THREADS * u + tid, n - 1));
+        uint32_t in = 0;
+        int before[ORDERED_EACH];
+        __syncthreads();                                           // sh may still be read from the last time round
+#pragma unroll
+        for (int u = 0; u < ORDERED_EACH; ++u) {
+            const bool yes = i0 + POOL_THREADS * u + tid < n && test(x[u]);
+            const unsigned long long who = __ballot(yes);
+            in |= (uint32_t)yes << u;
+            before[u] = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+            if (lane == 0) sh[u * POOL_WAVES + wave] = (int)__popcll(who);
+        }
+        __syncthreads();
+        const int a = sh[lane], b = sh[64 + lane], to_a = wave_scan(a), all_a = __shfl(to_a, 63, RS_WAVE), to_b = wave_scan(b) + all_a;
+#pragma unroll
+        for (int u = 0; u < ORDERED_EACH; ++u) {
+            const int c = u * POOL_WAVES + wave, at = c < 64 ? __shfl(to_a - a, c & 63, RS_WAVE) : __shfl(to_b - b, c & 63, RS_WAVE);
+            if (in >> u & 1) found(i0 + POOL_THREADS * u + tid, rank + at + before[u]);
+        }
+        rank += __shfl(to_b, 63, RS_WAVE);
     }
     return rank;
+}
+
+// Which row names a number first: a table of twice as many places as there can be rows.
+struct FirstRow { int key[2 * POOL_ROWS], row[2 * POOL_ROWS]; };
+__device__ __forceinline__ void first_clear(FirstRow &f) {
+    for (int i = threadIdx.x; i < 2 * POOL_ROWS; i += POOL_THREADS) { f.key[i] = -1; f.row[i] = POOL_ROWS; }
+}
+__device__ __forceinline__ int first_enter(FirstRow &f, int key, int row) {          // key >= 0; returns its place
+    int h = (int)((uint32_t)key * 2654435761u >> 21);
+    for (;;) {
+        const int seen = atomicCAS(&f.key[h], -1, key);
+        if (seen == -1 || seen == key) break;
+        h = (h + 1) & (2 * POOL_ROWS - 1);
+    }
+    atomicMin(&f.row[h], row);
+    return h;
 }
 
 // ---------------------------------------------------------------- rs_pages_release
@@ -96,49 +132,72 @@ __global__ void __launch_bounds__(256) k_pool_release(RangeArgs a) {
 }
 
 // ---------------------------------------------------------------- rs_pages_reserve
-// grid 1, block POOL_THREADS: the entries of all rows' ranges that name no page, in order, and the free pages, in order
+// grid 1, block POOL_THREADS.  Counts the entries that lack a page, row by row, with as many lanes a row as the longest row has entries; finds as many
+// free pages; hands them out in the same walk.
+constexpr int RESERVE_EACH = 4;                                    // entries a lane looks at together
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
-    __shared__ int sh[POOL_WAVES], slot_of[POOL_ROWS], first_of[POOL_ROWS], start[POOL_ROWS + 1], lack_end[POOL_ROWS];
-    const int tid = threadIdx.x, n = a.n;
-    // a thread a row: its range of entries
-    int slot = -1, from = 0, to = 0, len = 0, total;
+    __shared__ FirstRow first;
+    __shared__ int sh[ORDERED_COUNTS], slot_of[POOL_ROWS], entry_of[POOL_ROWS], len_of[POOL_ROWS], lack_of[POOL_ROWS], longest;
+    const int tid = threadIdx.x, lane = tid & 63, n = a.n, ps = 1 << a.p.page_shift;
+    int slot = -1, from = 0, to = 0, len = 0, place = 0;
     const bool ok = tid < n && pool_range(a, tid, slot, from, to);
-    if (tid < n) slot_of[tid] = slot;
+    first_clear(first);
+    if (tid == 0) longest = 0;
     __syncthreads();
-    bool again = false;
-    for (int i = 0; i < tid && tid < n; ++i) again |= slot_of[i] == slot;
-    if (tid < n && (!ok || again)) pool_flag(a.p, tid, RS_FLAG_BADARG);
-    const int ps = 1 << a.p.page_shift, e0 = from >> a.p.page_shift;
-    if (ok && !again && to > from) len = ((to + ps - 1) >> a.p.page_shift) - e0;
-    // (the entries of a call are no more than rows times table entries, below 2^31 as checked on the host)
-    const int at = block_scan(len, sh, total);
-    if (tid < n) { first_of[tid] = e0; start[tid] = at; lack_end[tid] = 0; }
-    if (tid == 0) start[n] = total;
+    if (tid < n && slot >= 0) place = first_enter(first, slot, tid);
     __syncthreads();
-    auto place = [&](int i, int &row) {                             // entry i of the call
-        int lo = 0, hi = n;
-        while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (start[mid] <= i) lo = mid; else hi = mid; }
-        row = lo;
-        return a.p.table + (size_t)slot_of[lo] * a.p.max_pages + first_of[lo] + (i - start[lo]);
+    if (tid < n) {
+        if (!ok || first.row[place] != tid) pool_flag(a.p, tid, RS_FLAG_BADARG);
+        else if (to > from) len = ((to + ps - 1) >> a.p.page_shift) - (from >> a.p.page_shift);
+        slot_of[tid] = slot; entry_of[tid] = from >> a.p.page_shift; len_of[tid] = len;
+        if (len) atomicMax(&longest, len);
+    }
+    __syncthreads();
+    if (!longest) return;
+    int shift = 0;
+    while (shift < 6 && 1 << shift < longest) ++shift;
+    const int lanes = 1 << shift, sub = lane & (lanes - 1), base = lane - sub;
+    const unsigned long long mates = (lanes == 64 ? ~0ull : (1ull << lanes) - 1) << base;
+    // f(entry, rank of it among the row's that lack a page) for each of those; returns how many there are
+    auto walk = [&](int r, auto f) __attribute__((always_inline)) {
+        int *row = a.p.table + (size_t)slot_of[r] * a.p.max_pages + entry_of[r], rank = 0;
+        const int m = len_of[r];
+        for (int e0 = 0; e0 < m; e0 += lanes * RESERVE_EACH) {
+            int page[RESERVE_EACH];
+#pragma unroll
+            for (int u = 0; u < RESERVE_EACH; ++u) page[u] = row[min(e0 + lanes * u + sub, m - 1)];
+#pragma unroll
+            for (int u = 0; u < RESERVE_EACH; ++u) {
+                const int e = e0 + lanes * u + sub;
+                const bool lacks = e < m && !is_page(a.p, page[u]);
+                const unsigned long long who = __ballot(lacks) & mates;
+                if (lacks) f(row + e, rank + (int)__popcll(who & ((1ull << lane) - 1)));
+                rank += (int)__popcll(who);
+            }
+        }
+        return rank;
     };
-    // how many entries lack a page, up to the end of each row
-    auto lacks = [&](int i) { int row; return !is_page(a.p, *place(i, row)); };
-    const int lack = ordered(total, 0x7fffffff, sh, lacks, [&](int i, int rank) { int row; (void)place(i, row); atomicMax(&lack_end[row], rank + 1); });
-    if (lack == 0) return;
+    for (int r = tid >> shift; r < n; r += POOL_THREADS >> shift) {
+        const int lack = walk(r, [](int *, int) {});
+        if (sub == 0) lack_of[r] = lack;
+    }
     __syncthreads();
-    const int have = ordered(a.p.n_pages, lack, sh, [&](int i) { return ref_load(a.p.ref + i) == 0; },
-                             [&](int i, int rank) { if (rank < lack) __hip_atomic_store(a.list + rank, i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
+    int wanted;
+    const int mine = tid < n ? lack_of[tid] : 0, before = block_scan(mine, sh, wanted);
+    if (!wanted) return;
+    const int have = ordered(a.p.n_pages, wanted, sh, [&](int i) { return a.p.ref[i]; }, [](int count) { return count == 0; },
+                             [&](int i, int rank) { if (rank < wanted) a.list[rank] = i; });
+    if (tid < n && mine && before + mine > have) { pool_flag(a.p, tid, RS_FLAG_NO_PAGE); len_of[tid] = 0; }
+    if (tid < n) lack_of[tid] = before;
     refs_settled();
-    if (tid < n && lack_end[tid] > have) pool_flag(a.p, tid, RS_FLAG_NO_PAGE);
-    // (a row's entries are looked at and filled in the same order by the same threads)
-    ordered(total, 0x7fffffff, sh, lacks, [&](int i, int rank) {
-        int row;
-        int *entry = place(i, row);
-        if (lack_end[row] > have) return;
-        const int page = __hip_atomic_load(a.list + rank, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        *entry = page;
-        ref_store(a.p.ref + page, 1);
-    });
+    for (int r = tid >> shift; r < n; r += POOL_THREADS >> shift) {
+        const int at = lack_of[r];
+        walk(r, [&](int *entry, int rank) {
+            const int page = __hip_atomic_load(a.list + at + rank, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *entry = page;
+            ref_store(a.p.ref + page, 1);
+        });
+    }
 }
 
 // ---------------------------------------------------------------- moving pages
@@ -152,53 +211,50 @@ struct CopyArgs {
     const PageMove *moves; const int *n_moves;                     // on the device; or
     const int *src, *dst; int n;                                   // pairs of the caller
     const int *map;                                                // not null: table entries follow it (k_pool_compact)
+    int pieces;                                                    // of a page's K or V of one layer, COPY_UNITS * 256 units each
 };
 
 constexpr int COPY_UNITS = 4;                                      // 16-byte units a thread
 
-// One piece of a page's K or V of one layer: units u0 + tid, ... of 16 bytes.
-__device__ __forceinline__ void copy_piece(const Pool &p, const uint16_t *src, uint16_t *dst, int part, bool is_v, int u0) {
-    const int ps = 1 << p.page_shift, row = is_v ? part / 8 : part * p.head_dim / 8, gap = is_v ? ps / 8 : ps * p.head_dim / 8;
-    const int units = (is_v ? p.n_kv * p.head_dim : p.n_kv) * row;
-    uint4 x[COPY_UNITS];
-    int at[COPY_UNITS];
-#pragma unroll
-    for (int i = 0; i < COPY_UNITS; ++i) {
-        const int u = u0 + threadIdx.x + 256 * i;
-        at[i] = u >= units ? -1 : part == ps ? u : u / row * gap + u % row;
-        if (at[i] >= 0) x[i] = reinterpret_cast<const uint4 *>(src)[at[i]];
-    }
-#pragma unroll
-    for (int i = 0; i < COPY_UNITS; ++i)
-        if (at[i] >= 0) reinterpret_cast<uint4 *>(dst)[at[i]] = x[i];
-}
-
-// grid any, block 256
+// grid (pieces * 2 * layers, any): a workgroup has its piece of every gridDim.y-th move.
+// A part of a page: of K the first `part` places of every head, of V the first `part` places of every channel.
 __global__ void __launch_bounds__(256) k_pool_copy(CopyArgs a) {
     const Pool &p = a.to;
-    const int ps = 1 << p.page_shift;
+    const int tid = threadIdx.x, ps = 1 << p.page_shift;
     if (a.map) {
-        const size_t entries = (size_t)p.n_slots * p.max_pages;
-        for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += (size_t)gridDim.x * 256) {
+        const long long entries = (long long)p.n_slots * p.max_pages, threads = (long long)gridDim.x * gridDim.y * 256;
+        for (long long i = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + tid; i < entries; i += threads) {
             const int page = p.table[i];
             if (is_page(p, page)) p.table[i] = a.map[page];
         }
     }
+    const int piece = blockIdx.x % a.pieces, half = blockIdx.x / a.pieces, layer = half >> 1;
+    const bool is_v = half & 1;
     const size_t page_values = (size_t)p.n_kv * p.head_dim << p.page_shift;
-    const int pieces = (int)((page_values / 8 + 256 * COPY_UNITS - 1) / (256 * COPY_UNITS));
-    const int n = a.moves ? *a.n_moves : a.n;
-    const long long items = (long long)n * p.n_layers * 2 * pieces;
-    for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-        const int piece = (int)(it % pieces), kv = (int)(it / pieces % 2), layer = (int)(it / pieces / 2 % p.n_layers), m = (int)(it / pieces / 2 / p.n_layers);
+    const u32x4_t *from = reinterpret_cast<const u32x4_t *>((is_v ? a.v : a.k) + (size_t)layer * a.from_pages * page_values);
+    u32x4_t *to = reinterpret_cast<u32x4_t *>((is_v ? p.v : p.k) + (size_t)layer * p.n_pages * page_values);
+    const int gap = is_v ? ps / 8 : ps / 8 * p.head_dim, rows = is_v ? p.n_kv * p.head_dim : p.n_kv, n = a.moves ? *a.n_moves : a.n;
+    for (int m = blockIdx.y; m < n; m += gridDim.y) {
         PageMove mv;
         if (a.moves) mv = a.moves[m];
         else {
             mv = {a.src[m], a.dst[m], ps, m};
-            if (mv.src < 0 || mv.src >= a.from_pages || !is_page(p, mv.dst)) { if (piece == 0 && kv == 0 && layer == 0 && threadIdx.x == 0) pool_flag(p, m, RS_FLAG_BADARG); continue; }
+            if (mv.src < 0 || mv.src >= a.from_pages || !is_page(p, mv.dst)) { if (blockIdx.x == 0 && tid == 0) pool_flag(p, m, RS_FLAG_BADARG); continue; }
         }
-        const uint16_t *src = (kv ? a.v : a.k) + ((size_t)layer * a.from_pages + mv.src) * page_values;
-        uint16_t *dst = (kv ? p.v : p.k) + ((size_t)layer * p.n_pages + mv.dst) * page_values;
-        if (src != dst) copy_piece(p, src, dst, mv.part, kv, piece * 256 * COPY_UNITS);
+        const u32x4_t *x = from + (size_t)mv.src * (page_values / 8);
+        u32x4_t *y = to + (size_t)mv.dst * (page_values / 8);
+        const int row = mv.part / 8 * (is_v ? 1 : p.head_dim), units = rows * row, u0 = piece * (256 * COPY_UNITS) + tid;
+        if (piece * (256 * COPY_UNITS) >= units || x == y) continue;
+        u32x4_t w[COPY_UNITS];
+        int at[COPY_UNITS];
+#pragma unroll
+        for (int i = 0; i < COPY_UNITS; ++i) {
+            const int u = min(u0 + 256 * i, units - 1);
+            at[i] = mv.part == ps ? u : u + u / row * (gap - row);
+            w[i] = x[at[i]];
+        }
+#pragma unroll
+        for (int i = 0; i < COPY_UNITS; ++i) if (u0 + 256 * i < units) y[at[i]] = w[i];
     }
 }
 
@@ -210,17 +266,20 @@ constexpr int FORK_EACH = 8;                                       // table entr
 // grid 1, block POOL_THREADS.  Reads everything before it writes a table entry: whether all rows are in range, the counts after the call, the rows that
 // need a page, the pages they get.
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
-    __shared__ int sh[POOL_WAVES], slot_of[POOL_ROWS], from_of[POOL_ROWS], whole_of[POOL_ROWS], tail_page[POOL_ROWS], new_page[POOL_ROWS], want_row[POOL_ROWS];
+    __shared__ FirstRow first;
+    __shared__ int sh[ORDERED_COUNTS], slot_of[POOL_ROWS], from_of[POOL_ROWS], whole_of[POOL_ROWS], new_page[POOL_ROWS], want_row[POOL_ROWS];
     const Pool &p = a.p;
     const int tid = threadIdx.x, n = a.n_groups * a.n_beams, mp = p.max_pages, ps = 1 << p.page_shift;
-    if (tid < n) slot_of[tid] = a.slot[tid];
+    const int slot = tid < n ? a.slot[tid] : -1, parent = tid < n ? a.parent[tid] : -1;
+    first_clear(first);
+    __syncthreads();
+    int place = 0;
+    if (tid < n) { slot_of[tid] = slot; if (slot >= 0) place = first_enter(first, slot, tid); }
     __syncthreads();
     // ---- a thread a row: its parent's slot and positions
     int bad = 0, from = -1, pos = 0, tail = 0, whole = 0, page = -1;
     if (tid < n) {
-        const int slot = slot_of[tid], parent = a.parent[tid];
-        bad = slot < 0 || slot >= p.n_slots || parent >= a.n_beams;
-        for (int i = 0; i < tid; ++i) bad |= slot_of[i] == slot;
+        bad = slot < 0 || slot >= p.n_slots || parent >= a.n_beams || first.row[place] != tid;
         if (!bad && parent >= 0) {
             const int q = tid / a.n_beams * a.n_beams + parent;
             from = slot_of[q]; pos = a.pos[q];
@@ -232,9 +291,11 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
     if (__syncthreads_or(bad)) { if (tid == 0) *a.n_moves = 0; return; }
     if (tid < n) {
         if (from >= 0 && tail) { page = p.table[(size_t)from * mp + whole]; if (!is_page(p, page)) page = -1; }
-        from_of[tid] = from; whole_of[tid] = whole; tail_page[tid] = page;
+        from_of[tid] = from; whole_of[tid] = whole;
     }
+    first_clear(first);                                            // (all have read it before the last barrier)
     __syncthreads();
+    if (page >= 0) place = first_enter(first, page, tid);
     // ---- counts: what the rows held goes, the whole pages of their parents come
     const long long entries = (long long)n * mp;
     auto count = [&](int by) {
@@ -249,11 +310,7 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
     };
     count(1);
     // ---- the last page of a parent: the first row that wants it keeps it if nobody else has it
-    bool keep = false;
-    if (page >= 0) {
-        keep = ref_load(p.ref + page) == 0;
-        for (int i = 0; i < tid && keep; ++i) keep = tail_page[i] != page;
-    }
+    const bool keep = page >= 0 && first.row[place] == tid && ref_load(p.ref + page) == 0;
     __syncthreads();                                               // (all have looked before the first count changes)
     if (keep) ref_store(p.ref + page, 1);
     const bool want = page >= 0 && !keep;
@@ -262,7 +319,8 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
     if (tid < n) new_page[tid] = keep ? page : -1;
     if (want) want_row[rank] = tid;
     refs_settled();
-    const int have = ordered(p.n_pages, wanted, sh, [&](int i) { return ref_load(p.ref + i) == 0; }, [&](int i, int k) { if (k < wanted) new_page[want_row[k]] = i; });
+    const int have = ordered(p.n_pages, wanted, sh, [&](int i) { return ref_load(p.ref + i); }, [](int count) { return count == 0; },
+                             [&](int i, int k) { if (k < wanted) new_page[want_row[k]] = i; });
     __syncthreads();
     if (have < wanted) {                                           // as before the call
         if (keep) ref_store(p.ref + page, 0);
@@ -305,15 +363,15 @@ struct CompactArgs { Pool p; int *used; PageMove *moves; int *n_moves, *map, *ga
 
 // grid 1, block POOL_THREADS: used pages from the number of used pages on, in order, go to the free ones below it, in order
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_compact(CompactArgs a) {
-    __shared__ int sh[POOL_WAVES];
+    __shared__ int sh[ORDERED_COUNTS];
     const Pool &p = a.p;
     const int tid = threadIdx.x;
     int mine = 0, used;
     for (int i = tid; i < p.n_pages; i += POOL_THREADS) { mine += p.ref[i] != 0; a.map[i] = i; }
     (void)block_scan(mine, sh, used);
-    ordered(used, 0x7fffffff, sh, [&](int i) { return p.ref[i] == 0; }, [&](int i, int k) { a.gaps[k] = i; });
+    ordered(used, 0x7fffffff, sh, [&](int i) { return p.ref[i]; }, [](int count) { return count == 0; }, [&](int i, int k) { a.gaps[k] = i; });
     refs_settled();
-    const int n = ordered(p.n_pages - used, 0x7fffffff, sh, [&](int i) { return p.ref[used + i] != 0; }, [&](int i, int k) {
+    const int n = ordered(p.n_pages - used, 0x7fffffff, sh, [&](int i) { return p.ref[used + i]; }, [](int count) { return count != 0; }, [&](int i, int k) {
         const int from = used + i, to = __hip_atomic_load(a.gaps + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         a.moves[k] = {from, to, 1 << p.page_shift, k};
         a.map[from] = to;
