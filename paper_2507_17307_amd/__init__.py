@@ -16,3 +16,4 @@ from .binding import (  # noqa: F401
     rs_beam_select, rs_beam_select_scratch_bytes, PagePool, rs_pages_scratch_bytes, rs_pages_reserve, rs_pages_release, rs_pages_fork, rs_pages_copy, rs_pages_compact,
     Model, PagedModel,
 )
+from .beam import Beam, BeamSearch  # noqa: F401

@@ -661,7 +661,8 @@ class PagedModel(Model):
     reserve(slot, positions) gives a slot the pages for its first `positions` positions (the calls do not do it by
     themselves: the tokens a call feeds need their pages before it, and a sequence without them is flagged and left as it
     is), release(slot) gives them back.  Both write the page table
-    on the current stream, after which calls on that stream see it."""
+    on the current stream, after which calls on that stream see it.  page_pool() hands the pages over to the calls on
+    pools of pages (rs_pages_reserve and the others), for sequences that branch; reserve and release are theirs from then on."""
 
     def __init__(self, weights, max_ctx: int, n_pages: int, page_size: int = 64, max_seqs: int = 1, max_rows: int = 64, device="cuda"):
         self.handle = 0
@@ -684,9 +685,24 @@ class PagedModel(Model):
         self.device = device
         self._free = list(range(n_pages - 1, -1, -1))
         self._held: List[List[int]] = [[] for _ in range(max_seqs)]
+        self._pool: Optional[PagePool] = None
         self.handle = rs_create_model_paged(self.cfg, weights, self.cache_struct, self.workspace)
 
+    def page_pool(self) -> PagePool:
+        """The pool over this model's pages and page table, with the pages that the slots hold counted."""
+        if self._pool is None:
+            count = torch.zeros(self.n_pages, dtype=torch.int32)
+            for held in self._held:
+                count[held] = 1
+            self._pool = PagePool(self.page_table, count.to(self.device), self.page_size, self.pages_k, self.pages_v)
+        return self._pool
+
+    def _host_pages(self) -> None:
+        if self._pool is not None:
+            raise RsError(-1, "the pages are a pool's: use rs_pages_reserve and rs_pages_release")
+
     def reserve(self, slot: int, positions: int) -> None:
+        self._host_pages()
         if not 0 <= slot < len(self._held):
             raise RsError(-1, f"slot {slot} out of range")
         held, more = self._held[slot], (positions + self.page_size - 1) // self.page_size - len(self._held[slot])
@@ -701,6 +717,7 @@ class PagedModel(Model):
         self.page_table[slot, at:len(held)] = self._i32(held[at:])
 
     def release(self, slot: int) -> None:
+        self._host_pages()
         if not 0 <= slot < len(self._held):
             raise RsError(-1, f"slot {slot} out of range")
         held = self._held[slot]
@@ -710,6 +727,7 @@ class PagedModel(Model):
 
     def kv_view(self, which: str, slot: int = 0) -> torch.Tensor:
         """[layer, kv_head, position, head_dim]: a copy of the positions of a slot's pages, in order."""
-        pages = torch.tensor(self._held[slot], dtype=torch.long, device=self.device)
+        held = self._held[slot] if self._pool is None else [p for p in self.page_table[slot].tolist() if p >= 0]
+        pages = torch.tensor(held, dtype=torch.long, device=self.device)
         t = self.pages_k[:, pages] if which == "k" else self.pages_v[:, pages].transpose(3, 4)
         return t.transpose(1, 2).flatten(2, 3)

@@ -58,11 +58,17 @@ static_assert(ORDERED_COUNTS == 128, "two counts a lane");
 template <typename L, typename T, typename F>
 __device__ __forceinline__ int ordered(int n, int enough, int *sh, L load, T test, F found) {       // sh: ORDERED_COUNTS ints of LDS
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int rank = 0;
-    for (int i0 = 0; i0 < n && rank < enough; i0 += POOL_THREADS * ORDERED_EACH) {
+    constexpr int STEP = POOL_THREADS * ORDERED_EACH;
+    int rank = 0, next[ORDERED_EACH];
+#pragma unroll
+    for (int u = 0; u < ORDERED_EACH; ++u) next[u] = n > 0 ? load(min(POOL_THREADS * u + tid, n - 1)) : 0;
+    for (int i0 = 0; i0 < n && rank < enough; i0 += STEP) {
         int x[ORDERED_EACH];
 #pragma unroll
-        for (int u = 0; u < ORDERED_EACH; ++u) x[u] = load(min(i0 + POOL_THREADS * u + tid, n - 1));
+        for (int u = 0; u < ORDERED_EACH; ++u) {
+            x[u] = next[u];
+            if (i0 + STEP < n) next[u] = load(min(i0 + STEP + POOL_THREADS * u + tid, n - 1));
+        }
         uint32_t in = 0;
         int before[ORDERED_EACH];
         __syncthreads();                                           // sh may still be read from the last time round
@@ -132,17 +138,17 @@ __global__ void __launch_bounds__(256) k_pool_release(RangeArgs a) {
 }
 
 // ---------------------------------------------------------------- rs_pages_reserve
-// grid 1, block POOL_THREADS.  Counts the entries that lack a page, row by row, with as many lanes a row as the longest row has entries; finds as many
-// free pages; hands them out in the same walk.
-constexpr int RESERVE_EACH = 4;                                    // entries a lane looks at together
+// grid 1, block POOL_THREADS.  Counts the entries that lack a page, row by row, with as many lanes a row as take the longest one in at once; finds as
+// many free pages; hands them out in the same walk.
+constexpr int RESERVE_EACH = 8;                                    // entries a lane looks at together
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
     __shared__ FirstRow first;
-    __shared__ int sh[ORDERED_COUNTS], slot_of[POOL_ROWS], entry_of[POOL_ROWS], len_of[POOL_ROWS], lack_of[POOL_ROWS], longest;
+    __shared__ int sh[ORDERED_COUNTS], slot_of[POOL_ROWS], entry_of[POOL_ROWS], len_of[POOL_ROWS], lack_of[POOL_ROWS], longest, taken;
     const int tid = threadIdx.x, lane = tid & 63, n = a.n, ps = 1 << a.p.page_shift;
     int slot = -1, from = 0, to = 0, len = 0, place = 0;
     const bool ok = tid < n && pool_range(a, tid, slot, from, to);
     first_clear(first);
-    if (tid == 0) longest = 0;
+    if (tid == 0) longest = taken = 0;
     __syncthreads();
     if (tid < n && slot >= 0) place = first_enter(first, slot, tid);
     __syncthreads();
@@ -155,7 +161,7 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
     __syncthreads();
     if (!longest) return;
     int shift = 0;
-    while (shift < 6 && 1 << shift < longest) ++shift;
+    while (shift < 6 && RESERVE_EACH << shift < longest) ++shift;
     const int lanes = 1 << shift, sub = lane & (lanes - 1), base = lane - sub;
     const unsigned long long mates = (lanes == 64 ? ~0ull : (1ull << lanes) - 1) << base;
     // f(entry, rank of it among the row's that lack a page) for each of those; returns how many there are
@@ -185,18 +191,20 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
     int wanted;
     const int mine = tid < n ? lack_of[tid] : 0, before = block_scan(mine, sh, wanted);
     if (!wanted) return;
+    // (a page is counted where it is found, side by side with its neighbours; 16000 counts set where the entries are written took 7 us more)
     const int have = ordered(a.p.n_pages, wanted, sh, [&](int i) { return a.p.ref[i]; }, [](int count) { return count == 0; },
-                             [&](int i, int rank) { if (rank < wanted) a.list[rank] = i; });
-    if (tid < n && mine && before + mine > have) { pool_flag(a.p, tid, RS_FLAG_NO_PAGE); len_of[tid] = 0; }
-    if (tid < n) lack_of[tid] = before;
+                             [&](int i, int rank) { if (rank < wanted) { a.list[rank] = i; a.p.ref[i] = 1; } });
+    if (tid < n) {
+        const bool served = before + mine <= have;
+        if (mine && !served) { pool_flag(a.p, tid, RS_FLAG_NO_PAGE); len_of[tid] = 0; }
+        if (mine && served) atomicMax(&taken, before + mine);
+        lack_of[tid] = before;
+    }
     refs_settled();
+    for (int i = taken + tid; i < min(have, wanted); i += POOL_THREADS) a.p.ref[__hip_atomic_load(a.list + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)] = 0;
     for (int r = tid >> shift; r < n; r += POOL_THREADS >> shift) {
         const int at = lack_of[r];
-        walk(r, [&](int *entry, int rank) {
-            const int page = __hip_atomic_load(a.list + at + rank, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            *entry = page;
-            ref_store(a.p.ref + page, 1);
-        });
+        walk(r, [&](int *entry, int rank) { *entry = __hip_atomic_load(a.list + at + rank, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
     }
 }
 
@@ -215,6 +223,10 @@ struct CopyArgs {
 };
 
 constexpr int COPY_UNITS = 4;                                      // 16-byte units a thread
+// Places of a channel of V that are written together: 128 bytes.  Writing part of such a line costs more than twice as much as all of it, so the places
+// behind the part are read from where they go to and written again (70 parts of pages of the 7B shape, 8 / 16 / 24 / 40 / 56 of 64 places: the part alone
+// 150 / 153 / 126 / 135 / 150 us, whole halves of a line 134 / 139 / 144 / 106 / 123, whole lines 89 / 91 / 95 / 106 / 124; whole pages 105).
+constexpr int COPY_BLOCK = 64;
 
 // grid (pieces * 2 * layers, any): a workgroup has its piece of every gridDim.y-th move.
 // A part of a page: of K the first `part` places of every head, of V the first `part` places of every channel.
@@ -243,15 +255,16 @@ __global__ void __launch_bounds__(256) k_pool_copy(CopyArgs a) {
         }
         const u32x4_t *x = from + (size_t)mv.src * (page_values / 8);
         u32x4_t *y = to + (size_t)mv.dst * (page_values / 8);
-        const int row = mv.part / 8 * (is_v ? 1 : p.head_dim), units = rows * row, u0 = piece * (256 * COPY_UNITS) + tid;
+        const int own = mv.part / 8, row = is_v ? min(ps, (mv.part + COPY_BLOCK - 1) / COPY_BLOCK * COPY_BLOCK) / 8 : own * p.head_dim;
+        const int units = rows * row, u0 = piece * (256 * COPY_UNITS) + tid;
         if (piece * (256 * COPY_UNITS) >= units || x == y) continue;
         u32x4_t w[COPY_UNITS];
         int at[COPY_UNITS];
 #pragma unroll
         for (int i = 0; i < COPY_UNITS; ++i) {
-            const int u = min(u0 + 256 * i, units - 1);
-            at[i] = mv.part == ps ? u : u + u / row * (gap - row);
-            w[i] = x[at[i]];
+            const int u = min(u0 + 256 * i, units - 1), r = row == gap ? 0 : u / row;
+            at[i] = u + r * (gap - row);
+            w[i] = (is_v && (row == gap ? u % gap : u - r * row) >= own ? y : x)[at[i]];
         }
 #pragma unroll
         for (int i = 0; i < COPY_UNITS; ++i) if (u0 + 256 * i < units) y[at[i]] = w[i];
