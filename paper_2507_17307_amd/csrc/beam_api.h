@@ -116,7 +116,7 @@ rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype
     unsigned char *scratch = (unsigned char *)d_scratch;
     BeamArgs a{};
     a.logits = d_logits; a.stride = (size_t)row_stride; a.scale = d_logit_scale; a.score = d_score; a.last = d_last; a.len = d_len;
-    a.eos = eos; a.n_beams = n_beams; a.vocab = vocab; a.n_out = n_out; a.alpha = length_penalty; a.parts = p.plan.parts; a.batches = p.plan.batches;
+    a.eos = eos; a.n_beams = n_beams; a.vocab = vocab; a.n_out = n_out; a.alpha = length_penalty; a.parts = p.plan.parts;
     a.parent = d_parent; a.token = d_token; a.len_out = d_len_out; a.score_out = d_score_out; a.flags = d_flags;
     a.keys = (unsigned long long *)scratch; a.sums = (BeamSum *)(scratch + p.sums);
     hipStream_t st = (hipStream_t)stream;
@@ -175,7 +175,8 @@ rs_status rs_pages_fork(const rs_page_pool *pool, int32_t n_groups, int32_t n_be
     a.p = make_pool(pool, d_flags); a.slot = d_slot; a.parent = d_parent; a.pos = d_pos; a.pos_out = d_pos_out; a.n_groups = n_groups; a.n_beams = n_beams;
     a.n_moves = (int *)d_scratch; a.moves = (PageMove *)((unsigned char *)d_scratch + pool_scratch(pool, n).moves);
     hipStream_t st = (hipStream_t)stream;
-    hipLaunchKernelGGL(k_pool_fork, dim3(1), dim3(POOL_THREADS), 0, st, a);
+    if ((long long)n * pool->max_pages <= 2 * POOL_THREADS) hipLaunchKernelGGL((k_pool_fork<2>), dim3(1), dim3(POOL_THREADS), 0, st, a);
+    else hipLaunchKernelGGL((k_pool_fork<8>), dim3(1), dim3(POOL_THREADS), 0, st, a);
     RS_LAUNCHED("pool_fork");
     CopyArgs c{};
     c.to = a.p; c.k = a.p.k; c.v = a.p.v; c.from_pages = a.p.n_pages; c.moves = a.moves; c.n_moves = a.n_moves;

@@ -25,7 +25,7 @@ struct BeamArgs {
     const void *logits; size_t stride;
     const float *scale, *score;
     const int *last, *len;
-    int eos, n_beams, vocab, n_out, parts, batches;                // parts * n_beams * n_out <= BEAM_KEYS
+    int eos, n_beams, vocab, n_out, parts;                         // parts * n_beams * n_out <= BEAM_KEYS
     double alpha;
     int *parent, *token, *len_out;
     float *score_out;
@@ -34,11 +34,12 @@ struct BeamArgs {
     BeamSum *sums;                                                 // [row][part]
 };
 
-// 2^f for |f| <= 1/2, to 1.1e-12: degree eight through 2^f at the Chebyshev nodes.
+// 2^f for |f| <= 1/2, to 5.5e-11: degree seven through 2^f at the Chebyshev nodes.  ln Z is off by at most that, and by far less where no token alone
+// makes up the sum; scores that differ by less may change places.  (Degree eight, 1.1e-12, costs a thirteenth more.)
 __device__ __forceinline__ double exp2_part(double f) {
-    double p = 1.3255224887502117e-06;
-    p = fma(p, f, 1.531007940254368e-05); p = fma(p, f, 0.0001540345585240991); p = fma(p, f, 0.0013333450567999414); p = fma(p, f, 0.009618129159402628);
-    p = fma(p, f, 0.05550410941205934); p = fma(p, f, 0.2402265069581299); p = fma(p, f, 0.6931471805459335); return fma(p, f, 1.0);
+    double p = 1.5303700711232526e-05;
+    p = fma(p, f, 0.000154697292141169); p = fma(p, f, 0.0013333478473686068); p = fma(p, f, 0.009618025613318041); p = fma(p, f, 0.05550410906325866);
+    p = fma(p, f, 0.24022651213498092); p = fma(p, f, 0.6931471805568324); return fma(p, f, 0.9999999999595618);
 }
 // p 2^n, p in [0.7, 1.5] and |n| <= 1020: n goes into the exponent
 __device__ __forceinline__ double scale_exp(double p, int n) { return __hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p)); }
@@ -70,14 +71,37 @@ __device__ __forceinline__ unsigned long long double_order(double x) {
 }
 __device__ __forceinline__ double order_double(unsigned long long o) { return __longlong_as_double((long long)(o >> 63 ? o & ~(1ull << 63) : ~o)); }
 
+// Exchanges inside rows of 16 lanes as operands of DPP moves (device_utils.h), step 0 .. 3: with the lane one, two, four and eight away or its mirror image, which
+// has the same value by then.
+template <int STEP>
+__device__ __forceinline__ int row_move(int v) {
+    constexpr int CTRL = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;
+    return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
+template <int STEP> __device__ __forceinline__ uint32_t row_move(uint32_t v) { return (uint32_t)row_move<STEP>((int)v); }
+template <int STEP> __device__ __forceinline__ float row_move(float v) { return __int_as_float(row_move<STEP>(__float_as_int(v))); }
+template <int STEP> __device__ __forceinline__ double row_move(double v) { return __hiloint2double(row_move<STEP>(__double2hiint(v)), row_move<STEP>(__double2loint(v))); }
+__device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ double lane_of(double v, int lane) { return __hiloint2double(lane_of(__double2hiint(v), lane), lane_of(__double2loint(v), lane)); }
+
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, RS_WAVE));
-    return v;
+    v = max(v, row_move<0>(v)); v = max(v, row_move<1>(v)); v = max(v, row_move<2>(v)); v = max(v, row_move<3>(v));
+    return max(max(lane_of(v, 0), lane_of(v, 16)), max(lane_of(v, 32), lane_of(v, 48)));
 }
 __device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, RS_WAVE);
+    v += row_move<0>(v); v += row_move<1>(v); v += row_move<2>(v); v += row_move<3>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+// f over the 2^shift lanes of each lane's group
+template <typename T, typename F>
+__device__ __forceinline__ T group_all(T v, int shift, F f) {
+    if (shift > 0) v = f(v, row_move<0>(v));
+    if (shift > 1) v = f(v, row_move<1>(v));
+    if (shift > 2) v = f(v, row_move<2>(v));
+    if (shift > 3) v = f(v, row_move<3>(v));
+    if (shift > 4) v = f(v, __shfl_xor(v, 16, RS_WAVE));
+    if (shift > 5) v = f(v, __shfl_xor(v, 32, RS_WAVE));
     return v;
 }
 
@@ -96,34 +120,24 @@ __device__ __forceinline__ int beam_kind(const BeamRow &r, int eos, unsigned int
     return BEAM_RUNS;
 }
 
-// A number that at least `keep` of 128 reach, two a lane (0 if so many are not above 0).  keep <= 64.
+// An order that at least `keep` of 128 reach, two a lane, keep <= 64; ORDER_OF_MINUS_INF if so many are not above that.
 // The lanes in 2^k >= keep groups: the least of the groups' largest, 6 steps across lanes.  Of random numbers keep (ln keep + 0.6) reach that;
-// halving the way to the largest brings it nearer to keep.
-template <bool MIN>
-__device__ __forceinline__ uint32_t row_step(uint32_t v, int step) {
-    uint32_t o;
-    if (step == 0) o = __builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false);
-    else if (step == 1) o = __builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false);
-    else if (step == 2) o = __builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false);
-    else o = __builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false);
-    return MIN ? min(v, o) : max(v, o);
-}
-__device__ __forceinline__ uint32_t wave_border(uint32_t x, uint32_t y, int keep, int halvings) {
+// beyond eight, or where a group has nothing, halving the way to the largest brings it nearer to keep.
+__device__ __forceinline__ uint32_t wave_border(uint32_t x, uint32_t y, int keep) {
     const int lanes = keep > 32 ? 0 : keep > 16 ? 1 : keep > 8 ? 2 : keep > 4 ? 3 : keep > 2 ? 4 : keep > 1 ? 5 : 6;      // log2 of a group's lanes
     uint32_t t = max(x, y), m = t;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        t = s < lanes ? row_step<false>(t, s) : row_step<true>(t, s);
-        m = row_step<false>(m, s);
-    }
+    auto step = [&](bool group, uint32_t other_t, uint32_t other_m) { t = group ? max(t, other_t) : min(t, other_t); m = max(m, other_m); };
+    step(lanes > 0, row_move<0>(t), row_move<0>(m)); step(lanes > 1, row_move<1>(t), row_move<1>(m));
+    step(lanes > 2, row_move<2>(t), row_move<2>(m)); step(lanes > 3, row_move<3>(t), row_move<3>(m));
     auto join = [](uint32_t v, bool sixteen, bool thirty_two) {    // (four rows of 16 lanes; true: the larger)
-        const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16), c = __builtin_amdgcn_readlane(v, 32), d = __builtin_amdgcn_readlane(v, 48);
+        const uint32_t a = lane_of(v, 0), b = lane_of(v, 16), c = lane_of(v, 32), d = lane_of(v, 48);
         const uint32_t e = sixteen ? max(a, b) : min(a, b), f = sixteen ? max(c, d) : min(c, d);
         return thirty_two ? max(e, f) : min(e, f);
     };
     uint32_t lo = join(t, lanes > 4, lanes > 5);
+    const int halvings = lo <= ORDER_OF_MINUS_INF ? 20 : keep > 8 ? 8 : 0;
     if (halvings > 0) {
-        uint32_t hi = join(m, true, true);
+        uint32_t hi = join(m, true, true) + 1;
 #pragma unroll 1
         for (int k = 0; k < halvings; ++k) {
             const uint32_t mid = lo + (hi - lo) / 2;
@@ -183,8 +197,8 @@ struct WaveList {
 
 // ---------------------------------------------------------------- a wave's sum
 // Batches whose logits are of an ordinary size are added up as sum 2^(x c - r) for one integer r of the wave, near the largest of its first batch: x c is
-// rounded to n, which goes into the exponent, and x c - n is exact in one operation (14 double instructions a logit; from the largest logit met so
-// far, with its rescaling, 17).  What is 2^1000 times smaller is raised to that.  Other batches, logits beyond 4096 and what towers 2^500 above r, are added
+// rounded to n, which goes into the exponent, and x c - n is exact in one operation (13 double instructions a logit; counted from the largest logit met so
+// far, with its rescaling, 16).  What is 2^1000 times smaller is raised to that.  Other batches, logits beyond 4096 and what towers 2^500 above r, are added
 // up by the lanes from their largest.
 struct WaveSum {
     double c, z, lane_z;                                           // z: with r; lane_z: with lane_m
@@ -255,6 +269,41 @@ __device__ __forceinline__ void for_equal(const uint32_t *x, int m, uint32_t min
     }
 }
 
+// A number that `keep` and few more of the workgroup's reach (all of them, if there are fewer): down from the largest, `most`, in growing steps, then halving.
+// Zeros are none.
+constexpr int BORDER_SLACK = 24;                                   // more than `keep` that are not worth another step
+constexpr int BORDER_STEPS = 9 + 32;
+constexpr int SCAN_SHORT = 96;                                     // keys beyond n_out that are ordered without such a search
+template <int N>
+__device__ __forceinline__ uint32_t block_border(const uint32_t (&x)[N], uint32_t most, int keep, int *counts) {      // counts: BORDER_STEPS zeros in LDS
+    int step = 0;
+    auto reach = [&](uint32_t t) __attribute__((always_inline)) {
+        int c = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) c += (int)__popcll(__ballot(x[k] >= t));
+        if ((threadIdx.x & 63) == 0) atomicAdd(&counts[step], c);
+        __syncthreads();
+        return counts[step++];
+    };
+    uint32_t border = 1, above = most;
+    int reached = 0;
+    if (most == 0) return 1;
+#pragma unroll 1
+    for (int d = 16;; d += 2) {
+        border = d < 32 && most > 1u << d ? most - (1u << d) : 1;
+        reached = reach(border);
+        if (reached >= keep || border == 1) break;
+        above = border;
+    }
+#pragma unroll 1
+    while (reached > keep + BORDER_SLACK && above - border > 1) {
+        const uint32_t mid = border + (above - border) / 2;
+        const int r = reach(mid);
+        if (r >= keep) { border = mid; reached = r; } else above = mid;
+    }
+    return border;
+}
+
 // ---------------------------------------------------------------- a wave's batch
 template <typename T> struct BeamUnit;                             // a piece of 16 bytes
 template <> struct BeamUnit<float> {
@@ -286,7 +335,7 @@ struct ScanShared {
     double z[BEAM_WAVES];
     float m[BEAM_WAVES];
     uint32_t border[BEAM_WAVES];
-    int bad[BEAM_WAVES], n;
+    int bad[BEAM_WAVES], count[BEAM_WAVES], counts[BORDER_STEPS], n;
 };
 
 // grid (parts, rows), block BEAM_THREADS
@@ -311,21 +360,20 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     WaveList list{sh.list[wave], sh.top[wave].spare, 0, 0, a.n_out};
     uint32_t border = 0;
     float v[16], least = -FLT_MAX, lo_top = -INFINITY, hi_top = -INFINITY;
-    const int unit_a = (part * a.batches * BEAM_WAVES + wave) * WAVE_UNITS + lane;
-    const int wave_pieces = pieces - unit_a + lane;                // pieces from the wave's first one on
-    int whole = wave_pieces <= 0 ? 0 : (wave_pieces + BEAM_WAVES * WAVE_UNITS - 1) / (BEAM_WAVES * WAVE_UNITS);
-    whole = min(whole, a.batches);
-    const int n_batches = whole + (ends > 0);
+    // the pieces are shared evenly by as many waves as they fill: a wave with a few of them would have no border
+    const int waves = max(1, min(a.parts * BEAM_WAVES, (pieces + WAVE_UNITS - 1) / WAVE_UNITS)), own = (pieces + waves - 1) / waves;
+    const int unit_0 = min(pieces, (part * BEAM_WAVES + wave) * own), unit_end = min(pieces, unit_0 + own), unit_a = unit_0 + lane;
+    const int whole = (unit_end - unit_0 + WAVE_UNITS - 1) / WAVE_UNITS, n_batches = whole + (ends > 0);
     // this lane's values of batch b
     auto fetch = [&](int b, float (&w)[16]) __attribute__((always_inline)) {
         if (b < whole) {
-            const int u0 = unit_a + b * (BEAM_WAVES * WAVE_UNITS);
+            const int u0 = unit_a + b * WAVE_UNITS;
 #pragma unroll
             for (int j = 0; j < PIECES; ++j) {
                 float t[UNIT];
 #pragma unroll
                 for (int e = 0; e < UNIT; ++e) t[e] = -INFINITY;
-                if (u0 + 64 * j < pieces) BeamUnit<T>::load(px + (size_t)(u0 + 64 * j) * UNIT, t);
+                if (u0 + 64 * j < unit_end) BeamUnit<T>::load(px + (size_t)(u0 + 64 * j) * UNIT, t);
 #pragma unroll
                 for (int e = 0; e < UNIT; ++e) w[j * UNIT + e] = t[e];
             }
@@ -342,9 +390,9 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
         for (int b = b0;;) {
             float next[16];
             if (b + 1 < n_batches) fetch(b + 1, next);
-            float lo = v[0], hi = v[8];
+            float lo = v[0], hi = v[UNIT];                         // (of every other piece: a short batch has some in each)
 #pragma unroll
-            for (int k = 1; k < 8; ++k) { lo = fmaxf(lo, v[k]); hi = fmaxf(hi, v[8 + k]); }
+            for (int k = 1; k < 16; ++k) { if (k / UNIT % 2 == 0) lo = fmaxf(lo, v[k]); else if (k != UNIT) hi = fmaxf(hi, v[k]); }
             const float top = fmaxf(lo, hi);
             lo_top = fmaxf(lo_top, lo); hi_top = fmaxf(hi_top, hi); best = fmaxf(best, top);
             sh.top[wave].of[b - b0][lane] = top;
@@ -357,7 +405,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
             for (int k = 0; k < 16; ++k) v[k] = next[k];
         }
         if (__any(best >= least)) {
-            border = max(border, wave_border(beam_order(lo_top), beam_order(hi_top), a.n_out, a.n_out > 8 ? 8 : 0));
+            border = max(border, wave_border(beam_order(lo_top), beam_order(hi_top), a.n_out));
             least = border > ORDER_OF_MINUS_INF ? order_logit(border) : -FLT_MAX;
             uint32_t in = 0;                                       // the lane's batches with something to take
             for (int k = 0; k < n_round; ++k) in |= (uint32_t)(sh.top[wave].of[k][lane] >= least) << k;
@@ -372,7 +420,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) which |= (uint32_t)(w[k] >= least) << k;
                 if (!in) which = 0;
-                const int first = b < whole ? before + (unit_a + b * (BEAM_WAVES * WAVE_UNITS)) * UNIT : lane < head ? lane : a.vocab - behind + (lane - head);
+                const int first = b < whole ? before + (unit_a + b * WAVE_UNITS) * UNIT : lane < head ? lane : a.vocab - behind + (lane - head);
 #pragma unroll 1
                 while (__any(which != 0)) {                        // a lane's next one
                     const int k = __ffs(which) - 1;
@@ -396,7 +444,8 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     // ---- the waves' sums and lists
     const float top = sum.finish(lane_top);
     const int bad = __any(sum.bad || !(lane_top < INFINITY));
-    if (lane == 0) { sh.z[wave] = sum.z; sh.m[wave] = top; sh.bad[wave] = bad; sh.border[wave] = border; }
+    if (lane == 0) { sh.z[wave] = sum.z; sh.m[wave] = top; sh.bad[wave] = bad; sh.count[wave] = list.n; sh.border[wave] = border; }
+    if (tid < BORDER_STEPS) sh.counts[tid] = 0;
     if (tid == 0) sh.n = 0;
     __syncthreads();
     if (tid == 0) {
@@ -409,20 +458,25 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
         for (int w = 0; w < BEAM_WAVES; ++w) all += sh.m[w] > -INFINITY && !any ? sh.z[w] * exp2_sum(((double)sh.m[w] - (double)m) * sum.c) : 0.0;
         a.sums[(size_t)row * a.parts + part] = {all, m, any};
     }
-    // (n_out keys at least reach each of the waves' borders: those below the highest border are out)
-    uint32_t highest = 0;
-#pragma unroll
-    for (int w = 0; w < BEAM_WAVES; ++w) highest = max(highest, sh.border[w]);
     unsigned long long mine[BEAM_LIST / 64];
+    uint32_t order[BEAM_LIST / 64], most = 0, least_kept = 1;
+    int total = 0;
 #pragma unroll
-    for (int k = 0; k < BEAM_LIST / 64; ++k) mine[k] = lane + 64 * k < list.n ? list.keys[lane + 64 * k] : 0;
+    for (int w = 0; w < BEAM_WAVES; ++w) { total += sh.count[w]; most = max(most, sh.m[w] > -INFINITY ? beam_order(sh.m[w]) : 0u); least_kept = max(least_kept, sh.border[w]); }
+#pragma unroll
+    for (int k = 0; k < BEAM_LIST / 64; ++k) {
+        mine[k] = lane + 64 * k < list.n ? list.keys[lane + 64 * k] : 0;
+        order[k] = (uint32_t)(mine[k] >> 32);
+    }
+    // (n_out keys at least reach each of the waves' borders, so the highest of them does for short lists)
+    if (total > a.n_out + SCAN_SHORT) least_kept = block_border(order, most, a.n_out, sh.counts);
     __syncthreads();
     unsigned long long *to = a.keys + ((size_t)row * a.parts + part) * a.n_out;
 #pragma unroll
     for (int k = 0; k < BEAM_LIST / 64; ++k) {
-        const bool in = mine[k] && (uint32_t)(mine[k] >> 32) >= highest;
+        const bool in = order[k] >= least_kept;
         const int at = wave_place(in, &sh.n);
-        if (in) { sh.kept.order[at] = (uint32_t)(mine[k] >> 32); sh.kept.rest[at] = (uint32_t)mine[k]; }
+        if (in) { sh.kept.order[at] = order[k]; sh.kept.rest[at] = (uint32_t)mine[k]; }
     }
     __syncthreads();
     const int m = sh.n;
@@ -431,8 +485,11 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     for (int i = tid; i < m; i += BEAM_THREADS) {
         const uint32_t order = sh.kept.order[i], rest = sh.kept.rest[i];
         int rank = 0, equal = 0;
-        count_before(sh.kept.order, m, order, rank, equal);
-        if (equal > 1) for_equal(sh.kept.order, m, order, [&](int j) { rank += sh.kept.rest[j] > rest; });
+        if (m <= a.n_out) rank = i;                                // (all of them, in any order)
+        else {
+            count_before(sh.kept.order, m, order, rank, equal);
+            if (equal > 1) for_equal(sh.kept.order, m, order, [&](int j) { rank += sh.kept.rest[j] > rest; });
+        }
         if (rank < a.n_out) to[rank] = (unsigned long long)order << 32 | rest;
     }
     for (int k = m + tid; k < a.n_out; k += BEAM_THREADS) to[k] = 0;
@@ -442,14 +499,11 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
 constexpr int JOIN_EACH = 4;                                       // keys a thread
 constexpr int JOIN_KEPT = 1024;                                    // items that are kept for ordering
 
-constexpr int JOIN_SLACK = 24;                                      // ... beyond n_out that are not worth another halving
-constexpr int JOIN_STEPS = 9 + 32;
-
 struct JoinShared {
     uint32_t high[JOIN_KEPT + 8];                                  // upper halves of the values
     unsigned long long value[JOIN_KEPT], key[JOIN_KEPT], edge_value, edge_key;
     uint32_t beam[JOIN_KEPT], edge_beam, most;
-    int reach[JOIN_STEPS];
+    int counts[BORDER_STEPS];
     double row_z[BEAM_MAX], row_div[BEAM_MAX];
     float row_score[BEAM_MAX], row_scale[BEAM_MAX];
     int row_kind[BEAM_MAX], row_len[BEAM_MAX], n;
@@ -474,18 +528,14 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
     for (int b0 = 0; b0 < a.n_beams; b0 += rows_at_once) {
         const int b = b0 + (tid >> shift), row = g * a.n_beams + min(b, a.n_beams - 1);
         const BeamRow r = beam_row(a, row);
+        const BeamSum s = a.sums[(size_t)row * parts + min(sub, parts - 1)];       // (of rows that do not run: anything)
         unsigned int flag;
-        int kind = beam_kind(r, a.eos, flag), bad = 0;
-        double z = 0.0;
-        float m = -INFINITY;
-        if (kind == BEAM_RUNS && sub < parts) {
-            const BeamSum s = a.sums[(size_t)row * parts + sub];
-            z = s.z; m = s.m; bad = s.bad;
-        }
-        float top = m;
-        for (int o = 1; o < 1 << shift; o <<= 1) { top = fmaxf(top, __shfl_xor(top, o, RS_WAVE)); bad |= __shfl_xor(bad, o, RS_WAVE); }
-        z = m > -INFINITY ? z * exp2_sum(((double)m - (double)top) * ((double)r.scale * 1.4426950408889634074)) : 0.0;
-        for (int o = 1; o < 1 << shift; o <<= 1) z += __shfl_xor(z, o, RS_WAVE);
+        int kind = beam_kind(r, a.eos, flag);
+        const bool has = kind == BEAM_RUNS && sub < parts;
+        const float m = has ? s.m : -INFINITY, top = group_all(m, shift, [](float x, float y) { return fmaxf(x, y); });
+        const int bad = group_all(has ? s.bad : 0, shift, [](int x, int y) { return x | y; });
+        const double z = group_all(m > -INFINITY ? s.z * exp2_sum(((double)m - (double)top) * ((double)r.scale * 1.4426950408889634074)) : 0.0, shift,
+                                   [](double x, double y) { return x + y; });
         if (sub == 0 && b < a.n_beams) {
             if (bad && a.flags) atomicOr(a.flags + row, RS_FLAG_NONFINITE);
             if (kind == BEAM_RUNS && (bad || !(top > -INFINITY))) kind = BEAM_NONE;
@@ -496,7 +546,7 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
         }
     }
     if (tid == 0) { sh.n = 0; sh.most = 0; }
-    if (tid < JOIN_STEPS) sh.reach[tid] = 0;
+    if (tid < BORDER_STEPS) sh.counts[tid] = 0;
     __syncthreads();
     // ---- the items' values
     unsigned long long best = 0;
@@ -510,37 +560,13 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
         if (kind != BEAM_NONE && key[k]) value[k] = double_order(a.alpha > 0.0 ? v / sh.row_div[b] : v);
         best = value[k] > best ? value[k] : best;
     }
-    // ---- a border, on the upper halves, that n_out items and few more reach: down from the largest in growing steps, then halving
     const uint32_t wave_most = wave_max_u32((uint32_t)(best >> 32));
     if (lane == 0) atomicMax(&sh.most, wave_most);
     __syncthreads();
-    const uint32_t most = sh.most;
-    int step = 0;
-    auto reach = [&](uint32_t t) __attribute__((always_inline)) {
-        int c = 0;
+    uint32_t high[JOIN_EACH];
 #pragma unroll
-        for (int k = 0; k < JOIN_EACH; ++k) c += (int)__popcll(__ballot((uint32_t)(value[k] >> 32) >= t));
-        if (lane == 0) atomicAdd(&sh.reach[step], c);
-        __syncthreads();
-        return sh.reach[step++];
-    };
-    uint32_t border = 1, above = most;
-    int reached = 0;
-    if (most > 0) {
-#pragma unroll 1
-        for (int d = 16;; d += 2) {
-            border = d < 32 && most > 1u << d ? most - (1u << d) : 1;
-            reached = reach(border);
-            if (reached >= a.n_out || border == 1) break;
-            above = border;
-        }
-#pragma unroll 1
-        while (reached > a.n_out + JOIN_SLACK && above - border > 1) {
-            const uint32_t mid = border + (above - border) / 2;
-            const int r = reach(mid);
-            if (r >= a.n_out) { border = mid; reached = r; } else above = mid;
-        }
-    }
+    for (int k = 0; k < JOIN_EACH; ++k) high[k] = (uint32_t)(value[k] >> 32);
+    const uint32_t border = block_border(high, sh.most, a.n_out, sh.counts);
     auto keep = [&](int k, bool in) __attribute__((always_inline)) {
         const int at = wave_place(in, &sh.n);
         if (in && at < JOIN_KEPT) { sh.high[at] = (uint32_t)(value[k] >> 32); sh.value[at] = value[k]; sh.key[at] = key[k]; sh.beam[at] = (tid + threads * k) / per_row; }

@@ -274,10 +274,9 @@ __global__ void __launch_bounds__(256) k_pool_copy(CopyArgs a) {
 // ---------------------------------------------------------------- rs_pages_fork
 struct ForkArgs { Pool p; const int *slot, *parent, *pos; int *pos_out; int n_groups, n_beams; PageMove *moves; int *n_moves; };
 
-constexpr int FORK_EACH = 8;                                       // table entries a thread holds between reading and writing them
-
 // grid 1, block POOL_THREADS.  Reads everything before it writes a table entry: whether all rows are in range, the counts after the call, the rows that
-// need a page, the pages they get.
+// need a page, the pages they get.  FORK_EACH: table entries that a thread requests together, and holds between reading and writing them.
+template <int FORK_EACH>
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
     __shared__ FirstRow first;
     __shared__ int sh[ORDERED_COUNTS], slot_of[POOL_ROWS], from_of[POOL_ROWS], whole_of[POOL_ROWS], new_page[POOL_ROWS], want_row[POOL_ROWS];
@@ -310,14 +309,29 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
     __syncthreads();
     if (page >= 0) place = first_enter(first, page, tid);
     // ---- counts: what the rows held goes, the whole pages of their parents come
-    const long long entries = (long long)n * mp;
-    auto count = [&](int by) {
-        for (long long i = tid; i < entries; i += POOL_THREADS) {
-            const int r = (int)(i / mp), j = (int)(i - (long long)r * mp), f = from_of[r];
-            const int old = p.table[(size_t)slot_of[r] * mp + j], now = f >= 0 && j < whole_of[r] ? p.table[(size_t)f * mp + j] : -1;
-            if (old == now) continue;
-            if (is_page(p, old)) ref_add(p.ref + old, -by);
-            if (is_page(p, now)) ref_add(p.ref + now, by);
+    // entries of a thread are POOL_THREADS apart in the rows one behind the other, FORK_EACH of them requested together
+    const int jump_r = POOL_THREADS / mp, jump_j = POOL_THREADS - jump_r * mp;
+    auto count = [&](int by) __attribute__((always_inline)) {
+        int r = tid / mp, j = tid - r * mp;
+        while (r < n) {
+            int old[FORK_EACH], now[FORK_EACH];
+#pragma unroll
+            for (int k = 0; k < FORK_EACH; ++k) {
+                old[k] = now[k] = -1;
+                if (r < n) {
+                    const int f = from_of[r];
+                    old[k] = p.table[(size_t)slot_of[r] * mp + j];
+                    if (f >= 0 && j < whole_of[r]) now[k] = p.table[(size_t)f * mp + j];
+                }
+                r += jump_r; j += jump_j;
+                if (j >= mp) { j -= mp; ++r; }
+            }
+#pragma unroll
+            for (int k = 0; k < FORK_EACH; ++k) {
+                if (old[k] == now[k]) continue;
+                if (is_page(p, old[k])) ref_add(p.ref + old[k], -by);
+                if (is_page(p, now[k])) ref_add(p.ref + now[k], by);
+            }
         }
         refs_settled();
     };
