@@ -224,7 +224,7 @@ struct WaveSum {
             const double shift = TO_INT - (double)r;
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-                const double x = (double)fmaxf(v[k], low), s = fma(x, c, shift);
+                const double x = (double)__builtin_amdgcn_fmed3f(v[k], low, INFINITY), s = fma(x, c, shift);       // (a maximum that takes NaN as it is)
                 z += scale_exp(exp2_part(fma(x, c, shift - s)), __double2loint(s));
             }
         } else {
@@ -308,19 +308,12 @@ __device__ __forceinline__ uint32_t block_border(const uint32_t (&x)[N], uint32_
 template <typename T> struct BeamUnit;                             // a piece of 16 bytes
 template <> struct BeamUnit<float> {
     static constexpr int N = 4;
-    static __device__ __forceinline__ void load(const float *p, float (&v)[4]) {
-        const float4 q = *reinterpret_cast<const float4 *>(p);
-        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-    }
+    static __device__ __forceinline__ float value(const u32x4_t &q, int i) { return __uint_as_float(q[i]); }
     static __device__ __forceinline__ float one(const float *p) { return *p; }
 };
 template <> struct BeamUnit<uint16_t> {
     static constexpr int N = 8;
-    static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[8]) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(p);
-        v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
-        v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
-    }
+    static __device__ __forceinline__ float value(const u32x4_t &q, int i) { return i & 1 ? bf16_hi(q[i / 2]) : bf16_lo(q[i / 2]); }
     static __device__ __forceinline__ float one(const uint16_t *p) { return bf16_to_f32(*p); }
 };
 
@@ -343,7 +336,7 @@ template <typename T>
 __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     constexpr int UNIT = BeamUnit<T>::N, PIECES = 16 / UNIT, WAVE_UNITS = 64 * PIECES;
     __shared__ ScanShared sh;
-    const int row = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const BeamRow r = beam_row(a, row);
     unsigned int flag;
     const int kind = beam_kind(r, a.eos, flag);
@@ -354,7 +347,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     const int before = min(a.vocab, (int)((16 - (uintptr_t)x % 16) % 16 / sizeof(T))), pieces = (a.vocab - before) / UNIT, behind = a.vocab - before - pieces * UNIT;
     // the values before are the first part's, those behind the last one's: a batch of their own, one a lane
     const int head = part == 0 ? before : 0, ends = wave == 0 ? head + (part == a.parts - 1 ? behind : 0) : 0;
-    const T *px = x + before;
+    const u32x4_t *px = reinterpret_cast<const u32x4_t *>(x + before);
     WaveSum sum;
     sum.init(r.scale);
     WaveList list{sh.list[wave], sh.top[wave].spare, 0, 0, a.n_out};
@@ -364,32 +357,37 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     const int waves = max(1, min(a.parts * BEAM_WAVES, (pieces + WAVE_UNITS - 1) / WAVE_UNITS)), own = (pieces + waves - 1) / waves;
     const int unit_0 = min(pieces, (part * BEAM_WAVES + wave) * own), unit_end = min(pieces, unit_0 + own), unit_a = unit_0 + lane;
     const int whole = (unit_end - unit_0 + WAVE_UNITS - 1) / WAVE_UNITS, n_batches = whole + (ends > 0);
-    // this lane's values of batch b
-    auto fetch = [&](int b, float (&w)[16]) __attribute__((always_inline)) {
-        if (b < whole) {
+    const int end_token = lane < head ? lane : a.vocab - behind + (lane - head);
+    const float end_value = lane < ends ? BeamUnit<T>::one(x + end_token) : -INFINITY;
+    // this lane's pieces of batch b < whole, and their values
+    auto fetch = [&](int b, u32x4_t (&w)[PIECES]) __attribute__((always_inline)) {
+        const int u0 = unit_a + b * WAVE_UNITS;
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) w[j] = px[min(u0 + 64 * j, unit_end - 1)];
+    };
+    auto values = [&](int b, const u32x4_t (&w)[PIECES], float (&x16)[16]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) x16[k] = BeamUnit<T>::value(w[k / UNIT], k % UNIT);
+        if (unit_0 + (b + 1) * WAVE_UNITS > unit_end) {
             const int u0 = unit_a + b * WAVE_UNITS;
 #pragma unroll
-            for (int j = 0; j < PIECES; ++j) {
-                float t[UNIT];
-#pragma unroll
-                for (int e = 0; e < UNIT; ++e) t[e] = -INFINITY;
-                if (u0 + 64 * j < unit_end) BeamUnit<T>::load(px + (size_t)(u0 + 64 * j) * UNIT, t);
-#pragma unroll
-                for (int e = 0; e < UNIT; ++e) w[j * UNIT + e] = t[e];
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) w[k] = -INFINITY;
-            if (lane < ends) w[0] = BeamUnit<T>::one(x + (lane < head ? lane : a.vocab - behind + (lane - head)));
+            for (int k = 0; k < 16; ++k) x16[k] = u0 + 64 * (k / UNIT) < unit_end ? x16[k] : -INFINITY;
         }
     };
-    if (n_batches > 0) fetch(0, v);
+    u32x4_t next[PIECES];                                          // under way while a batch is added up (two batches ahead was no faster)
+    if (whole > 0) fetch(0, next);
     for (int b0 = 0; b0 < n_batches; b0 += BEAM_ROUND) {
         const int n_round = min(BEAM_ROUND, n_batches - b0);
         float best = -INFINITY;
-        for (int b = b0;;) {
-            float next[16];
-            if (b + 1 < n_batches) fetch(b + 1, next);
+        for (int b = b0; b < b0 + n_round; ++b) {
+            if (b < whole) {
+                values(b, next, v);
+                if (b + 1 < whole) fetch(b + 1, next);
+            } else {
+#pragma unroll
+                for (int k = 1; k < 16; ++k) v[k] = -INFINITY;
+                v[0] = end_value;
+            }
             float lo = v[0], hi = v[UNIT];                         // (of every other piece: a short batch has some in each)
 #pragma unroll
             for (int k = 1; k < 16; ++k) { if (k / UNIT % 2 == 0) lo = fmaxf(lo, v[k]); else if (k != UNIT) hi = fmaxf(hi, v[k]); }
@@ -399,10 +397,6 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
 #pragma unroll
             for (int k = 0; k < 16; k += 2) sum.bad |= __builtin_isunordered(v[k], v[k + 1]);
             sum.add(v, top);
-            ++b;
-            if (b == b0 + n_round) break;
-#pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] = next[k];
         }
         if (__any(best >= least)) {
             border = max(border, wave_border(beam_order(lo_top), beam_order(hi_top), a.n_out));
@@ -415,12 +409,12 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
                 float w[16];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) w[k] = v[k];
-                if (in && b != b0 + n_round - 1) fetch(b, w);
+                if (in && b != b0 + n_round - 1) { u32x4_t again[PIECES]; fetch(b, again); values(b, again, w); }
                 uint32_t which = 0;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) which |= (uint32_t)(w[k] >= least) << k;
                 if (!in) which = 0;
-                const int first = b < whole ? before + (unit_a + b * WAVE_UNITS) * UNIT : lane < head ? lane : a.vocab - behind + (lane - head);
+                const int first = b < whole ? before + (unit_a + b * WAVE_UNITS) * UNIT : end_token;
 #pragma unroll 1
                 while (__any(which != 0)) {                        // a lane's next one
                     const int k = __ffs(which) - 1;
@@ -438,7 +432,6 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
                 in &= in - 1;
             }
         }
-        if (b0 + BEAM_ROUND < n_batches) fetch(b0 + BEAM_ROUND, v);
     }
     const float lane_top = fmaxf(lo_top, hi_top);
     // ---- the waves' sums and lists
