@@ -523,12 +523,12 @@ rs_status rs_create_model_paged(const rs_config *cfg, const rs_weights *weights,
  *   d_logit_scale   DEVICE fp32 [rows] or NULL (= 1): > 0 and finite
  *   d_score         DEVICE fp32 [rows]: sum of log probabilities; -inf: the beam is not there (its logits are not read)
  *   d_last          DEVICE int32 [rows] or NULL: the beams' last tokens;  eos: a token or -1 (no beam ends)
- *   length_penalty  >= 0: candidates are ordered by score / length^length_penalty, length at least 1
- *   d_len           DEVICE int32 [rows] or NULL (with length_penalty 0): tokens of the beams so far, >= 0; a continuation has one more
+ *   length_penalty  0 .. 30: candidates are ordered by score / length^length_penalty, length at least 1
+ *   d_len           DEVICE int32 [rows] or NULL (with length_penalty 0): tokens of the beams so far, 0 .. 2^31 - 2; a continuation has one more
  *   d_parent        DEVICE int32 [n_groups * n_out]: the candidate's beam, 0 .. n_beams - 1
  *   d_token, d_score_out, d_len_out (or NULL)  its token, score (not divided) and length
  *   d_flags         DEVICE uint32 [rows] or NULL: RS_FLAG_NONFINITE is or-ed in where a logit is NaN or +inf,
- *                   RS_FLAG_BADARG where a score is NaN or +inf, a length negative or a scale not positive and finite; such rows
+ *                   RS_FLAG_BADARG where a score is NaN or +inf, a length out of range or a scale not positive and finite; such rows
  *                   have no candidates (the caller clears the words)
  *   d_scratch       DEVICE, 256-byte aligned, of at least rs_beam_select_scratch_bytes (0 on a bad argument); any content.  Calls and
  *                   graph replays that overlap must not share it

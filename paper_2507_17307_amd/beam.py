@@ -74,6 +74,8 @@ class BeamSearch:
         cfg, nb = self.model.cfg, self.n_beams
         if len(prompts) != self.n_prompts or any(len(p) < 1 for p in prompts) or n_tokens < 1:
             raise ValueError("one prompt of at least one token each, and at least one token to generate")
+        if any(not 0 <= t < cfg.vocab for p in prompts for t in p):
+            raise ValueError("a prompt's token is out of range")
         if max(len(p) for p in prompts) + n_tokens - 1 > cfg.max_ctx:
             raise ValueError("prompt + tokens exceed max_ctx")
         parents = torch.zeros(n_tokens, self.rows, dtype=torch.int32, device=self.model.device)

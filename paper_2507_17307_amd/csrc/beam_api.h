@@ -104,7 +104,7 @@ rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype
     if (!need) return RS_EINVAL;
     if (row_stride < vocab || row_stride > ((int64_t)1 << 40)) return fail(RS_EINVAL, "row_stride must be at least vocab and at most 2^40");
     if (eos < -1 || eos >= vocab) return fail(RS_EINVAL, "eos must be -1 or a token");
-    if (!(length_penalty >= 0.0) || !std::isfinite(length_penalty)) return fail(RS_EINVAL, "length_penalty must be finite and not negative");
+    if (!(length_penalty >= 0.0 && length_penalty <= 30.0)) return fail(RS_EINVAL, "length_penalty must be in 0..30");      // ((2^31)^30 is a double)
     if (!d_len && (length_penalty > 0.0 || d_len_out)) return fail(RS_EINVAL, "lengths are needed for length_penalty and d_len_out");
     if ((uintptr_t)d_logits % (dtype == RS_F32 ? 4 : 2)) return fail(RS_EINVAL, "logits are not aligned to their type");
     if (((uintptr_t)d_logit_scale | (uintptr_t)d_score | (uintptr_t)d_last | (uintptr_t)d_len | (uintptr_t)d_parent | (uintptr_t)d_token | (uintptr_t)d_score_out |

@@ -14,7 +14,7 @@ def select(logits, n_groups, n_beams, score, n_out, scale=None, last=None, eos=-
         for b in range(n_beams):
             r = g * n_beams + b
             s, c, n = float(score[r]), 1.0 if scale is None else float(scale[r]), 0 if length is None else int(length[r])
-            if math.isnan(s) or s == math.inf or n < 0:
+            if math.isnan(s) or s == math.inf or not 0 <= n < 2**31 - 1:
                 bad.add(r)
                 continue
             if s == -math.inf:
@@ -44,7 +44,7 @@ def select(logits, n_groups, n_beams, score, n_out, scale=None, last=None, eos=-
 
 
 def check_scores(got, want, what=""):
-    """Scores rounded once to fp32.  In double they are off by the exponentials' 5.5e-11, by up to 2^18 additions of positive numbers (2^18 2^-53 < 3e-11) in ln Z
+    """Scores rounded once to fp32.  In double they are off by the exponentials' 1.1e-12, by up to 2^18 additions of positive numbers (2^18 2^-53 < 3e-11) in ln Z
     and by a few roundings of numbers below 2^20 (2^-33 each): 1e-9 covers that."""
     got = got.double().cpu()
     assert torch.equal(got == -math.inf, want == -math.inf), what

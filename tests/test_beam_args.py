@@ -18,7 +18,7 @@ def select(lib, **change):
     (dict(dtype=2), -1, "dtype"), (dict(groups=0), -1, "n_groups"), (dict(beams=0), -1, "n_beams"), (dict(beams=65), -1, "n_beams"),
     (dict(n_out=0), -1, "n_out"), (dict(n_out=65), -1, "n_out"), (dict(vocab=0), -1, "vocab"), (dict(groups=30000), -2, "65535"),
     (dict(stride=99), -1, "row_stride"), (dict(stride=1 << 41), -1, "row_stride"), (dict(eos=100), -1, "eos"), (dict(eos=-2), -1, "eos"),
-    (dict(penalty=-0.5), -1, "length_penalty"), (dict(penalty=float("nan")), -1, "length_penalty"), (dict(penalty=float("inf")), -1, "length_penalty"),
+    (dict(penalty=-0.5), -1, "length_penalty"), (dict(penalty=float("nan")), -1, "length_penalty"), (dict(penalty=float("inf")), -1, "length_penalty"), (dict(penalty=30.5, length=4096), -1, "length_penalty"),
     (dict(penalty=1.0), -1, "lengths"), (dict(len_out=4096), -1, "lengths"), (dict(logits=4098), -1, "aligned"), (dict(logits=4097, dtype=1), -1, "aligned"),
     (dict(token=4098), -1, "4-byte"), (dict(flags=4097), -1, "4-byte"), (dict(scratch=4112), -1, "256-byte"), (dict(bytes=16), -1, "smaller"),
 ])

@@ -104,6 +104,7 @@ def test_too_few_pages_are_told_and_pages_belong_to_the_pool():
             P.BeamSearch(model, *args)
     with pytest.raises(ValueError):
         search.generate([[1] * 40], 30)
-    with pytest.raises(ValueError):
-        search.generate([[]], 3)
+    for prompt in ([], [1, W.TINY_S.vocab], [-1]):
+        with pytest.raises(ValueError):
+            search.generate([prompt], 3)
     model.close()

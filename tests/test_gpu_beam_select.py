@@ -146,6 +146,8 @@ def test_bad_rows_are_flagged_and_have_no_candidates():
     assert got[4].tolist() == [8, 8, 0, 16, 16, 16, 16, 16] and set(got[0].tolist()) == {2}
     length = torch.tensor([1, 1, 1, 1, 1, 1, 1, -1], dtype=torch.int32)
     compare(x, 2, 4, score, 5, length=length, alpha=1.0)
+    length[2] = 2**31 - 1
+    compare(x, 2, 4, score, 5, length=length, alpha=1.0)
     assert run(x, 1, 8, score, 5, scale=scale, flags=False)[0].tolist() == got[0].tolist()
 
 
@@ -166,6 +168,63 @@ def test_neighbours_that_32_bits_do_not_tell_apart():
         y[up, 12] = math.log(2.0 ** -30)                                  # the beam's ln Z grows by 2^-30
         got = run(y, 1, 2, score, 2)
         assert got[0].tolist() == [1 - up, up] and got[1].tolist() == [11, 11]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_batches_a_wave(dtype):
+    """64 x 64 candidates leave a row one workgroup: 13 batches a wave, whose logits rise past what one exponent serves (2^500 above the first), and past
+    the size up to which they are added up in that way at all."""
+    x, score, g = normal(13, 64, 50257, dtype)
+    x[1, 30000:] += 1000.0
+    x[2, 9000:40000] += 2000.0
+    x[3, 20000] = 3500.0
+    x[4, 13000:] -= 2500.0
+    x[5] *= 500.0
+    x[6, 100:50000] = -math.inf
+    x[7, 5000:] = -math.inf
+    x[8] -= 1000.0
+    x[9, 50256] = 90.0
+    compare(x, 1, 64, score, 64)
+    compare(x, 1, 64, score * 0, 64, scale=torch.rand(64, generator=g) * 2 + 0.1)
+
+
+def test_thousands_of_equal_candidates():
+    x = torch.zeros(128, 300)
+    got = compare(x, 2, 64, torch.full((128,), -1.0), 64)
+    assert got[0].tolist() == [0] * 128 and got[1].tolist() == list(range(64)) * 2
+    score = torch.full((128,), -1.0)
+    score[:40] = -3.0                                                         # (3000 equals from beam 40 on, others below them)
+    x[70, 5] = 1.0
+    compare(x, 2, 64, score, 64)
+
+
+def test_scores_far_apart_and_beams_that_are_not_there():
+    x, score, g = normal(14, 64, 4000)
+    score[:] = -torch.arange(64) * 40.0
+    score[::4] = -math.inf
+    compare(x, 1, 64, score, 64)
+    compare(x, 2, 32, score.flip(0), 32)
+    score[:] = -math.inf
+    score[0], score[32] = 0.0, 0.0                                            # a search's first step
+    compare(x, 2, 32, score, 64)
+
+
+def test_two_calls_at_once():
+    import paper_2507_17307_amd as P
+    calls = []
+    for k in range(2):
+        x, score, g = normal(20 + k, 24, 100003)
+        out = [torch.zeros(48, dtype=torch.int32, device="cuda") for _ in range(2)] + [torch.zeros(48, device="cuda")]
+        calls.append((x.cuda(), score.cuda(), out, torch.empty(P.rs_beam_select_scratch_bytes(6, 4, 100003, 8), dtype=torch.uint8, device="cuda"), torch.cuda.Stream(), x, score))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, score, out, scratch, stream, _, _ in calls:
+            P.rs_beam_select(x, 6, 4, None, score, None, -1, 0.0, None, 8, out[0], out[1], out[2], None, scratch, stream=stream)
+    torch.cuda.synchronize()
+    for _, _, out, _, _, x, score in calls:
+        want = beam.select(x, 6, 4, score, 8)
+        assert out[0].tolist() == want[0] and out[1].tolist() == want[1]
+        beam.check_scores(out[2], want[2])
 
 
 def test_in_place_and_replayed():
