@@ -218,7 +218,7 @@ struct WaveSum {
             if (fabs(x) < 4096.0) {
                 r = (int)__builtin_rint(x);
                 low = (float)((double)(r - 1000) / c); high = (float)((double)(r + 500) / c);
-                ready = true;
+                ready = low > -INFINITY;                           // (scales under 2^-115 or so: nothing is 2^1000 smaller but masked logits, which the lanes drop)
             }
         }
         if (ready && !__any(top > high)) {

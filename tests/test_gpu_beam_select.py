@@ -227,6 +227,16 @@ def test_two_calls_at_once():
         beam.check_scores(out[2], want[2])
 
 
+@pytest.mark.parametrize("scale", [1e-30, 1e-34, 1e-36, 1e-40, 1e-45])
+def test_scales_next_to_nothing(scale):
+    """All tokens but the masked ones are equally likely."""
+    x, score, g = normal(15, 4, 5003)
+    x[0, ::2] = -math.inf
+    x[1, 1:] = -math.inf
+    x[2, :5000] = -math.inf
+    compare(x, 2, 2, score, 6, scale=torch.full((4,), scale))
+
+
 def test_in_place_and_replayed():
     import paper_2507_17307_amd as P
     x, score, g = normal(12, 12, 60000)
