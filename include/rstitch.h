@@ -561,7 +561,7 @@ typedef struct rs_page_pool {
     int32_t n_slots;             /* >= 1                                                      */
     int32_t max_pages;           /* >= 1; page_size * max_pages <= 2^30, n_slots * max_pages < 2^31 */
     int32_t n_kv_heads;          /* 1 .. 1024                                                 */
-    int32_t head_dim;            /* 32, 64 or 128                                             */
+    int32_t head_dim;            /* 32, 64 or 128; a page of all layers, K and V, is 256 GiB at most */
 } rs_page_pool;
 
 /* DEVICE scratch of the calls below, 256-byte aligned, for n rows (n_groups * n_beams; 1 for rs_pages_compact); 0 on a bad

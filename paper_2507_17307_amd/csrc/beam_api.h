@@ -19,6 +19,12 @@ const char *check_pool(const rs_page_pool *c) {
     return nullptr;
 }
 
+// Workgroups for a page's K or V of one layer in k_pool_copy.
+long long page_pieces(const rs_page_pool *c) {
+    const long long units = (long long)c->n_kv_heads * c->head_dim * c->page_size / 8;
+    return (units + 256 * COPY_UNITS - 1) / (256 * COPY_UNITS);
+}
+
 // ... of a call that moves what is in the pages
 const char *check_contents(const rs_page_pool *c) {
     if (const char *why = check_pool(c)) return why;
@@ -26,6 +32,7 @@ const char *check_contents(const rs_page_pool *c) {
     if (((uintptr_t)c->k | (uintptr_t)c->v) % 16) return "K and V pages must be 16-byte aligned";
     if (c->n_layers < 1 || c->n_layers > 65536 || c->n_kv_heads < 1 || c->n_kv_heads > 1024) return "n_layers must be in 1..65536, n_kv_heads in 1..1024";
     if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 32, 64 or 128";
+    if (page_pieces(c) * 2 * c->n_layers > 0xffffff) return "a page of all layers is too large";      // (what a grid takes)
     return nullptr;
 }
 
@@ -62,11 +69,9 @@ rs_status check_pool_rows(int32_t n, const void *a, const void *b, const void *c
 }
 
 constexpr int COPY_WGS = 4096;                                     // workgroups of k_pool_copy, about
-rs_status launch_copy(CopyArgs a, int moves_most, hipStream_t st) {
-    const long long units = (long long)a.to.n_kv * a.to.head_dim << a.to.page_shift >> 3, halves = 2LL * a.to.n_layers;
-    a.pieces = (int)((units + 256 * COPY_UNITS - 1) / (256 * COPY_UNITS));
-    const long long x = a.pieces * halves, y = (COPY_WGS + x - 1) / x;
-    if (x > 0xffffff) return fail(RS_EINVAL, "a page of all layers is too large");
+rs_status launch_copy(const rs_page_pool *to, CopyArgs a, int moves_most, hipStream_t st) {
+    a.pieces = (int)page_pieces(to);
+    const long long x = a.pieces * 2LL * to->n_layers, y = (COPY_WGS + x - 1) / x;
     hipLaunchKernelGGL(k_pool_copy, dim3((unsigned)x, (unsigned)(y < moves_most ? y : moves_most < 1 ? 1 : moves_most)), dim3(256), 0, st, a);
     RS_LAUNCHED("pool_copy");
     return RS_OK;
@@ -180,7 +185,7 @@ rs_status rs_pages_fork(const rs_page_pool *pool, int32_t n_groups, int32_t n_be
     RS_LAUNCHED("pool_fork");
     CopyArgs c{};
     c.to = a.p; c.k = a.p.k; c.v = a.p.v; c.from_pages = a.p.n_pages; c.moves = a.moves; c.n_moves = a.n_moves;
-    return launch_copy(c, n, st);
+    return launch_copy(pool, c, n, st);
 }
 
 rs_status rs_pages_copy(const rs_page_pool *to, const rs_page_pool *from, int32_t n, const int32_t *d_src, const int32_t *d_dst, uint32_t *d_flags, void *stream) {
@@ -194,7 +199,7 @@ rs_status rs_pages_copy(const rs_page_pool *to, const rs_page_pool *from, int32_
     if (((uintptr_t)d_src | (uintptr_t)d_dst | (uintptr_t)d_flags) % 4) return fail(RS_EINVAL, "pages and flags must be 4-byte aligned");
     CopyArgs c{};
     c.to = make_pool(to, d_flags); c.k = (const uint16_t *)from->k; c.v = (const uint16_t *)from->v; c.from_pages = from->n_pages; c.src = d_src; c.dst = d_dst; c.n = n;
-    return launch_copy(c, n, (hipStream_t)stream);
+    return launch_copy(to, c, n, (hipStream_t)stream);
 }
 
 rs_status rs_pages_compact(const rs_page_pool *pool, int32_t *d_used, void *d_scratch, size_t scratch_bytes, void *stream) {
@@ -211,7 +216,7 @@ rs_status rs_pages_compact(const rs_page_pool *pool, int32_t *d_used, void *d_sc
     RS_LAUNCHED("pool_compact");
     CopyArgs c{};
     c.to = a.p; c.k = a.p.k; c.v = a.p.v; c.from_pages = a.p.n_pages; c.moves = a.moves; c.n_moves = a.n_moves; c.map = a.map;
-    return launch_copy(c, pool->n_pages / 2, st);
+    return launch_copy(pool, c, pool->n_pages / 2, st);
 }
 
 }  // extern "C"

@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
 
 // ---------------------------------------------------------------- moving pages
 // What a move of one page is: `part` places (a multiple of 8) from page src to page dst, in all layers.
-struct PageMove { int src, dst, part, row; };
+struct alignas(16) PageMove { int src, dst, part; };
 
 struct CopyArgs {
     Pool to;
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(256) k_pool_copy(CopyArgs a) {
         PageMove mv;
         if (a.moves) mv = a.moves[m];
         else {
-            mv = {a.src[m], a.dst[m], ps, m};
+            mv = {a.src[m], a.dst[m], ps};
             if (mv.src < 0 || mv.src >= a.from_pages || !is_page(p, mv.dst)) { if (blockIdx.x == 0 && tid == 0) pool_flag(p, m, RS_FLAG_BADARG); continue; }
         }
         const u32x4_t *x = from + (size_t)mv.src * (page_values / 8);
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
     }
     if (want) {
         ref_store(p.ref + new_page[tid], 1);
-        a.moves[rank] = {page, new_page[tid], (tail + 7) / 8 * 8, tid};
+        a.moves[rank] = {page, new_page[tid], (tail + 7) / 8 * 8};
     }
     if (tid == 0) *a.n_moves = wanted;
     if (a.pos_out && tid < n) a.pos_out[tid] = pos;                // (every row's position was read before)
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_compact(CompactArgs a) {
     refs_settled();
     const int n = ordered(p.n_pages - used, 0x7fffffff, sh, [&](int i) { return p.ref[used + i]; }, [](int count) { return count != 0; }, [&](int i, int k) {
         const int from = used + i, to = __hip_atomic_load(a.gaps + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        a.moves[k] = {from, to, 1 << p.page_shift, k};
+        a.moves[k] = {from, to, 1 << p.page_shift};
         a.map[from] = to;
         p.ref[to] = p.ref[from];
         p.ref[from] = 0;

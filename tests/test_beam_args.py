@@ -69,6 +69,14 @@ def test_calls_that_move_pages_refuse_a_pool_without_them(change, word):
         assert status() == -1 and word in P.rs_last_error(), P.rs_last_error()
 
 
+def test_a_page_that_no_grid_covers_is_refused_before_anything_is_done():
+    import paper_2507_17307_amd as P
+    p, lib, n = C.byref(pool_struct(P, n_layers=65536, n_kv_heads=1024, head_dim=128, page_size=1024)), P.lib, 1 << 20
+    for call in (lambda: lib.rs_pages_fork(p, 1, 1, 4096, 4096, 4096, None, None, 4096, n, None), lambda: lib.rs_pages_copy(p, p, 1, 4096, 4096, None, None),
+                 lambda: lib.rs_pages_compact(p, 4096, 4096, n, None)):
+        assert call() == -1 and "too large" in P.rs_last_error(), P.rs_last_error()
+
+
 def test_rows_and_scratch_of_pool_calls():
     import paper_2507_17307_amd as P
     p, lib, n = C.byref(pool_struct(P)), P.lib, 1 << 20
