@@ -28,6 +28,11 @@ class BeamSearch:
         cfg, rows = model.cfg, n_prompts * n_beams
         if n_prompts < 1 or n_beams < 1 or rows > cfg.max_seqs or rows > cfg.max_rows:
             raise ValueError(f"{n_prompts} x {n_beams} beams do not fit {cfg.max_seqs} slots / {cfg.max_rows} rows")
+        if not -1 <= eos < cfg.vocab or not 0 <= length_penalty <= 30 or not 0 < logit_scale < float("inf"):
+            raise ValueError("need eos -1 or a token, length_penalty in 0..30 and a positive logit_scale")
+        n = B.rs_beam_select_scratch_bytes(n_prompts, n_beams, cfg.vocab, n_beams)
+        if n == 0 or rows > 1024:
+            raise ValueError(f"more than 64 beams of a prompt or 1024 of all: {n_prompts} x {n_beams}")
         self.model, self.n_prompts, self.n_beams, self.eos, self.length_penalty, self.rows = model, n_prompts, n_beams, eos, length_penalty, rows
         dev = model.device
         self.pool = model.page_pool()
@@ -45,11 +50,8 @@ class BeamSearch:
         self.flags, self.bad_rows = ints(rows), ints(rows)
         self.all_slots, self.everything = torch.arange(cfg.max_seqs, dtype=torch.int32, device=dev), ints(cfg.max_seqs, model.page_size * model.page_table.shape[1])
         self.pool_scratch = torch.empty(B.rs_pages_scratch_bytes(self.pool, rows), dtype=torch.uint8, device=dev)
-        n = B.rs_beam_select_scratch_bytes(n_prompts, n_beams, cfg.vocab, n_beams)
-        if n == 0:
-            raise B.RsError(-1, B.rs_last_error())
         self.scratch = torch.empty(n, dtype=torch.uint8, device=dev)
-        torch.cuda.synchronize()
+        torch.cuda.synchronize(dev)
 
     def _prefill(self, prompts: Sequence[Sequence[int]]) -> None:
         """Every prompt into the slot of its first beam; the logits behind it into that beam's row."""
@@ -80,10 +82,11 @@ class BeamSearch:
             raise ValueError("prompt + tokens exceed max_ctx")
         parents = torch.zeros(n_tokens, self.rows, dtype=torch.int32, device=self.model.device)
         tokens = torch.zeros_like(parents)
-        self.stream.wait_stream(torch.cuda.current_stream())
+        self.stream.wait_stream(torch.cuda.current_stream(self.model.device))
         with torch.cuda.stream(self.stream):
             # the slots give back what they hold; only the first beam of every prompt is there yet
-            B.rs_pages_release(self.pool, cfg.max_seqs, self.all_slots, None, self.everything)
+            for at in range(0, cfg.max_seqs, 1024):
+                B.rs_pages_release(self.pool, min(1024, cfg.max_seqs - at), self.all_slots[at:], None, self.everything[at:])
             self.flags.zero_(), self.bad_rows.zero_(), self.pos.zero_(), self.length.zero_(), self.token.fill_(-1)
             self.score.fill_(float("-inf"))
             self.score[::nb] = 0.0

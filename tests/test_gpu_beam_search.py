@@ -90,7 +90,10 @@ def test_too_few_pages_are_told_and_pages_belong_to_the_pool():
     import paper_2507_17307_amd as P
     w = W.make_weights(W.TINY_S, seed=5, role=0).to("cuda")
     model = P.PagedModel(w, max_ctx=64, n_pages=5, page_size=16, max_seqs=4, max_rows=4)
-    model.reserve(2, 20)
+    for more in (dict(eos=-2), dict(eos=W.TINY_S.vocab), dict(length_penalty=-1.0), dict(length_penalty=31.0), dict(logit_scale=0.0)):
+        with pytest.raises(ValueError):
+            P.BeamSearch(model, 1, 4, **more)
+    model.reserve(2, 20)                                                      # (the pages are still the model's)
     search = P.BeamSearch(model, 1, 4, logit_scale=6.0)
     assert search.pool.page_ref.tolist() == [1, 1, 0, 0, 0]
     with pytest.raises(P.RsError, match="pages"):
