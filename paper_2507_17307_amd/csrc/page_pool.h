@@ -119,7 +119,7 @@ __device__ __forceinline__ bool pool_range(const RangeArgs &a, int r, int &slot,
     return slot >= 0 && slot < a.p.n_slots && from >= 0 && to >= from && to <= (long long)a.p.max_pages << a.p.page_shift;
 }
 
-// grid n, block 256: the entries whose pages lie wholly in the row's range
+// grid n, block 256: the entries whose pages lie wholly in the row's range.  A launch and one chain entry -> count: 3.2 us for 128 rows of up to 125 entries.
 __global__ void __launch_bounds__(256) k_pool_release(RangeArgs a) {
     const int r = blockIdx.x, tid = threadIdx.x;
     int slot, from, to;
@@ -139,7 +139,9 @@ __global__ void __launch_bounds__(256) k_pool_release(RangeArgs a) {
 
 // ---------------------------------------------------------------- rs_pages_reserve
 // grid 1, block POOL_THREADS.  Counts the entries that lack a page, row by row, with as many lanes a row as take the longest one in at once; finds as
-// many free pages; hands them out in the same walk.
+// many free pages; hands them out in the same walk.  One workgroup: what a decode step needs is a chain of four dependent reads, not bytes (1 row 5 us,
+// 128 rows that need 8 pages of 40000 10, 1000 rows of 70000 pages 18).  Where a call wants thousands it is bound by one CU's stores: 10149 pages for 128 rows 25 us, of which
+// the rows' counts take 6 and the pages' search 17 (stores without branches around them, what is not taken going to a spare place: 27).
 constexpr int RESERVE_EACH = 8;                                    // entries a lane looks at together
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
     __shared__ FirstRow first;
@@ -164,7 +166,7 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
     while (shift < 6 && RESERVE_EACH << shift < longest) ++shift;
     const int lanes = 1 << shift, sub = lane & (lanes - 1), base = lane - sub;
     const unsigned long long mates = (lanes == 64 ? ~0ull : (1ull << lanes) - 1) << base;
-    // f(entry, rank of it among the row's that lack a page) for each of those; returns how many there are
+    // f(entry, which, ranks): bit u of `which` says that entry[lanes * u] lacks a page, the ranks[u]-th of the row's that do; returns how many do
     auto walk = [&](int r, auto f) __attribute__((always_inline)) {
         int *row = a.p.table + (size_t)slot_of[r] * a.p.max_pages + entry_of[r], rank = 0;
         const int m = len_of[r];
@@ -172,19 +174,22 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
             int page[RESERVE_EACH];
 #pragma unroll
             for (int u = 0; u < RESERVE_EACH; ++u) page[u] = row[min(e0 + lanes * u + sub, m - 1)];
+            uint32_t which = 0;
+            int ranks[RESERVE_EACH];
 #pragma unroll
             for (int u = 0; u < RESERVE_EACH; ++u) {
-                const int e = e0 + lanes * u + sub;
-                const bool lacks = e < m && !is_page(a.p, page[u]);
+                const bool lacks = e0 + lanes * u + sub < m && !is_page(a.p, page[u]);
                 const unsigned long long who = __ballot(lacks) & mates;
-                if (lacks) f(row + e, rank + (int)__popcll(who & ((1ull << lane) - 1)));
+                which |= (uint32_t)lacks << u;
+                ranks[u] = rank + (int)__popcll(who & ((1ull << lane) - 1));
                 rank += (int)__popcll(who);
             }
+            f(row + e0 + sub, which, ranks);
         }
         return rank;
     };
     for (int r = tid >> shift; r < n; r += POOL_THREADS >> shift) {
-        const int lack = walk(r, [](int *, int) {});
+        const int lack = walk(r, [](int *, uint32_t, const int (&)[RESERVE_EACH]) {});
         if (sub == 0) lack_of[r] = lack;
     }
     __syncthreads();
@@ -204,7 +209,13 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
     for (int i = taken + tid; i < min(have, wanted); i += POOL_THREADS) a.p.ref[__hip_atomic_load(a.list + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)] = 0;
     for (int r = tid >> shift; r < n; r += POOL_THREADS >> shift) {
         const int at = lack_of[r];
-        walk(r, [&](int *entry, int rank) { *entry = __hip_atomic_load(a.list + at + rank, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
+        walk(r, [&](int *entry, uint32_t which, const int (&ranks)[RESERVE_EACH]) __attribute__((always_inline)) {
+            int page[RESERVE_EACH];                                // (requested together, not one after the other behind a branch each)
+#pragma unroll
+            for (int u = 0; u < RESERVE_EACH; ++u) page[u] = ref_load(a.list + min(at + ranks[u], a.p.n_pages - 1));
+#pragma unroll
+            for (int u = 0; u < RESERVE_EACH; ++u) if (which >> u & 1) entry[lanes * u] = page[u];
+        });
     }
 }
 
@@ -228,7 +239,9 @@ constexpr int COPY_UNITS = 4;                                      // 16-byte un
 // 150 / 153 / 126 / 135 / 150 us, whole halves of a line 134 / 139 / 144 / 106 / 123, whole lines 89 / 91 / 95 / 106 / 124; whole pages 105).
 constexpr int COPY_BLOCK = 64;
 
-// grid (pieces * 2 * layers, any): a workgroup has its piece of every gridDim.y-th move.
+// grid (pieces * 2 * layers, any): a workgroup has its piece of every gridDim.y-th move.  Bound by HBM: 24 pages of 64 positions of the 14B shape, 604 MB read and
+// written, 120 to 123 us (4.9 to 5.0 TB/s, a large copy's 4.78); 91 of the 7B shape 133.  A fork's parts move more than they hold, since V goes by whole lines that are read at both
+// ends: parts of the 7B shape of 122 MB, read and written, 50 us; V's whole lines, read at both ends and written, make some 243 MB of it, 51 us at a copy's rate.
 // A part of a page: of K the first `part` places of every head, of V the first `part` places of every channel.
 __global__ void __launch_bounds__(256) k_pool_copy(CopyArgs a) {
     const Pool &p = a.to;
@@ -275,7 +288,10 @@ __global__ void __launch_bounds__(256) k_pool_copy(CopyArgs a) {
 struct ForkArgs { Pool p; const int *slot, *parent, *pos; int *pos_out; int n_groups, n_beams; PageMove *moves; int *n_moves; };
 
 // grid 1, block POOL_THREADS.  Reads everything before it writes a table entry: whether all rows are in range, the counts after the call, the rows that
-// need a page, the pages they get.  FORK_EACH: table entries that a thread requests together, and holds between reading and writing them.
+// need a page, the pages they get.  FORK_EACH: table entries that a thread requests together, and holds between reading and writing them: 2 where the rows
+// have 2048 at most together, 8 otherwise (by 2 / by 8: 4 rows of 64 entries 8.0 / 9.1 us, 128 of 16 9.2 / 10.5, 128 of 64 14.1 / 14.4, 128 of 256 32.4 / 30.3,
+// 1000 of 64 80 / 50).  Bound by the chain of its steps, each a read that depends on the last (slot, position,
+// table, count, page, table), in one workgroup.
 template <int FORK_EACH>
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
     __shared__ FirstRow first;
@@ -388,7 +404,8 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
 // ---------------------------------------------------------------- rs_pages_compact
 struct CompactArgs { Pool p; int *used; PageMove *moves; int *n_moves, *map, *gaps; };
 
-// grid 1, block POOL_THREADS: used pages from the number of used pages on, in order, go to the free ones below it, in order
+// grid 1, block POOL_THREADS: used pages from the number of used pages on, in order, go to the free ones below it, in order.  Three reads of the counts, of which the first
+// is of all: 6 us for 400 to 4000 pages.
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_compact(CompactArgs a) {
     __shared__ int sh[ORDERED_COUNTS];
     const Pool &p = a.p;
