@@ -79,7 +79,7 @@ rs_status launch_copy(const rs_page_pool *to, CopyArgs a, int moves_most, hipStr
     return RS_OK;
 }
 
-constexpr int BEAM_SLOTS = 1024;                                   // workgroups of k_beam_scan that run at once: four a CU, by its LDS and registers
+constexpr int BEAM_SLOTS = 1024;                                   // workgroups of k_beam_scan that run at once: four a CU, by its registers
 struct BeamScratch { BeamPlan plan; size_t sums, total; };
 BeamScratch beam_scratch(int n_groups, int n_beams, int vocab, int n_out) {
     BeamScratch s{};
