@@ -256,6 +256,22 @@ __device__ __forceinline__ void count_before(const uint32_t *x, int m, uint32_t 
     }
 }
 
+// How many of m keys are above hi:lo.  Their halves: in LDS, 16-byte aligned, with zeros up to a multiple of eight.  (Halves above first and, where some are equal,
+// the lower ones of those: as fast for fp32 logits, but bf16 has many equals: k_beam_scan of 72 rows of 109300 with 6 candidates 16.4 us this way, 18.6 that.)
+__device__ __forceinline__ int count_keys_before(const uint32_t *high, const uint32_t *low, int m, uint32_t hi, uint32_t lo) {
+    const unsigned long long mine = (unsigned long long)hi << 32 | lo;
+    int rank = 0;
+#pragma unroll 1
+    for (int j = 0; j < m; j += 8) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(high + j), b = *reinterpret_cast<const uint4 *>(high + j + 4);
+        const uint4 c = *reinterpret_cast<const uint4 *>(low + j), d = *reinterpret_cast<const uint4 *>(low + j + 4);
+        const uint32_t h[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, l[8] = {c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) rank += ((unsigned long long)h[k] << 32 | l[k]) > mine;
+    }
+    return rank;
+}
+
 // f(j) for those that equal it.
 template <typename F>
 __device__ __forceinline__ void for_equal(const uint32_t *x, int m, uint32_t mine, F f) {
@@ -270,37 +286,61 @@ __device__ __forceinline__ void for_equal(const uint32_t *x, int m, uint32_t min
     }
 }
 
-// A number that `keep` and few more of the workgroup's reach (all of them, if there are fewer): down from the largest, `most`, in growing steps, then halving.
-// Zeros are none.
+// A number that `keep` and few more of the workgroup's reach (all of them, if there are fewer): down from the largest, `most`, in growing steps, then what lies
+// between is divided, four numbers at a time, since each time costs a barrier (one at a time: k_beam_join of 13 groups of 2304 keys 11.1 us in the place of 10.1, of 39 groups of 150 7.7
+// in the place of 7.2).  Zeros are none.
 constexpr int BORDER_SLACK = 24;                                   // more than `keep` that are not worth another step
-constexpr int BORDER_STEPS = 9 + 32;
+constexpr int BORDER_AT_ONCE = 4;
+// three times down (2^16, 2^18 .. 2^30, all); then w -> w / 5 + 4 at most, 32 bits in 14 times, and 5 -> 1
+constexpr int BORDER_COUNTS = BORDER_AT_ONCE * (3 + 14 + 4);
 constexpr int SCAN_SHORT = 96;                                     // keys beyond n_out that are ordered without such a search
 template <int N>
-__device__ __forceinline__ uint32_t block_border(const uint32_t (&x)[N], uint32_t most, int keep, int *counts) {      // counts: BORDER_STEPS zeros in LDS
-    int step = 0;
-    auto reach = [&](uint32_t t) __attribute__((always_inline)) {
-        int c = 0;
+__device__ __forceinline__ uint32_t block_border(const uint32_t (&x)[N], uint32_t most, int keep, int *counts) {      // counts: BORDER_COUNTS zeros in LDS, 16-byte aligned
+    const int lane = threadIdx.x & 63;
+    auto reach = [&](const uint32_t (&t)[BORDER_AT_ONCE], int (&r)[BORDER_AT_ONCE]) __attribute__((always_inline)) {
+        int mine = 0;
 #pragma unroll
-        for (int k = 0; k < N; ++k) c += (int)__popcll(__ballot(x[k] >= t));
-        if ((threadIdx.x & 63) == 0) atomicAdd(&counts[step], c);
+        for (int q = 0; q < BORDER_AT_ONCE; ++q) {
+            int c = 0;
+#pragma unroll
+            for (int k = 0; k < N; ++k) c += (int)__popcll(__ballot(x[k] >= t[q]));
+            mine = lane == q ? c : mine;
+        }
+        if (lane < BORDER_AT_ONCE) atomicAdd(&counts[lane], mine);
         __syncthreads();
-        return counts[step++];
+        const int4 c = *reinterpret_cast<const int4 *>(counts);
+        r[0] = c.x; r[1] = c.y; r[2] = c.z; r[3] = c.w;
+        counts += BORDER_AT_ONCE;
     };
     uint32_t border = 1, above = most;
-    int reached = 0;
+    int reached = -1;
     if (most == 0) return 1;
 #pragma unroll 1
-    for (int d = 16;; d += 2) {
-        border = d < 32 && most > 1u << d ? most - (1u << d) : 1;
-        reached = reach(border);
-        if (reached >= keep || border == 1) break;
-        above = border;
+    for (int d = 16; reached < 0; d += 2 * BORDER_AT_ONCE) {
+        uint32_t t[BORDER_AT_ONCE];
+        int r[BORDER_AT_ONCE];
+#pragma unroll
+        for (int q = 0; q < BORDER_AT_ONCE; ++q) t[q] = d + 2 * q < 32 && most > 1u << (d + 2 * q & 31) ? most - (1u << (d + 2 * q & 31)) : 1;
+        reach(t, r);
+#pragma unroll
+        for (int q = 0; q < BORDER_AT_ONCE; ++q) {
+            if (reached >= 0) continue;
+            if (r[q] >= keep || t[q] == 1) { border = t[q]; reached = r[q]; } else above = t[q];
+        }
     }
 #pragma unroll 1
     while (reached > keep + BORDER_SLACK && above - border > 1) {
-        const uint32_t mid = border + (above - border) / 2;
-        const int r = reach(mid);
-        if (r >= keep) { border = mid; reached = r; } else above = mid;
+        const uint32_t step = max((above - border) / (BORDER_AT_ONCE + 1), 1u), last = above - 1;
+        uint32_t t[BORDER_AT_ONCE];
+        int r[BORDER_AT_ONCE];
+#pragma unroll
+        for (int q = 0; q < BORDER_AT_ONCE; ++q) t[q] = min(border + (q + 1) * step, last);
+        reach(t, r);
+#pragma unroll
+        for (int q = BORDER_AT_ONCE - 1; q >= 0; --q) {
+            if (r[q] < keep) above = t[q];
+            else { border = t[q]; reached = r[q]; break; }
+        }
     }
     return border;
 }
@@ -323,13 +363,14 @@ constexpr int BEAM_ROUND = 8;                                      // batches be
 struct ScanShared {
     union {
         unsigned long long list[BEAM_WAVES][BEAM_LIST];
-        struct { uint32_t order[BEAM_WAVES * BEAM_LIST + 8], rest[BEAM_WAVES * BEAM_LIST]; } kept;
+        struct { uint32_t order[BEAM_WAVES * BEAM_LIST + 8], rest[BEAM_WAVES * BEAM_LIST + 8]; } kept;
     };
     union { float of[BEAM_ROUND][64]; unsigned long long spare[BEAM_MAX]; } top[BEAM_WAVES];
     double z[BEAM_WAVES];
     float m[BEAM_WAVES];
     uint32_t border[BEAM_WAVES];
-    int bad[BEAM_WAVES], count[BEAM_WAVES], counts[BORDER_STEPS], n;
+    int bad[BEAM_WAVES], count[BEAM_WAVES], n;
+    alignas(16) int counts[BORDER_COUNTS];
 };
 
 // grid (parts, rows), block BEAM_THREADS.  Two borders near each other: the 78 MB of 128 rows of 152064 fp32 logits take 12.4 us as a streaming read (6.3 TB/s), and
@@ -442,7 +483,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     const float top = sum.finish(lane_top);
     const int bad = __any(sum.bad || !(lane_top < INFINITY));
     if (lane == 0) { sh.z[wave] = sum.z; sh.m[wave] = top; sh.bad[wave] = bad; sh.count[wave] = list.n; sh.border[wave] = border; }
-    if (tid < BORDER_STEPS) sh.counts[tid] = 0;
+    if (tid < BORDER_COUNTS) sh.counts[tid] = 0;
     if (tid == 0) sh.n = 0;
     __syncthreads();
     if (tid == 0) {
@@ -477,16 +518,11 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     }
     __syncthreads();
     const int m = sh.n;
-    if (tid < 8) sh.kept.order[m + tid] = 0;
+    if (tid < 8) sh.kept.order[m + tid] = sh.kept.rest[m + tid] = 0;
     __syncthreads();
     for (int i = tid; i < m; i += BEAM_THREADS) {
         const uint32_t order = sh.kept.order[i], rest = sh.kept.rest[i];
-        int rank = 0, equal = 0;
-        if (m <= a.n_out) rank = i;                                // (all of them, in any order)
-        else {
-            count_before(sh.kept.order, m, order, rank, equal);
-            if (equal > 1) for_equal(sh.kept.order, m, order, [&](int j) { rank += sh.kept.rest[j] > rest; });
-        }
+        const int rank = m <= a.n_out ? i : count_keys_before(sh.kept.order, sh.kept.rest, m, order, rest);      // (few: in any order)
         if (rank < a.n_out) to[rank] = (unsigned long long)order << 32 | rest;
     }
     for (int k = m + tid; k < a.n_out; k += BEAM_THREADS) to[k] = 0;
@@ -500,7 +536,7 @@ struct JoinShared {
     uint32_t high[JOIN_KEPT + 8];                                  // upper halves of the values
     unsigned long long value[JOIN_KEPT], key[JOIN_KEPT], edge_value, edge_key;
     uint32_t beam[JOIN_KEPT], edge_beam, most;
-    int counts[BORDER_STEPS];
+    alignas(16) int counts[BORDER_COUNTS];
     double row_z[BEAM_MAX], row_div[BEAM_MAX];
     float row_score[BEAM_MAX], row_scale[BEAM_MAX];
     int row_kind[BEAM_MAX], row_len[BEAM_MAX], n;
@@ -544,7 +580,7 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
         }
     }
     if (tid == 0) { sh.n = 0; sh.most = 0; }
-    if (tid < BORDER_STEPS) sh.counts[tid] = 0;
+    if (tid < BORDER_COUNTS) sh.counts[tid] = 0;
     __syncthreads();
     // ---- the items' values
     unsigned long long best = 0;
