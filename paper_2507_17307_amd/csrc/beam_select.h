@@ -375,7 +375,7 @@ struct ScanShared {
 
 // grid (parts, rows), block BEAM_THREADS.  Two borders near each other: the 78 MB of 128 rows of 152064 fp32 logits take 12.4 us as a streaming read (6.3 TB/s), and
 // some 25 vector operations a logit, 14 of them in double, four cycles each, 12 us.  24 us measured (3.2 TB/s): 15.5 without exponentials and candidates,
-// 4 each of those, the rest what reads and operations keep of each other.  bf16 with 32 candidates of 384 rows, 72 of them ended: 55 us,
+// 4 each of those, the rest what reads and operations keep of each other.  bf16 with 32 candidates of 384 rows, 72 of them ended: 54 us,
 // 95 MB and 30 us of operations.
 template <typename T>
 __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
