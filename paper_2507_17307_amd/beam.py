@@ -2,8 +2,9 @@
 
 Every prompt has n_beams slots of the model.  A step is one rs_decode_step for all beams of all prompts, rs_beam_select on its logits, and
 rs_pages_fork, after which each beam's page table row holds its parent's state: whole pages are shared, a part-filled last one is copied where two
-beams go on from it.  rs_pages_reserve then hands out what the next position needs.  All of it is enqueued; the host reads the steps'
-parents and tokens once, at the end (and, now and then, whether all beams have ended).
+beams go on from it.  A beam that ended, or is not there, takes over nothing: its logits are not looked at any more, so it holds no page, the decode step skips
+it, and what it wrote is in the steps' tokens.  rs_pages_reserve then hands out what the next position of the others needs.  All of it is
+enqueued; the host reads the steps' parents and tokens once, at the end (and, now and then, whether all beams have ended).
 """
 from __future__ import annotations
 
@@ -68,7 +69,9 @@ class BeamSearch:
     def _select(self) -> None:
         B.rs_beam_select(self.logits, self.n_prompts, self.n_beams, self.scale, self.score, self.token, self.eos, self.length_penalty, self.length, self.n_beams,
                          self.parent, self.token, self.score, self.length, self.scratch, self.bad_rows, self.stream)
-        B.rs_pages_fork(self.pool, self.n_prompts, self.n_beams, self.slot, self.parent, self.pos, self.pos, self.pool_scratch, self.flags, self.stream)
+        self.runs = (self.token >= 0) & (self.token != self.eos)
+        heir = torch.where(self.runs, self.parent, -1)
+        B.rs_pages_fork(self.pool, self.n_prompts, self.n_beams, self.slot, heir, self.pos, self.pos, self.pool_scratch, self.flags, self.stream)
 
     def generate(self, prompts: Sequence[Sequence[int]], n_tokens: int, check_every: int = 16) -> List[List[Beam]]:
         """The n_beams best continuations of every prompt by n_tokens tokens (or up to eos), best first.  check_every: how often, in steps,
@@ -96,7 +99,7 @@ class BeamSearch:
             done = n_tokens
             for t in range(n_tokens):
                 if t > 0:
-                    torch.add(self.pos, 1, out=self.end)
+                    torch.add(self.pos, self.runs, out=self.end)              # (rows that do not run: no position, no page, and so no decode step)
                     B.rs_pages_reserve(self.pool, self.rows, self.slot, self.pos, self.end, self.pool_scratch, self.flags)
                     B.rs_decode_step(self.model.handle, self.rows, self.slot, self.token, self.pos, None, 0.5, B.RS_LLM, self.record, self.logits, self.stream)
                     self.pos.copy_(self.end)
