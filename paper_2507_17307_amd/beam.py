@@ -25,7 +25,9 @@ class Beam:
 
 class BeamSearch:
     def __init__(self, model: B.PagedModel, n_prompts: int, n_beams: int, eos: int = -1, length_penalty: float = 0.0, logit_scale: float = 1.0):
-        """Takes over the model's pages (PagedModel.page_pool).  n_prompts * n_beams <= the model's max_seqs and max_rows."""
+        """Takes over the model's pages (PagedModel.page_pool).  n_prompts * n_beams <= the model's max_seqs and max_rows.  The search's
+        slots are 0 .. n_prompts * n_beams - 1.  Every generate empties the slots of all searches made on the model (the most rows of any); it leaves
+        the slots beyond them and their pages as they are."""
         cfg, rows = model.cfg, n_prompts * n_beams
         if n_prompts < 1 or n_beams < 1 or rows > cfg.max_seqs or rows > cfg.max_rows:
             raise ValueError(f"{n_prompts} x {n_beams} beams do not fit {cfg.max_seqs} slots / {cfg.max_rows} rows")
@@ -37,19 +39,20 @@ class BeamSearch:
         self.model, self.n_prompts, self.n_beams, self.eos, self.length_penalty, self.rows = model, n_prompts, n_beams, eos, length_penalty, rows
         dev = model.device
         self.pool = model.page_pool()
+        model.search_slots = max(model.search_slots, rows)
         self.stream = torch.cuda.Stream(device=dev)          # a capturable (non-default) stream: repeated steps are replayed as a graph
 
         def ints(n: int, value: int = 0) -> torch.Tensor:
             return torch.full((n,), value, dtype=torch.int32, device=dev)
         # buffers of a step, at fixed addresses
-        self.slot = torch.arange(rows, dtype=torch.int32, device=dev)
+        self.slot = torch.arange(cfg.max_seqs, dtype=torch.int32, device=dev)
         self.pos, self.end, self.token, self.length, self.parent = ints(rows), ints(rows), ints(rows), ints(rows), ints(rows)
         self.score = torch.zeros(rows, device=dev)
         self.scale = torch.full((rows,), logit_scale, device=dev)
         self.logits = torch.zeros(rows, cfg.vocab, device=dev)
         self.record = B.new_route_out(rows, dev)
         self.flags, self.bad_rows = ints(rows), ints(rows)
-        self.all_slots, self.everything = torch.arange(cfg.max_seqs, dtype=torch.int32, device=dev), ints(cfg.max_seqs, model.page_size * model.page_table.shape[1])
+        self.everything = ints(cfg.max_seqs, model.page_size * model.page_table.shape[1])
         self.pool_scratch = torch.empty(B.rs_pages_scratch_bytes(self.pool, rows), dtype=torch.uint8, device=dev)
         self.scratch = torch.empty(n, dtype=torch.uint8, device=dev)
         torch.cuda.synchronize(dev)
@@ -87,9 +90,8 @@ class BeamSearch:
         tokens = torch.zeros_like(parents)
         self.stream.wait_stream(torch.cuda.current_stream(self.model.device))
         with torch.cuda.stream(self.stream):
-            # the slots give back what they hold; only the first beam of every prompt is there yet
-            for at in range(0, cfg.max_seqs, 1024):
-                B.rs_pages_release(self.pool, min(1024, cfg.max_seqs - at), self.all_slots[at:], None, self.everything[at:])
+            # the searches' slots give back what they hold; only the first beam of every prompt is there yet
+            B.rs_pages_release(self.pool, self.model.search_slots, self.slot, None, self.everything)
             self.flags.zero_(), self.bad_rows.zero_(), self.pos.zero_(), self.length.zero_(), self.token.fill_(-1)
             self.score.fill_(float("-inf"))
             self.score[::nb] = 0.0

@@ -686,6 +686,7 @@ class PagedModel(Model):
         self._free = list(range(n_pages - 1, -1, -1))
         self._held: List[List[int]] = [[] for _ in range(max_seqs)]
         self._pool: Optional[PagePool] = None
+        self.search_slots = 0                                    # slots 0 .. search_slots - 1 are beam searches'
         self.handle = rs_create_model_paged(self.cfg, weights, self.cache_struct, self.workspace)
 
     def page_pool(self) -> PagePool:
