@@ -518,10 +518,11 @@ rs_status rs_create_model_paged(const rs_config *cfg, const rs_weights *weights,
  * d_logit_scale[r] * logits; a logit of -inf is no candidate.  A beam whose last token is
  * eos has ended: its logits are not read, it is its own only candidate, with token
  * eos and its score and length unchanged.
- *   d_logits        DEVICE [n_groups * n_beams][vocab], dtype RS_F32 or RS_BF16, rows row_stride elements apart
+ *   d_logits        DEVICE [n_groups * n_beams][vocab], rows row_stride elements apart
+ *   dtype           of the logits, RS_F32 or RS_BF16; RS_SCORES_F64 or-ed in: d_score and d_score_out are double
  *   n_beams, n_out  1 .. 64;  n_groups * n_beams <= 65535
  *   d_logit_scale   DEVICE fp32 [rows] or NULL (= 1): > 0 and finite
- *   d_score         DEVICE fp32 [rows]: sum of log probabilities; -inf: the beam is not there (its logits are not read)
+ *   d_score         DEVICE fp32 or double [rows]: sum of log probabilities; -inf: the beam is not there (its logits are not read)
  *   d_last          DEVICE int32 [rows] or NULL: the beams' last tokens;  eos: a token or -1 (no beam ends)
  *   length_penalty  0 .. 30: candidates are ordered by score / length^length_penalty, length at least 1
  *   d_len           DEVICE int32 [rows] or NULL (with length_penalty 0): tokens of the beams so far, 0 .. 2^31 - 2; a continuation has one more
@@ -534,14 +535,19 @@ rs_status rs_create_model_paged(const rs_config *cfg, const rs_weights *weights,
  *                   graph replays that overlap must not share it
  * Fewer candidates than n_out: the rest have parent -1, token -1, score -inf and length 0.  Equals (in double, in which sums are held
  * and candidates compared) go to the lower beam, within a beam to the larger logit and then to the lower token.
+ * Log probabilities are off by some 1e-12.  fp32 scores are rounded once a call, by up to 2^-24 of their value (below fp32's range to -inf), and a search that feeds
+ * them back adds these up: after n steps beams are told apart to n 2^-24 of the score, where double scores keep 1e-12 n.  Also, with fp32 scores
+ * ln sum exp x is one double, off by 2^-53 of the largest |x|: a row all of whose logits are the type's lowest value (a mask that leaves nothing
+ * is to be of -inf) has tokens of log probability 0 in the place of -ln vocab; with double scores it is right for logits of any size.
  * With n_out == n_beams outputs may be the inputs of the same kind (d_score_out = d_score, d_token = d_last, d_len_out = d_len).
  * Errors: RS_EINVAL, RS_ECAPACITY (more than 65535 rows), RS_EHIP. */
+#define RS_SCORES_F64 256
 size_t    rs_beam_select_scratch_bytes(int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t n_out);
 rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype,
                          int32_t n_groups, int32_t n_beams, int32_t vocab,
-                         const float *d_logit_scale, const float *d_score, const int32_t *d_last, int32_t eos,
+                         const float *d_logit_scale, const void *d_score, const int32_t *d_last, int32_t eos,
                          double length_penalty, const int32_t *d_len, int32_t n_out,
-                         int32_t *d_parent, int32_t *d_token, float *d_score_out, int32_t *d_len_out,
+                         int32_t *d_parent, int32_t *d_token, void *d_score_out, int32_t *d_len_out,
                          uint32_t *d_flags, void *d_scratch, size_t scratch_bytes, void *stream);
 
 /* Pages that several sequences hold together: the pages of all layers as in

@@ -47,7 +47,7 @@ class BeamSearch:
         # buffers of a step, at fixed addresses
         self.slot = torch.arange(cfg.max_seqs, dtype=torch.int32, device=dev)
         self.pos, self.end, self.token, self.length, self.parent = ints(rows), ints(rows), ints(rows), ints(rows), ints(rows)
-        self.score = torch.zeros(rows, device=dev)
+        self.score = torch.zeros(rows, dtype=torch.float64, device=dev)      # (sums over all steps: fp32 would round each of them)
         self.scale = torch.full((rows,), logit_scale, device=dev)
         self.logits = torch.zeros(rows, cfg.vocab, device=dev)
         self.record = B.new_route_out(rows, dev)

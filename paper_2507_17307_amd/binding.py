@@ -281,7 +281,7 @@ def rs_set_sampling(handle: int, enabled: bool, key: int = 0) -> None:
 
 
 # ------------------------------------------------------------------ caches in pages
-RS_F32, RS_BF16 = 0, 1
+RS_F32, RS_BF16, RS_SCORES_F64 = 0, 1, 256
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BY_PARTS = range(3)
 _ROW_TYPES = {torch.float32: RS_F32, torch.bfloat16: RS_BF16}
 _INT_TYPES = (torch.int32, torch.uint32)
@@ -430,12 +430,12 @@ def rs_beam_select_scratch_bytes(n_groups: int, n_beams: int, vocab: int, n_out:
     return lib.rs_beam_select_scratch_bytes(n_groups, n_beams, vocab, n_out)
 
 
-def _floats(name: str, t: Optional[torch.Tensor], n: int, device: int) -> Optional[int]:
-    """Address of n fp32 numbers."""
+def _floats(name: str, t: Optional[torch.Tensor], n: int, device: int, kind: torch.dtype = torch.float32) -> Optional[int]:
+    """Address of n numbers of a type, fp32 by default."""
     if t is None:
         return None
-    if t.dtype is not torch.float32 or not t.is_contiguous() or t.numel() < n or t.get_device() != device:
-        raise ValueError(f"{name} must hold {n} contiguous fp32 numbers on {_device_name(device)}")
+    if t.dtype is not kind or not t.is_contiguous() or t.numel() < n or t.get_device() != device:
+        raise ValueError(f"{name} must hold {n} contiguous {kind} numbers on {_device_name(device)}")
     return t.data_ptr()
 
 
@@ -448,16 +448,18 @@ def _scratch(t: torch.Tensor, device: int):
 
 def rs_beam_select(d_logits: torch.Tensor, n_groups: int, n_beams: int, d_logit_scale, d_score, d_last, eos: int, length_penalty: float, d_len, n_out: int,
                    d_parent, d_token, d_score_out, d_len_out, d_scratch, d_flags=None, stream=None) -> None:
-    """d_logits: fp32 or bf16 [rows, vocab] with the values of a row side by side, at least n_groups * n_beams rows; d_score, d_logit_scale (or None): fp32;
-    d_last, d_len (or None): int32 of a row each; d_parent, d_token, d_len_out (or None): int32, d_score_out: fp32 of n_groups * n_out."""
+    """d_logits: fp32 or bf16 [rows, vocab] with the values of a row side by side, at least n_groups * n_beams rows; d_logit_scale (or None): fp32,
+    d_score: fp32 or fp64, d_last, d_len (or None): int32 of a row each; d_parent, d_token, d_len_out (or None): int32, d_score_out: d_score's type, of n_groups * n_out."""
     dev, rows, n = d_logits.get_device(), n_groups * n_beams, n_groups * n_out
     if d_logits.dtype not in _ROW_TYPES or d_logits.dim() != 2 or d_logits.shape[0] < rows or d_logits.stride(1) != 1 and d_logits.shape[1] != 1:
         raise ValueError(f"d_logits must be fp32 or bf16 [{rows}, vocab] with the values of a row side by side, not {d_logits.dtype} {tuple(d_logits.shape)}")
     vocab = d_logits.shape[1]
     stride = d_logits.stride(0) if d_logits.shape[0] != 1 else vocab
-    _check(lib.rs_beam_select(d_logits.data_ptr(), stride, _ROW_TYPES[d_logits.dtype], n_groups, n_beams, vocab, _floats("d_logit_scale", d_logit_scale, rows, dev),
-                              _floats("d_score", d_score, rows, dev), _ints("d_last", d_last, rows, dev), eos, length_penalty, _ints("d_len", d_len, rows, dev), n_out,
-                              _ints("d_parent", d_parent, n, dev), _ints("d_token", d_token, n, dev), _floats("d_score_out", d_score_out, n, dev),
+    wide = d_score is not None and d_score.dtype is torch.float64
+    kind = torch.float64 if wide else torch.float32
+    _check(lib.rs_beam_select(d_logits.data_ptr(), stride, _ROW_TYPES[d_logits.dtype] + (RS_SCORES_F64 if wide else 0), n_groups, n_beams, vocab, _floats("d_logit_scale", d_logit_scale, rows, dev),
+                              _floats("d_score", d_score, rows, dev, kind), _ints("d_last", d_last, rows, dev), eos, length_penalty, _ints("d_len", d_len, rows, dev), n_out,
+                              _ints("d_parent", d_parent, n, dev), _ints("d_token", d_token, n, dev), _floats("d_score_out", d_score_out, n, dev, kind),
                               _ints("d_len_out", d_len_out, n, dev), _ints("d_flags", d_flags, rows, dev), *_scratch(d_scratch, dev), _device_stream(dev, stream)))
 
 

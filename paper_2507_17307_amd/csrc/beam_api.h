@@ -80,13 +80,14 @@ rs_status launch_copy(const rs_page_pool *to, CopyArgs a, int moves_most, hipStr
 }
 
 constexpr int BEAM_SLOTS = 1024;                                   // workgroups of k_beam_scan that run at once: four a CU, by its registers
-struct BeamScratch { BeamPlan plan; size_t sums, total; };
+struct BeamScratch { BeamPlan plan; size_t sums, scores, total; };
 BeamScratch beam_scratch(int n_groups, int n_beams, int vocab, int n_out) {
     BeamScratch s{};
     s.plan = beam_plan(n_groups * n_beams, n_beams, vocab, n_out, BEAM_SLOTS);
     const size_t parts = (size_t)n_groups * n_beams * s.plan.parts;
     s.sums = align_up(parts * n_out * 8);
-    s.total = s.sums + align_up(parts * sizeof(BeamSum));
+    s.scores = s.sums + align_up(parts * sizeof(BeamSum));
+    s.total = s.scores + align_up((size_t)n_groups * n_beams * 8);
     return s;
 }
 
@@ -101,11 +102,13 @@ size_t rs_beam_select_scratch_bytes(int32_t n_groups, int32_t n_beams, int32_t v
 }
 
 rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype, int32_t n_groups, int32_t n_beams, int32_t vocab,
-                         const float *d_logit_scale, const float *d_score, const int32_t *d_last, int32_t eos, double length_penalty,
-                         const int32_t *d_len, int32_t n_out, int32_t *d_parent, int32_t *d_token, float *d_score_out, int32_t *d_len_out,
+                         const float *d_logit_scale, const void *d_score, const int32_t *d_last, int32_t eos, double length_penalty,
+                         const int32_t *d_len, int32_t n_out, int32_t *d_parent, int32_t *d_token, void *d_score_out, int32_t *d_len_out,
                          uint32_t *d_flags, void *d_scratch, size_t scratch_bytes, void *stream) {
     if (!d_logits || !d_score || !d_parent || !d_token || !d_score_out || !d_scratch) return fail(RS_EINVAL, "null argument");
-    if (dtype != RS_F32 && dtype != RS_BF16) return fail(RS_EINVAL, "dtype must be RS_F32 or RS_BF16");
+    const bool wide = dtype >= 0 && (dtype & RS_SCORES_F64);
+    if (wide) dtype -= RS_SCORES_F64;
+    if (dtype != RS_F32 && dtype != RS_BF16) return fail(RS_EINVAL, "dtype must be RS_F32 or RS_BF16, with or without RS_SCORES_F64");
     if (n_groups >= 1 && n_beams >= 1 && (long long)n_groups * n_beams > 65535) return fail(RS_ECAPACITY, "%lld rows exceed 65535", (long long)n_groups * n_beams);
     const size_t need = rs_beam_select_scratch_bytes(n_groups, n_beams, vocab, n_out);
     if (!need) return RS_EINVAL;
@@ -116,6 +119,7 @@ rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype
     if ((uintptr_t)d_logits % (dtype == RS_F32 ? 4 : 2)) return fail(RS_EINVAL, "logits are not aligned to their type");
     if (((uintptr_t)d_logit_scale | (uintptr_t)d_score | (uintptr_t)d_last | (uintptr_t)d_len | (uintptr_t)d_parent | (uintptr_t)d_token | (uintptr_t)d_score_out |
          (uintptr_t)d_len_out | (uintptr_t)d_flags) % 4) return fail(RS_EINVAL, "row arguments and outputs must be 4-byte aligned");
+    if (wide && ((uintptr_t)d_score | (uintptr_t)d_score_out) % 8) return fail(RS_EINVAL, "double scores must be 8-byte aligned");
     if ((uintptr_t)d_scratch % ALIGN) return fail(RS_EINVAL, "scratch must be 256-byte aligned");
     if (scratch_bytes < need) return fail(RS_EINVAL, "scratch of %zu bytes is smaller than the %zu needed", scratch_bytes, need);
     const int rows = n_groups * n_beams;
@@ -124,8 +128,8 @@ rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype
     BeamArgs a{};
     a.logits = d_logits; a.stride = (size_t)row_stride; a.scale = d_logit_scale; a.score = d_score; a.last = d_last; a.len = d_len;
     a.eos = eos; a.n_beams = n_beams; a.vocab = vocab; a.n_out = n_out; a.alpha = length_penalty; a.parts = p.plan.parts;
-    a.parent = d_parent; a.token = d_token; a.len_out = d_len_out; a.score_out = d_score_out; a.flags = d_flags;
-    a.keys = (unsigned long long *)scratch; a.sums = (BeamSum *)(scratch + p.sums);
+    a.parent = d_parent; a.token = d_token; a.len_out = d_len_out; a.score_out = d_score_out; a.wide = wide; a.flags = d_flags;
+    a.keys = (unsigned long long *)scratch; a.sums = (BeamSum *)(scratch + p.sums); a.scores = (double *)(scratch + p.scores);
     hipStream_t st = (hipStream_t)stream;
     const dim3 grid(a.parts, rows);
     if (dtype == RS_F32) hipLaunchKernelGGL((k_beam_scan<float>), grid, dim3(BEAM_THREADS), 0, st, a);

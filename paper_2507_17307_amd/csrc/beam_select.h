@@ -2,7 +2,8 @@
 //
 // The continuation of beam b by token t is worth score_b + (x_t - ln Z_b), x = scale * logits, Z = sum e^x.  Neighbours in the order of a vocabulary,
 // and more so across beams, may be nearer than fp32 sums can tell, so the sum of exponentials and all that is compared across beams are double; within a
-// row the order is that of the logits themselves.
+// row the order is that of the logits themselves.  The scores that go from call to call are double or fp32, as the caller holds them: fp32 ones are rounded
+// once a call, which adds up over a search.
 //
 // k_beam_scan makes one pass over the logits.  A wave takes 1024 of them at a time, 16 a lane: their exponentials go into its sum, the largest of each lane's 16
 // into LDS.  After eight batches it sets a border that n_out of its values at least reach, from what the lanes had as their largest, and only lanes
@@ -23,15 +24,18 @@ struct BeamSum { double z; float m; int bad; };                    // sum of 2^(
 
 struct BeamArgs {
     const void *logits; size_t stride;
-    const float *scale, *score;
+    const float *scale;
+    const void *score;                                             // double if `wide`, else float; so is score_out
     const int *last, *len;
     int eos, n_beams, vocab, n_out, parts;                         // parts * n_beams * n_out <= BEAM_KEYS
     double alpha;
     int *parent, *token, *len_out;
-    float *score_out;
+    void *score_out;
+    int wide;                                                      // 0 or 1
     unsigned int *flags;
     unsigned long long *keys;                                      // [row][part][n_out]; 0: none
     BeamSum *sums;                                                 // [row][part]
+    double *scores;                                                // [row]: as double, whatever the caller's are
 };
 
 // 2^f for |f| <= 1/2, to 1.1e-12: degree eight through 2^f at the nine Chebyshev nodes, of which 0 is one.  2^0 is exactly 1, so that a token that makes up
@@ -108,9 +112,15 @@ __device__ __forceinline__ T group_all(T v, int shift, F f) {
 
 // What a row takes part with: its vocabulary, its end, or nothing.
 enum { BEAM_NONE, BEAM_ENDED, BEAM_RUNS };
-struct BeamRow { float score, scale; int last, len; };
-__device__ __forceinline__ BeamRow beam_row(const BeamArgs &a, int row) {
-    return {a.score[row], a.scale ? a.scale[row] : 1.f, a.last ? a.last[row] : -2, a.len ? a.len[row] : 0};
+struct BeamRow { double score; float scale; int last, len; };
+__device__ __forceinline__ double beam_score(const BeamArgs &a, int row) {
+    // (both words of a double are asked for at once, which for a float are one and the same: no branch before the load)
+    const int *word = (const int *)a.score + ((size_t)row << a.wide);
+    const int low = word[0], high = word[a.wide];
+    return a.wide ? __hiloint2double(high, low) : (double)__int_as_float(low);
+}
+__device__ __forceinline__ BeamRow beam_row(const BeamArgs &a, int row, double score) {
+    return {score, a.scale ? a.scale[row] : 1.f, a.last ? a.last[row] : -2, a.len ? a.len[row] : 0};
 }
 __device__ __forceinline__ int beam_kind(const BeamRow &r, int eos, unsigned int &flag) {
     flag = 0;
@@ -382,8 +392,9 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     constexpr int UNIT = BeamUnit<T>::N, PIECES = 16 / UNIT, WAVE_UNITS = 64 * PIECES;
     __shared__ ScanShared sh;
     const int row = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const BeamRow r = beam_row(a, row);
+    const BeamRow r = beam_row(a, row, beam_score(a, row));
     unsigned int flag;
+    if (part == 0 && tid == 0) a.scores[row] = r.score;
     const int kind = beam_kind(r, a.eos, flag);
     if (flag && part == 0 && tid == 0 && a.flags) atomicOr(a.flags + row, flag);
     if (kind != BEAM_RUNS) return;
@@ -532,14 +543,15 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
 constexpr int JOIN_EACH = 4;                                       // keys a thread
 constexpr int JOIN_KEPT = 1024;                                    // items that are kept for ordering
 
+struct alignas(16) JoinRow { double score, top, z, div; float scale; int kind, len; };      // (side by side: three reads of 16 bytes an item)
+
 struct JoinShared {
     uint32_t high[JOIN_KEPT + 8];                                  // upper halves of the values
     unsigned long long value[JOIN_KEPT], key[JOIN_KEPT], edge_value, edge_key;
     uint32_t beam[JOIN_KEPT], edge_beam, most;
     alignas(16) int counts[BORDER_COUNTS];
-    double row_z[BEAM_MAX], row_div[BEAM_MAX];
-    float row_score[BEAM_MAX], row_scale[BEAM_MAX];
-    int row_kind[BEAM_MAX], row_len[BEAM_MAX], n;
+    JoinRow row[BEAM_MAX];
+    int n;
 };
 
 // The order of items: larger values first, of equals the lower beam, in one beam the larger key.
@@ -561,7 +573,7 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
     const int shift = parts <= 1 ? 0 : 32 - __clz(parts - 1), rows_at_once = threads >> shift, sub = lane & ((1 << shift) - 1);
     for (int b0 = 0; b0 < a.n_beams; b0 += rows_at_once) {
         const int b = b0 + (tid >> shift), row = g * a.n_beams + min(b, a.n_beams - 1);
-        const BeamRow r = beam_row(a, row);
+        const BeamRow r = beam_row(a, row, a.scores[row]);
         const BeamSum s = a.sums[(size_t)row * parts + min(sub, parts - 1)];       // (of rows that do not run: anything)
         unsigned int flag;
         int kind = beam_kind(r, a.eos, flag);
@@ -574,24 +586,36 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
             if (bad && a.flags) atomicOr(a.flags + row, RS_FLAG_NONFINITE);
             if (kind == BEAM_RUNS && (bad || !(top > -INFINITY))) kind = BEAM_NONE;
             const int len = r.len + (kind == BEAM_RUNS);
-            sh.row_kind[b] = kind; sh.row_len[b] = len; sh.row_score[b] = r.score; sh.row_scale[b] = r.scale;
-            sh.row_z[b] = kind == BEAM_RUNS ? log(z) + (double)top * (double)r.scale : 0.0;
-            sh.row_div[b] = a.alpha > 0.0 ? pow((double)max(len, 1), a.alpha) : 1.0;
+            sh.row[b] = {r.score, kind == BEAM_RUNS ? (double)top * (double)r.scale : 0.0, kind == BEAM_RUNS ? z : 1.0, 1.0, r.scale, kind, len};
         }
     }
     if (tid == 0) { sh.n = 0; sh.most = 0; }
     if (tid < BORDER_COUNTS) sh.counts[tid] = 0;
     __syncthreads();
+    // ln Z = ln z + top.  With double scores top is taken from a logit first, so that ln z is kept however large the logits are; with fp32 scores ln Z is one
+    // double, in which ln z is off by 2^-53 of top: less than their own rounding for logits up to 2^29 times the score.
+    if (tid < a.n_beams) {
+        const double top = sh.row[tid].top, ln_z = log(sh.row[tid].z);
+        sh.row[tid].top = a.wide ? top : 0.0;
+        sh.row[tid].z = a.wide ? ln_z : ln_z + top;
+        if (a.alpha > 0.0) sh.row[tid].div = pow((double)max(sh.row[tid].len, 1), a.alpha);
+    }
+    __syncthreads();
+    auto worth = [](const JoinRow &r, unsigned long long item) __attribute__((always_inline)) {
+        const double v = r.score + (((double)key_logit(item) * (double)r.scale - r.top) - r.z);
+        return r.kind == BEAM_RUNS ? v : r.score;
+    };
     // ---- the items' values
     unsigned long long best = 0;
 #pragma unroll
     for (int k = 0; k < JOIN_EACH; ++k) {
-        const int i = tid + threads * k, b = min(i / per_row, a.n_beams - 1), kind = i < n ? sh.row_kind[b] : BEAM_NONE;
+        const int i = tid + threads * k, b = min(i / per_row, a.n_beams - 1);
+        const JoinRow r = sh.row[b];
+        const int kind = i < n ? r.kind : BEAM_NONE;
         value[k] = 0;
-        double v = sh.row_score[b];
-        if (kind == BEAM_RUNS) v += (double)key_logit(key[k]) * (double)sh.row_scale[b] - sh.row_z[b];
+        const double v = worth(r, key[k]);
         if (kind == BEAM_ENDED) key[k] = i == b * per_row ? 1ull << 32 | (uint32_t)~a.eos : 0;
-        if (kind != BEAM_NONE && key[k]) value[k] = double_order(a.alpha > 0.0 ? v / sh.row_div[b] : v);
+        if (kind != BEAM_NONE && key[k]) value[k] = double_order(a.alpha > 0.0 ? v / r.div : v);
         best = value[k] > best ? value[k] : best;
     }
     const uint32_t wave_most = wave_max_u32((uint32_t)(best >> 32));
@@ -643,12 +667,16 @@ __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
         if (equal > 1)
             for_equal(sh.high, m, high, [&](int j) { rank += item_before(sh.value[j], sh.beam[j], sh.key[j], v, b, x); });
         if (rank < a.n_out) {
-            a.parent[o + rank] = (int)b; a.token[o + rank] = key_token(x); a.score_out[o + rank] = (float)(order_double(v) * sh.row_div[b]);
-            if (a.len_out) a.len_out[o + rank] = sh.row_len[b];
+            // (where lengths count: not the quotient times the divisor, so that an ended beam's score stays as it is, bit by bit)
+            const double score = a.alpha > 0.0 ? worth(sh.row[b], x) : order_double(v);
+            a.parent[o + rank] = (int)b; a.token[o + rank] = key_token(x);
+            if (a.wide) ((double *)a.score_out)[o + rank] = score; else ((float *)a.score_out)[o + rank] = (float)score;
+            if (a.len_out) a.len_out[o + rank] = sh.row[b].len;
         }
     }
     for (int k = m + tid; k < a.n_out; k += threads) {
-        a.parent[o + k] = -1; a.token[o + k] = -1; a.score_out[o + k] = -INFINITY;
+        a.parent[o + k] = -1; a.token[o + k] = -1;
+        if (a.wide) ((double *)a.score_out)[o + k] = -INFINITY; else ((float *)a.score_out)[o + k] = -INFINITY;
         if (a.len_out) a.len_out[o + k] = 0;
     }
 }
