@@ -399,21 +399,16 @@ __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     if (flag && part == 0 && tid == 0 && a.flags) atomicOr(a.flags + row, flag);
     if (kind != BEAM_RUNS) return;
     const T *x = (const T *)a.logits + (size_t)row * a.stride;
-    // values before the first 16-byte border, whole pieces from there, values behind the last piece
-    const int before = min(a.vocab, (int)((16 - (uintptr_t)x % 16) % 16 / sizeof(T))), pieces = (a.vocab - before) / UNIT, behind = a.vocab - before - pieces * UNIT;
-    // the values before are the first part's, those behind the last one's: a batch of their own, one a lane
-    const int head = part == 0 ? before : 0, ends = wave == 0 ? head + (part == a.parts - 1 ? behind : 0) : 0;
+    const BeamShare share = beam_share((int)((uintptr_t)x % 16), (int)sizeof(T), a.vocab, a.parts, part, wave);
+    const int before = share.before, ends = share.ends, unit_0 = share.unit_0, unit_end = share.unit_end, unit_a = unit_0 + lane;
     const u32x4_t *px = reinterpret_cast<const u32x4_t *>(x + before);
     WaveSum sum;
     sum.init(r.scale);
     WaveList list{sh.list[wave], sh.top[wave].spare, 0, 0, a.n_out};
     uint32_t border = 0;
     float v[16], least = -FLT_MAX, lo_top = -INFINITY, hi_top = -INFINITY;
-    // the pieces are shared evenly by as many waves as they fill: a wave with a few of them would have no border
-    const int waves = max(1, min(a.parts * BEAM_WAVES, (pieces + WAVE_UNITS - 1) / WAVE_UNITS)), own = (pieces + waves - 1) / waves;
-    const int unit_0 = min(pieces, (part * BEAM_WAVES + wave) * own), unit_end = min(pieces, unit_0 + own), unit_a = unit_0 + lane;
-    const int whole = (unit_end - unit_0 + WAVE_UNITS - 1) / WAVE_UNITS, n_batches = whole + (ends > 0);
-    const int end_token = lane < head ? lane : a.vocab - behind + (lane - head);
+    const int whole = (unit_end - unit_0 + WAVE_UNITS - 1) / WAVE_UNITS, n_batches = whole + (ends > 0);      // (the single values: a batch of their own, one a lane)
+    const int end_token = beam_end_token(share, lane);
     const float end_value = lane < ends ? BeamUnit<T>::one(x + end_token) : -INFINITY;
     // this lane's pieces of batch b < whole, and their values
     auto fetch = [&](int b, u32x4_t (&w)[PIECES]) __attribute__((always_inline)) {
