@@ -1,0 +1,116 @@
+"""Calls on pools of pages where a workgroup has several moves, or a row several strides of entries, against plain lists."""
+import random
+
+import pytest
+import torch
+
+from test_gpu_page_pool import Both, ints
+
+pytestmark = pytest.mark.gpu
+
+# page size, channels, heads, layers.  The copying kernel has about 4096 workgroups, which stand side by side over a page's K and V of all layers (pieces of 8192 values):
+# 96 and 48 of them, so that 43 and 86 moves are made at once.
+SHAPES = [(16, 32, 1, 48), (64, 128, 8, 3)]
+
+
+def shape(b):
+    return b.k.shape[0] * 2 * -(-b.k[0, 0].numel() // 8192)
+
+
+@pytest.mark.parametrize("page, hd, heads, layers", SHAPES)
+def test_more_copies_than_are_made_at_once(page, hd, heads, layers):
+    import paper_2507_17307_amd as P
+    n = 100
+    b, rng = Both(1, 1, 2 * n + 5, page, layers, heads, hd, seed=page), random.Random(page)
+    assert -(-4096 // shape(b)) < n
+    order = rng.sample(range(2 * n + 5), 2 * n)
+    src, dst = order[:n], order[n:]
+    src[40], dst[60] = -1, 2 * n + 5                                          # (pairs that are skipped)
+    flags = ints([0] * n)
+    P.rs_pages_copy(b.pool, b.pool, n, ints(src), ints(dst), flags)
+    for s, d in zip(src, dst):
+        if s >= 0 and d < 2 * n + 5:
+            b.model.k[:, d], b.model.v[:, d] = b.model.k[:, s], b.model.v[:, s]
+    b.same()
+    assert [i for i, f in enumerate(flags.tolist()) if f] == [40, 60] and set(flags.tolist()) == {0, 16}
+
+
+@pytest.mark.parametrize("page, hd, heads, layers", [(16, 32, 1, 48), (128, 32, 1, 48), (64, 128, 8, 3)])
+def test_more_parts_than_are_copied_at_once(page, hd, heads, layers):
+    """Four beams of 34 groups that all go on from the first: 102 copies of last pages of all lengths."""
+    groups, beams = 34, 4
+    n, rng = groups * beams, random.Random(page + heads)
+    b = Both(n, 3, 5 * groups + 8, page, layers, heads, hd, seed=page + 1)
+    assert -(-4096 // shape(b)) < 3 * groups
+    slot, held = rng.sample(range(n), n), [page + rng.randrange(1, page) for _ in range(groups)]
+    pos = [held[r // beams] if r % beams == 0 else 0 for r in range(n)]
+    b.reserve(slot, None, pos)
+    assert not any(b.fork(beams, slot, [0] * n, pos))
+    b.same()
+
+
+@pytest.mark.parametrize("page, hd, heads, layers", SHAPES)
+def test_more_pages_compacted_than_are_moved_at_once(page, hd, heads, layers):
+    n_pages = 220
+    b, rng = Both(4, 60, n_pages, page, layers, heads, hd, seed=page + 2), random.Random(page + 7)
+    for i, p in enumerate(list(range(0, 20)) + rng.sample(range(110, n_pages), 95)):
+        b.model.table[i % 4][i // 4] = p
+        b.model.ref[p] += 1
+    b.push()
+    assert -(-4096 // shape(b)) < sum(p >= 115 and r > 0 for p, r in enumerate(b.model.ref))
+    b.compact()
+    b.same()
+
+
+@pytest.mark.parametrize("max_pages", [600, 1025, 2049, 5000])
+def test_reserve_and_release_long_rows(max_pages):
+    """More entries of a row than its lanes take at once (512), in rows that hold some of them already."""
+    rng, page = random.Random(max_pages), 16
+    b = Both(5, max_pages, 3 * max_pages, page, contents=False)
+    for j in rng.sample(range(max_pages), max_pages // 3):
+        b.model.table[1][j] = 2 * max_pages + j
+        b.model.ref[2 * max_pages + j] = 1
+    b.push()
+    assert b.reserve([1, 3, 0], [0, 7, page * (max_pages - 550)], [page * max_pages, page * max_pages - 5, page * max_pages]) == [0, 0, 0]
+    b.same()
+    b.release([3, 1], [page * 3 + 1, 0], [page * max_pages, page * (max_pages - 20)])
+    b.same()
+    # two rows get all of theirs, and the third, for which the pages do not suffice, none
+    assert b.reserve([4, 2, 3], None, [page * max_pages] * 3) == [0, 0, 128]
+    b.same()
+
+
+@pytest.mark.parametrize("groups, beams, max_pages", [(1, 1, 1025), (1, 1, 2048), (1, 2, 1024), (1, 3, 1500), (2, 3, 2049), (1, 4, 5000)])
+def test_fork_of_long_rows(groups, beams, max_pages):
+    """Tables of more entries a row than the workgroup has threads, by two and by eight entries a thread."""
+    n, page, rng = groups * beams, 16, random.Random(max_pages + groups)
+    b = Both(n + 2, max_pages, max_pages * (groups + 1) + 40 * n, page, layers=1, heads=1, seed=beams)
+    slot = rng.sample(range(n + 2), n)
+    held = [page * max_pages - rng.randrange(1, 400) for _ in range(groups)]
+    pos = [held[r // beams] if r % beams == 0 else 0 for r in range(n)]
+    b.reserve(slot, None, pos)
+    b.same()
+    assert not any(b.fork(beams, slot, [0] * n, pos))
+    b.same()
+    pos = [held[r // beams] - 30 * (r % beams) for r in range(n)]            # some are taken back into whole pages that others hold
+    assert not any(b.fork(beams, slot, [(r * 7 + 1) % beams for r in range(n)], pos))
+    b.same()
+    # a slot beside the call's shares all of the first row's pages: its last one is copied
+    spare = next(s for s in range(n + 2) if s not in slot)
+    b.model.table[spare] = list(b.model.table[slot[0]])
+    for p in b.model.table[spare]:
+        if p >= 0:
+            b.model.ref[p] += 1
+    b.push()
+    assert not any(b.fork(beams, slot, [r % beams for r in range(n)], [min(p, page * max_pages) for p in pos]))
+    b.same()
+
+
+def test_fork_without_pages_puts_long_rows_counts_back():
+    page, max_pages = 16, 1500
+    b = Both(4, max_pages, max_pages + 2, page, layers=1, heads=1)
+    b.reserve([0], None, [page * max_pages - 3])
+    before = list(b.model.ref)
+    assert b.fork(4, [0, 1, 2, 3], [0] * 4, [page * max_pages - 3, 0, 0, 0]) == [128] * 4
+    b.same()
+    assert b.model.ref == before and torch.equal(b.ref.cpu(), torch.tensor(before, dtype=torch.int32))
