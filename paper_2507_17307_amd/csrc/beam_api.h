@@ -186,7 +186,7 @@ rs_status rs_pages_fork(const rs_page_pool *pool, int32_t n_groups, int32_t n_be
     a.p = make_pool(pool, d_flags); a.slot = d_slot; a.parent = d_parent; a.pos = d_pos; a.pos_out = d_pos_out; a.n_groups = n_groups; a.n_beams = n_beams;
     a.n_moves = (int *)d_scratch; a.moves = (PageMove *)((unsigned char *)d_scratch + pool_scratch(pool, n).moves);
     hipStream_t st = (hipStream_t)stream;
-    if ((long long)n * pool->max_pages <= 2 * POOL_THREADS) hipLaunchKernelGGL((k_pool_fork<2>), dim3(1), dim3(POOL_THREADS), 0, st, a);
+    if ((long long)n * pool->max_pages <= FORK_FEW_ENTRIES) hipLaunchKernelGGL((k_pool_fork<FORK_FEW>), dim3(1), dim3(POOL_THREADS), 0, st, a);
     else hipLaunchKernelGGL((k_pool_fork<8>), dim3(1), dim3(POOL_THREADS), 0, st, a);
     RS_LAUNCHED("pool_fork");
     CopyArgs c{};

@@ -288,10 +288,12 @@ __global__ void __launch_bounds__(256) k_pool_copy(CopyArgs a) {
 struct ForkArgs { Pool p; const int *slot, *parent, *pos; int *pos_out; int n_groups, n_beams; PageMove *moves; int *n_moves; };
 
 // grid 1, block POOL_THREADS.  Reads everything before it writes a table entry: whether all rows are in range, the counts after the call, the rows that
-// need a page, the pages they get.  FORK_EACH: table entries that a thread requests together, and holds between reading and writing them: 2 where the rows
-// have 2048 at most together, 8 otherwise (by 2 / by 8: 4 rows of 64 entries 8.0 / 9.1 us, 128 of 16 9.2 / 10.5, 128 of 64 14.1 / 14.4, 128 of 256 32.4 / 30.3,
-// 1000 of 64 80 / 50).  Bound by the chain of its steps, each a read that depends on the last (slot, position,
+// need a page, the pages they get.  FORK_EACH: table entries that a thread requests together, and holds between reading and writing them: FORK_FEW where the
+// rows have FORK_FEW_ENTRIES at most together, 8 otherwise.  us of a call without copies by 2 / by 8, rows whose entries all change: 4 rows of 64 entries 7.1 / 8.6, 128 of 16
+// 8.6 / 9.9, 4096 entries (4 to 512 rows) 9.9 to 10.2 / 10.8 to 11.1, 8192 (4 to 512 rows) 13.0 to 13.4 / 13.2 to 13.5, 1000 rows of 8 14.9 / 14.0, 128 of 128 19.8 / 18.6, 1000 of
+// 64 92 / 51.  Bound by the chain of its steps, each a read that depends on the last (slot, position,
 // table, count, page, table), in one workgroup.
+constexpr int FORK_FEW = 2, FORK_FEW_ENTRIES = 4096;
 template <int FORK_EACH>
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
     __shared__ FirstRow first;

@@ -114,3 +114,17 @@ def test_fork_without_pages_puts_long_rows_counts_back():
     assert b.fork(4, [0, 1, 2, 3], [0] * 4, [page * max_pages - 3, 0, 0, 0]) == [128] * 4
     b.same()
     assert b.model.ref == before and torch.equal(b.ref.cpu(), torch.tensor(before, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("groups, beams, max_pages", [(128, 8, 4), (20, 50, 3), (1, 64, 64), (16, 4, 64), (1, 4, 1024), (13, 5, 63), (1, 4, 1025), (16, 64, 5)])
+def test_fork_around_4096_entries(groups, beams, max_pages):
+    """Where the kernel goes from two to eight entries a thread, from many short rows to few long ones; beams change places, share and end."""
+    n, page, rng = groups * beams, 16, random.Random(max_pages)
+    b = Both(n, max_pages, n * max_pages + n, page, layers=1, heads=1, seed=n)
+    slot, pos = rng.sample(range(n), n), [rng.randrange(0, page * max_pages + 1) for _ in range(n)]
+    b.reserve(slot, None, pos)
+    for turn in range(2):
+        parent = [(r + 1) % beams if turn == 0 else rng.randrange(-1, beams) for r in range(n)]
+        assert not any(b.fork(beams, slot, parent, pos))
+        b.same(turn)
+        pos = [pos[r // beams * beams + p] if p >= 0 else 0 for r, p in enumerate(parent)]
