@@ -34,8 +34,8 @@ class BeamSearch:
         if not -1 <= eos < cfg.vocab or not 0 <= length_penalty <= 30 or not 0 < logit_scale < float("inf"):
             raise ValueError("need eos -1 or a token, length_penalty in 0..30 and a positive logit_scale")
         n = B.rs_beam_select_scratch_bytes(n_prompts, n_beams, cfg.vocab, n_beams)
-        if n == 0 or rows > 1024:
-            raise ValueError(f"more than 64 beams of a prompt or 1024 of all: {n_prompts} x {n_beams}")
+        if n == 0:
+            raise ValueError(f"more than 64 beams of a prompt: {n_prompts} x {n_beams}")
         self.model, self.n_prompts, self.n_beams, self.eos, self.length_penalty, self.rows = model, n_prompts, n_beams, eos, length_penalty, rows
         dev = model.device
         self.pool = model.page_pool()
