@@ -46,7 +46,7 @@ class BeamSearch:
             return torch.full((n,), value, dtype=torch.int32, device=dev)
         # buffers of a step, at fixed addresses
         self.slot = torch.arange(cfg.max_seqs, dtype=torch.int32, device=dev)
-        self.pos, self.end, self.token, self.length, self.parent = ints(rows), ints(rows), ints(rows), ints(rows), ints(rows)
+        self.pos, self.end, self.token, self.length = ints(rows), ints(rows), ints(rows), ints(rows)
         self.score = torch.zeros(rows, dtype=torch.float64, device=dev)      # (sums over all steps: fp32 would round each of them)
         self.scale = torch.full((rows,), logit_scale, device=dev)
         self.logits = torch.zeros(rows, cfg.vocab, device=dev)
@@ -69,12 +69,12 @@ class BeamSearch:
                 B.rs_catchup_prefill(model.handle, 1, len(chunk), self.slot[r:], span, span[len(chunk):], span[len(chunk) + 2:], None, 0.5, B.RS_LLM,
                                      self.record, logits, self.stream)
 
-    def _select(self) -> None:
+    def _select(self, parent: torch.Tensor) -> None:
+        """parent: where the parents of the step go."""
         B.rs_beam_select(self.logits, self.n_prompts, self.n_beams, self.scale, self.score, self.token, self.eos, self.length_penalty, self.length, self.n_beams,
-                         self.parent, self.token, self.score, self.length, self.scratch, self.bad_rows, self.stream)
-        self.runs = (self.token >= 0) & (self.token != self.eos)
-        heir = torch.where(self.runs, self.parent, -1)
-        B.rs_pages_fork(self.pool, self.n_prompts, self.n_beams, self.slot, heir, self.pos, self.pos, self.pool_scratch, self.flags, self.stream)
+                         parent, self.token, self.score, self.length, self.scratch, self.bad_rows, self.stream)
+        heir = parent if self.eos < 0 else parent.masked_fill(self.token == self.eos, -1)      # (a beam that is not there has parent -1 already)
+        B.rs_pages_fork(self.pool, self.n_prompts, self.n_beams, self.slot, heir, self.end, self.pos, self.pool_scratch, self.flags, self.stream)
 
     def generate(self, prompts: Sequence[Sequence[int]], n_tokens: int, check_every: int = 16) -> List[List[Beam]]:
         """The n_beams best continuations of every prompt by n_tokens tokens (or up to eos), best first.  check_every: how often, in steps,
@@ -96,17 +96,17 @@ class BeamSearch:
             self.score.fill_(float("-inf"))
             self.score[::nb] = 0.0
             self.pos[::nb] = torch.tensor([len(p) for p in prompts], dtype=torch.int32, device=self.model.device)
+            self.end.copy_(self.pos)
             B.rs_pages_reserve(self.pool, self.rows, self.slot, None, self.pos, self.pool_scratch, self.flags)
             self._prefill(prompts)
             done = n_tokens
             for t in range(n_tokens):
                 if t > 0:
-                    torch.add(self.pos, self.runs, out=self.end)              # (rows that do not run: no position, no page, and so no decode step)
+                    torch.add(self.pos, self.pos > 0, out=self.end)           # (rows that do not run hold 0 positions and get none: no page, and so no decode step)
                     B.rs_pages_reserve(self.pool, self.rows, self.slot, self.pos, self.end, self.pool_scratch, self.flags)
                     B.rs_decode_step(self.model.handle, self.rows, self.slot, self.token, self.pos, None, 0.5, B.RS_LLM, self.record, self.logits, self.stream)
-                    self.pos.copy_(self.end)
-                self._select()
-                parents[t], tokens[t] = self.parent, self.token
+                self._select(parents[t])
+                tokens[t] = self.token
                 if self.eos >= 0 and check_every and (t + 1) % check_every == 0 and bool(((self.token == self.eos) | (self.token < 0)).all()):
                     done = t + 1
                     break
