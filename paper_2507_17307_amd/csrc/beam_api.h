@@ -68,8 +68,8 @@ rs_status check_pool_rows(int32_t n, const void *a, const void *b, const void *c
     return RS_OK;
 }
 
-// Workgroups of k_pool_copy, about: those without a move of their own cost their start (4096 / 16384: 300 moves of the smallest pages, compacted, 17 / 22 us; 24
-// pages of the 14B shape 123 / 126; 91 of the 7B shape, compacted, 146 / 142).
+// Workgroups of k_pool_copy, about: those without a move of their own cost their start (4096 / 16384, us of a call: 300 of the smallest pages, compacted, 18 / 23; 24
+// pages of the 14B shape 126 / 121; 91 of the 7B shape, compacted, 149 / 145).
 constexpr int COPY_WGS = 4096;
 rs_status launch_copy(const rs_page_pool *to, CopyArgs a, int moves_most, hipStream_t st) {
     a.pieces = (int)page_pieces(to);
@@ -135,7 +135,7 @@ rs_status rs_beam_select(const void *d_logits, int64_t row_stride, int32_t dtype
     if (dtype == RS_F32) hipLaunchKernelGGL((k_beam_scan<float>), grid, dim3(BEAM_THREADS), 0, st, a);
     else hipLaunchKernelGGL((k_beam_scan<uint16_t>), grid, dim3(BEAM_THREADS), 0, st, a);
     RS_LAUNCHED("beam_scan");
-    const int keys = n_beams * a.parts * n_out;                    // (the smallest block that holds them: 608 keys 5.6 us with 256 or 512 threads, 6.7 with 1024)
+    const int keys = n_beams * a.parts * n_out;                    // (the smallest block that holds them: 608 keys, a call 12.6 us with 256 threads, 12.7 with 512, 13.6 with 1024)
     hipLaunchKernelGGL(k_beam_join, dim3(n_groups), dim3(keys <= 256 * JOIN_EACH ? 256 : keys <= 512 * JOIN_EACH ? 512 : 1024), 0, st, a);
     RS_LAUNCHED("beam_join");
     return RS_OK;

@@ -14,8 +14,8 @@ constexpr int BEAM_KEYS = 4096;                                    // keys of a 
 struct BeamPlan { int parts, batches; };                           // workgroups of a row; batches of each wave of one by which it was chosen (beam_share deals them out)
 
 // The parts with the least of rounds * (batches + BEAM_START): `slots` workgroups run at once, and one costs as much as three batches before its first and behind its
-// last one.  us of k_beam_scan, 152064 fp32 logits a row, of 24 x 16 rows with 32 candidates in 3 / 4 / 5 / 8 parts 75 / 71 / 71 / 83 (the rule takes 2 of
-// 19 batches or 5 of 8, which cost the same by it), of 32 x 4 with 4 in 4 / 8 / 10 / 13 / 19 parts 25.7 / 24.5 / 26.7 / 27.3 / 29.3.
+// last one.  us of a call, 152064 fp32 logits a row: 24 x 16 rows with 32 candidates in 2 / 3 / 4 / 5 / 8 parts 64 / 70 / 69 / 72 / 76 (2 of 19 batches
+// and 5 of 8 cost the same by the rule, which takes the 5), 32 x 4 with 4 in 4 / 8 / 10 / 13 / 19 parts 30.4 / 30.4 / 32.5 / 33.0 / 35.2 (it takes 8).
 constexpr int BEAM_START = 3;
 RS_HD BeamPlan beam_plan(int rows, int n_beams, int vocab, int n_out, int slots) {
     const long long all = ((long long)vocab + BEAM_BATCH * BEAM_WAVES - 1) / (BEAM_BATCH * BEAM_WAVES);      // parts of one batch a wave

@@ -40,7 +40,7 @@ struct BeamArgs {
 
 // 2^f for |f| <= 1/2, to 1.1e-12: degree eight through 2^f at the nine Chebyshev nodes, of which 0 is one.  2^0 is exactly 1, so that a token that makes up
 // the whole sum has log probability 0, and equal scores stay equal.  Scores nearer than ln Z's error may change places.  (Degree seven through 1 at 0 is off
-// by 1.1e-10: k_beam_scan of 128 rows of 152064 fp32 logits takes 25.0 us in the place of 25.5.)
+// by 1.1e-10: a call on 128 rows of 152064 fp32 logits takes 28.6 us in the place of 29.2.)
 __device__ __forceinline__ double exp2_part(double f) {
     double p = 1.3255224887502117e-06;
     p = fma(p, f, 1.531007940254368e-05); p = fma(p, f, 0.0001540345585240991); p = fma(p, f, 0.0013333450567999414); p = fma(p, f, 0.009618129159402628);
@@ -266,8 +266,8 @@ __device__ __forceinline__ void count_before(const uint32_t *x, int m, uint32_t 
     }
 }
 
-// How many of m keys are above hi:lo.  Their halves: in LDS, 16-byte aligned, with zeros up to a multiple of eight.  (Halves above first and, where some are equal,
-// the lower ones of those: as fast for fp32 logits, but bf16 has many equals: k_beam_scan of 72 rows of 109300 with 6 candidates 16.4 us this way, 18.6 that.)
+// How many of m keys are above hi:lo.  Their halves: in LDS, 16-byte aligned, with zeros up to a multiple of eight.  (Whole keys, since
+// bf16 logits have many equal upper halves.)
 __device__ __forceinline__ int count_keys_before(const uint32_t *high, const uint32_t *low, int m, uint32_t hi, uint32_t lo) {
     const unsigned long long mine = (unsigned long long)hi << 32 | lo;
     int rank = 0;
@@ -297,8 +297,7 @@ __device__ __forceinline__ void for_equal(const uint32_t *x, int m, uint32_t min
 }
 
 // A number that `keep` and few more of the workgroup's reach (all of them, if there are fewer): down from the largest, `most`, in growing steps, then what lies
-// between is divided, four numbers at a time, since each time costs a barrier (one at a time: k_beam_join of 13 groups of 2304 keys 11.1 us in the place of 10.1, of 39 groups of 150 7.7
-// in the place of 7.2).  Zeros are none.
+// between is divided, four numbers at a time, since each time costs a barrier.  Zeros are none.
 constexpr int BORDER_SLACK = 24;                                   // more than `keep` that are not worth another step
 constexpr int BORDER_AT_ONCE = 4;
 // three times down (2^16, 2^18 .. 2^30, all); then w -> w / 5 + 4 at most, 32 bits in 14 times, and 5 -> 1
@@ -384,9 +383,9 @@ struct ScanShared {
 };
 
 // grid (parts, rows), block BEAM_THREADS.  Two borders near each other: the 78 MB of 128 rows of 152064 fp32 logits take 12.4 us as a streaming read (6.3 TB/s), and
-// some 25 vector operations a logit, 14 of them in double, four cycles each, 12 us.  24 us measured (3.2 TB/s): 15.5 without exponentials and candidates,
-// 4 each of those, the rest what reads and operations keep of each other.  bf16 with 32 candidates of 384 rows, 72 of them ended: 54 us,
-// 95 MB and 30 us of operations.
+// some 25 vector operations a logit, 14 of them in double, four cycles each, 12 us.  25 us measured (3.1 TB/s).  The whole call takes
+// 29.7 us, 25.1 without candidates and 20.4 without candidates and exponentials: the parts add up, since the workgroups of the one round there is start, read and end
+// together.  bf16 with 32 candidates of 384 rows, a sixth of them ended: 74 us, 58 and 30.
 template <typename T>
 __global__ void __launch_bounds__(BEAM_THREADS) k_beam_scan(BeamArgs a) {
     constexpr int UNIT = BeamUnit<T>::N, PIECES = 16 / UNIT, WAVE_UNITS = 64 * PIECES;
@@ -554,8 +553,8 @@ __device__ __forceinline__ bool item_before(unsigned long long v, uint32_t b, un
     return v > v2 || (v == v2 && (b < b2 || (b == b2 && k > k2)));
 }
 
-// grid groups, block 256, 512 or 1024: JOIN_EACH keys a thread.  Bound by the chain of its steps (keys and sums, logarithm, values, border, order): 4 to 6 us of 608 to
-// 1024 keys a group, 10 of 2560.
+// grid groups, block 256, 512 or 1024: JOIN_EACH keys a thread.  Bound by the chain of its steps (keys and sums, logarithm, values, border, order): 5.8 us of 608 to
+// 1024 keys a group, 11 of 2560.
 __global__ void __launch_bounds__(1024) k_beam_join(BeamArgs a) {
     __shared__ JoinShared sh;
     const int g = blockIdx.x, tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, parts = a.parts;

@@ -119,7 +119,7 @@ __device__ __forceinline__ bool pool_range(const RangeArgs &a, int r, int &slot,
     return slot >= 0 && slot < a.p.n_slots && from >= 0 && to >= from && to <= (long long)a.p.max_pages << a.p.page_shift;
 }
 
-// grid n, block 256: the entries whose pages lie wholly in the row's range.  A launch and one chain entry -> count: 3.2 us for 128 rows of up to 125 entries.
+// grid n, block 256: the entries whose pages lie wholly in the row's range.  A launch and one chain entry -> count: 1.9 us for a row, 4.7 for 128 rows of up to 125 entries.
 __global__ void __launch_bounds__(256) k_pool_release(RangeArgs a) {
     const int r = blockIdx.x, tid = threadIdx.x;
     int slot, from, to;
@@ -139,9 +139,9 @@ __global__ void __launch_bounds__(256) k_pool_release(RangeArgs a) {
 
 // ---------------------------------------------------------------- rs_pages_reserve
 // grid 1, block POOL_THREADS.  Counts the entries that lack a page, row by row, with as many lanes a row as take the longest one in at once; finds as
-// many free pages; hands them out in the same walk.  One workgroup: what a decode step needs is a chain of four dependent reads, not bytes (1 row 5 us,
-// 128 rows that need 8 pages of 40000 10, 1000 rows of 70000 pages 18).  Where a call wants thousands it is bound by one CU's stores: 10149 pages for 128 rows 25 us, of which
-// the rows' counts take 6 and the pages' search 17 (stores without branches around them, what is not taken going to a spare place: 27).
+// many free pages; hands them out in the same walk.  One workgroup: what a decode step needs is a chain of four dependent reads, not bytes (1 row 3 us,
+// 128 rows that need 8 pages behind 35800 held ones 19, 1000 rows that need 63 behind 44000 31).  Where a call wants thousands it is bound by one CU's stores: 10149 pages
+// for 128 rows 24 us.
 constexpr int RESERVE_EACH = 8;                                    // entries a lane looks at together
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
     __shared__ FirstRow first;
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_reserve(RangeArgs a) {
     int wanted;
     const int mine = tid < n ? lack_of[tid] : 0, before = block_scan(mine, sh, wanted);
     if (!wanted) return;
-    // (a page is counted where it is found, side by side with its neighbours; 16000 counts set where the entries are written took 7 us more)
+    // (a page is counted where it is found, side by side with its neighbours, which entries are not)
     const int have = ordered(a.p.n_pages, wanted, sh, [&](int i) { return a.p.ref[i]; }, [](int count) { return count == 0; },
                              [&](int i, int rank) { if (rank < wanted) { a.list[rank] = i; a.p.ref[i] = 1; } });
     if (tid < n) {
@@ -235,13 +235,13 @@ struct CopyArgs {
 
 constexpr int COPY_UNITS = 4;                                      // 16-byte units a thread
 // Places of a channel of V that are written together: 128 bytes.  Writing part of such a line costs more than twice as much as all of it, so the places
-// behind the part are read from where they go to and written again (70 parts of pages of the 7B shape, 8 / 16 / 24 / 40 / 56 of 64 places: the part alone
-// 150 / 153 / 126 / 135 / 150 us, whole halves of a line 134 / 139 / 144 / 106 / 123, whole lines 89 / 91 / 95 / 106 / 124; whole pages 105).
+// behind the part are read from where they go to and written again (a fork with 70 parts of pages of the 7B shape, 8 / 16 / 24 / 40 / 56 of 64 places: the part
+// alone 163 / 166 / 137 / 137 / 149 us, whole halves of a line 144 / 149 / 153 / 121 / 141, whole lines 99 / 101 / 105 / 117 / 136; 70 whole pages copied 104).
 constexpr int COPY_BLOCK = 64;
 
 // grid (pieces * 2 * layers, any): a workgroup has its piece of every gridDim.y-th move.  Bound by HBM: 24 pages of 64 positions of the 14B shape, 604 MB read and
-// written, 120 to 123 us (4.9 to 5.0 TB/s, a large copy's 4.78); 91 of the 7B shape 133.  A fork's parts move more than they hold, since V goes by whole lines that are read at both
-// ends: parts of the 7B shape of 122 MB, read and written, 50 us; V's whole lines, read at both ends and written, make some 243 MB of it, 51 us at a copy's rate.
+// written, 124 us (4.9 TB/s, a large copy's 4.78); 90 of the 7B shape 136.  A fork's parts move more than they hold, since V goes by whole lines that are read at both
+// ends: parts of the 7B shape of 122 MB, read and written, 51 us; V's whole lines, read at both ends and written, make some 243 MB of it, 51 us at a copy's rate.
 // A part of a page: of K the first `part` places of every head, of V the first `part` places of every channel.
 __global__ void __launch_bounds__(256) k_pool_copy(CopyArgs a) {
     const Pool &p = a.to;
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(POOL_THREADS) k_pool_fork(ForkArgs a) {
 struct CompactArgs { Pool p; int *used; PageMove *moves; int *n_moves, *map, *gaps; };
 
 // grid 1, block POOL_THREADS: used pages from the number of used pages on, in order, go to the free ones below it, in order.  Three reads of the counts, of which the first
-// is of all: 6 us for 400 to 4000 pages.
+// is of all: 6.5 us for 400 pages, 7.7 for 4000.
 __global__ void __launch_bounds__(POOL_THREADS) k_pool_compact(CompactArgs a) {
     __shared__ int sh[ORDERED_COUNTS];
     const Pool &p = a.p;
