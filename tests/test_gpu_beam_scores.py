@@ -174,3 +174,35 @@ def test_a_search_adds_its_scores_up_in_double(monkeypatch):
                 total += float(torch.log_softmax(seen[step][6 * g + at] * 0.5, 0)[search.trace[1][step][r]])
             assert total < -100 and abs(got[g][b].score - total) <= 120 * STEP
     model.close()
+
+
+def test_calls_of_both_score_types_replayed_side_by_side():
+    """Two captured calls, one with double and one with fp32 scores, in place, replayed on two streams at once; every replay against the 64-bit loop of what it started from."""
+    import paper_2507_17307_amd as P
+    g = torch.Generator().manual_seed(21)
+    x = [torch.randn(12, 30011, generator=g).cuda() * 3 for _ in range(2)]
+    scores = [(-400 * torch.rand(12, generator=g, dtype=torch.float64)).to(t).cuda() for t in (torch.float64, torch.float32)]
+    states = [(torch.ones(12, dtype=torch.int32).cuda(), torch.full((12,), 9, dtype=torch.int32).cuda(), torch.zeros(12, dtype=torch.int32).cuda(),
+               torch.full((P.rs_beam_select_scratch_bytes(3, 4, 30011, 4),), 255, dtype=torch.uint8).cuda()) for _ in range(2)]
+    graphs, streams = [], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for logits, score, (last, length, parent, scratch), stream in zip(x, scores, states, streams):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            P.rs_beam_select(logits, 3, 4, None, score, last, 5, 0.5, length, 4, parent, last, score, length, scratch)
+        graphs.append(graph)
+    for step in range(4):
+        for logits in x:
+            logits.mul_(0.9).add_(torch.randn(12, 1, generator=g).cuda())
+        wants = [beam.select(logits.cpu(), 3, 4, score.cpu(), 4, last=s[0].cpu(), eos=5, alpha=0.5, length=s[1].cpu()) for logits, score, s in zip(x, scores, states)]
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for k, (want, score, s) in enumerate(zip(wants, scores, states)):
+            assert s[2].tolist() == want[0] and s[0].tolist() == want[1] and s[1].tolist() == want[3], (step, k)
+            if k == 0:
+                assert float((score.cpu() - want[2]).abs().max()) <= STEP
+            else:
+                beam.check_scores(score, want[2])
